@@ -25,8 +25,8 @@
  * enqueued.  HIP failures return ASPIS_ERR_DEVICE.  aspis_last_error()
  * returns a message for the calling thread's last failure.
  *
- * Asynchrony: aspis_detect and aspis_aggregate only enqueue work on the
- * stream.  aspis_clique is host code.  aspis_detect_aggregate synchronises
+ * Asynchrony: aspis_detect, aspis_aggregate and the norm, clipping and
+ * update calls only enqueue work on the stream.  aspis_clique is host code.  aspis_detect_aggregate synchronises
  * the stream (it needs the agreement graph on the host) and returns with
  * its work complete.
  *
@@ -394,6 +394,142 @@ aspis_status aspis_simulate(int32_t K, int32_t r, int32_t q, aspis_attack attack
  * 0 <= q <= K. */
 aspis_status aspis_detox(int32_t K, int32_t r, int32_t q, aspis_attack attack,
                          int64_t *distorted_groups, double *epsilon);
+
+/* ---- norms, clipping and the model update -----------------------------
+ *
+ * What a training run does with gradients around the detect-and-aggregate
+ * step: a worker clips each file's gradient before it uploads it, a server
+ * bounds what one replica can add, and the aggregated gradient is clipped by
+ * its global norm and applied to the model.
+ *
+ * Clip coefficient of a norm N and a bound M (max_norm >= 0):
+ *   c = 1 where N <= M or M = inf, else M / N.
+ * An infinite norm gives c = 0 (finite elements become 0, infinite ones
+ * NaN), a NaN norm c = NaN.  c = 1 returns every element's own bits.
+ *
+ * Sums of squares are held in fp64 (the square of every f32 fits), and the
+ * product c * x is rounded once to f32 and once more to a 16-bit result.
+ * Results depend on the values and the sizes alone -- not on addresses,
+ * alignment, strides or the device's number of compute units -- so that
+ * workers clipping the same gradient upload the same bits.
+ *
+ * All entry points below only enqueue work on the stream.  None allocates;
+ * scratch comes through the caller's workspace, which needs no particular
+ * contents.  Calls that overlap must not share workspaces or outputs. */
+typedef enum { ASPIS_F32 = 0, ASPIS_BF16 = 1, ASPIS_F16 = 2 } aspis_dtype;
+
+/* A list of tensors, as the kernels read it: an array of aspis_chunk that
+ * aspis_tensor_table writes and the caller copies to the device (16-byte
+ * aligned).  It names the tensors' addresses: a table is good for as long as
+ * they stay where they are.  Tensors are contiguous spans of elements and
+ * need no more alignment than their type. */
+typedef struct {
+    uint64_t addr;
+    int32_t n;
+    int32_t info;
+} aspis_chunk;
+
+/* Entries of the table of `count` tensors with numel[i] >= 0 elements, and
+ * how many of them are chunks (n_chunks of the calls below; it depends on
+ * the sizes alone).  -1 on invalid arguments or more than 2^31-1 entries. */
+int64_t aspis_tensor_chunks(const int64_t *numel, int32_t count);
+int64_t aspis_tensor_entries(const int64_t *numel, int32_t count);
+
+/* Writes the table (host memory, caller-owned, cap >= aspis_tensor_entries):
+ * tensor i has numel[i] elements of type dtype[i] (aspis_dtype) at device
+ * address ptr[i] (may be NULL where numel[i] is 0).
+ * Errors: INVALID_ARG (negative count or numel, unknown type, NULL or
+ * misaligned address), OVERFLOW, BUFFER_SMALL (nothing written). */
+aspis_status aspis_tensor_table(const void *const *ptr, const int64_t *numel,
+                                const int32_t *dtype, int32_t count,
+                                aspis_chunk *table, int64_t cap);
+
+/* Bytes of workspace aspis_grad_norm, aspis_clip_grads and the updates need
+ * for a list of n_chunks chunks; 0 on an invalid argument. */
+size_t aspis_norm_workspace(int64_t n_chunks);
+
+/* The global L2 norm of a list of tensors.
+ *   table      device, as aspis_tensor_table wrote it
+ *   n_chunks, n_tensors   of that list (both may be 0: the norm is 0)
+ *   sumsq      device double [1]: the sum of squares (all-reduce it where
+ *              ranks hold shards of one model)
+ *   norm       device float [1]: its square root
+ *   each       device float [n_tensors], every tensor's own norm, or NULL
+ *   workspace  device, >= aspis_norm_workspace(n_chunks) bytes, 16-aligned */
+aspis_status aspis_grad_norm(const aspis_chunk *table, int64_t n_chunks,
+                             int32_t n_tensors, double *sumsq, float *norm,
+                             float *each, void *workspace, size_t ws_bytes,
+                             void *stream);
+
+#define ASPIS_CLIP_HAVE_SUMSQ 1u      /* sumsq holds the sum of squares (of
+                                         all ranks): no norm pass          */
+#define ASPIS_CLIP_SKIP_NONFINITE 2u  /* updates: leave everything as it is
+                                         where the norm is not finite      */
+
+/* Clips a list of tensors by its global norm: out = c * x, rounded to the
+ * type.  out_table NULL (or table itself) clips in place; otherwise it lists
+ * tensors of the same sizes and types, disjoint from the inputs.  Writes
+ * sumsq (unless ASPIS_CLIP_HAVE_SUMSQ) and norm, the norm before clipping. */
+aspis_status aspis_clip_grads(const aspis_chunk *table, const aspis_chunk *out_table,
+                              int64_t n_chunks, double max_norm, double *sumsq,
+                              float *norm, uint32_t flags, void *workspace,
+                              size_t ws_bytes, void *stream);
+
+/* Rows: x holds `rows` rows of d elements, ld >= d elements from one row's
+ * start to the next (a replica tensor [f][r][d] has f*r rows, a worker's
+ * upload [l][d] has l).  aspis_row_workspace: bytes of workspace for them
+ * (may be 0; SIZE_MAX on invalid arguments). */
+size_t aspis_row_workspace(int64_t rows, int64_t d, aspis_dtype dtype);
+
+/* norms[i] = the L2 norm of row i (device float [rows]). */
+aspis_status aspis_row_norms(const void *x, int64_t rows, int64_t d, int64_t ld,
+                             aspis_dtype dtype, float *norms, void *workspace,
+                             size_t ws_bytes, void *stream);
+
+/* Clips every row by its own norm: out_i = c_i * x_i, rounded to the type.
+ * out: rows of ldo >= d elements of the same type; x itself (with ldo = ld)
+ * clips in place, anything else must not overlap x.  norms: device float
+ * [rows], the norms before clipping, or NULL. */
+aspis_status aspis_clip_rows(const void *x, int64_t rows, int64_t d, int64_t ld,
+                             aspis_dtype dtype, double max_norm, void *out,
+                             int64_t ldo, float *norms, void *workspace,
+                             size_t ws_bytes, void *stream);
+
+/* The model update with the clip applied as the gradient is read:
+ * g = c * grad in f32 (c of the global norm of `grads`), then
+ *   SGD:   g += weight_decay * p;  mean = momentum * mean + g;
+ *          p -= lr * (nesterov ? g + momentum * mean : mean)
+ *   AdamW: p *= 1 - lr * weight_decay;  mean = beta1 * mean + (1 - beta1) * g;
+ *          square = beta2 * square + (1 - beta2) * g * g;
+ *          p -= lr / (1 - beta1^step) * mean
+ *               / (sqrt(square / (1 - beta2^step)) + eps)
+ * in f32.  params, mean and square are tables of f32 tensors, grads of any
+ * types; copies, when not NULL, lists tensors of any type that receive the
+ * new parameters, rounded (a model's low-precision weights).  All tables
+ * list tensors of the same sizes in the same order, and all tensors written
+ * are disjoint from the others.  SGD's mean may be NULL when momentum is 0.
+ * sumsq, norm, flags, workspace: as aspis_clip_grads. */
+typedef struct {
+    double lr, momentum, weight_decay, max_norm;
+    int32_t nesterov;
+    uint32_t flags;
+} aspis_sgd;
+typedef struct {
+    double lr, beta_one, beta_two, eps, weight_decay, max_norm;
+    int64_t step;              /* 1 for the first update                     */
+    uint32_t flags;
+    uint32_t reserved;
+} aspis_adamw;
+aspis_status aspis_clipped_sgd(const aspis_chunk *params, const aspis_chunk *grads,
+                               const aspis_chunk *mean, const aspis_chunk *copies,
+                               int64_t n_chunks, const aspis_sgd *opt, double *sumsq,
+                               float *norm, void *workspace, size_t ws_bytes,
+                               void *stream);
+aspis_status aspis_clipped_adamw(const aspis_chunk *params, const aspis_chunk *grads,
+                                 const aspis_chunk *mean, const aspis_chunk *square,
+                                 const aspis_chunk *copies, int64_t n_chunks,
+                                 const aspis_adamw *opt, double *sumsq, float *norm,
+                                 void *workspace, size_t ws_bytes, void *stream);
 
 /* Message describing the calling thread's last failure ("" if none). */
 const char *aspis_last_error(void);

@@ -8,6 +8,7 @@ the library -- there is no fallback.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from dataclasses import dataclass
@@ -25,6 +26,8 @@ FLAG_TIMING = 2
 FLAG_FULL_KEYS = 4
 FLAG_HALF_KEYS = 8
 FLAG_PROBE_PREFIX = 16
+CLIP_HAVE_SUMSQ = 1
+CLIP_SKIP_NONFINITE = 2
 
 EXPORTED = (
     "aspis_num_files", "aspis_assign", "aspis_detect", "aspis_clique",
@@ -33,6 +36,9 @@ EXPORTED = (
     "aspis_plan",
     "aspis_read_probe_sink_words", "aspis_read_probe", "aspis_simulate", "aspis_detox",
     "aspis_last_error",
+    "aspis_tensor_chunks", "aspis_tensor_entries", "aspis_tensor_table", "aspis_norm_workspace",
+    "aspis_grad_norm", "aspis_clip_grads", "aspis_row_workspace", "aspis_row_norms",
+    "aspis_clip_rows", "aspis_clipped_sgd", "aspis_clipped_adamw",
 )
 
 
@@ -106,6 +112,24 @@ class KernelPlan(ctypes.Structure):
         return d
 
 
+class Chunk(ctypes.Structure):
+    _fields_ = [("addr", ctypes.c_uint64), ("n", ctypes.c_int32), ("info", ctypes.c_int32)]
+
+
+class SgdOptions(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("momentum", ctypes.c_double),
+                ("weight_decay", ctypes.c_double), ("max_norm", ctypes.c_double),
+                ("nesterov", ctypes.c_int32), ("flags", ctypes.c_uint32)]
+
+
+class AdamwOptions(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta_one", ctypes.c_double),
+                ("beta_two", ctypes.c_double), ("eps", ctypes.c_double),
+                ("weight_decay", ctypes.c_double), ("max_norm", ctypes.c_double),
+                ("step", ctypes.c_int64), ("flags", ctypes.c_uint32),
+                ("reserved", ctypes.c_uint32)]
+
+
 _lib = None
 
 
@@ -163,6 +187,30 @@ def lib():
     L.aspis_detox.argtypes = [i32, i32, i32, ctypes.c_int, ctypes.POINTER(i64),
                               ctypes.POINTER(ctypes.c_double)]
     L.aspis_detox.restype = ctypes.c_int
+    f64, size = ctypes.c_double, ctypes.c_size_t
+    L.aspis_tensor_chunks.argtypes = [P, i32]
+    L.aspis_tensor_chunks.restype = i64
+    L.aspis_tensor_entries.argtypes = [P, i32]
+    L.aspis_tensor_entries.restype = i64
+    L.aspis_tensor_table.argtypes = [P, P, P, i32, P, i64]
+    L.aspis_tensor_table.restype = ctypes.c_int
+    L.aspis_norm_workspace.argtypes = [i64]
+    L.aspis_norm_workspace.restype = size
+    L.aspis_grad_norm.argtypes = [P, i64, i32, P, P, P, P, size, P]
+    L.aspis_grad_norm.restype = ctypes.c_int
+    L.aspis_clip_grads.argtypes = [P, P, i64, f64, P, P, u32, P, size, P]
+    L.aspis_clip_grads.restype = ctypes.c_int
+    L.aspis_row_workspace.argtypes = [i64, i64, ctypes.c_int]
+    L.aspis_row_workspace.restype = size
+    L.aspis_row_norms.argtypes = [P, i64, i64, i64, ctypes.c_int, P, P, size, P]
+    L.aspis_row_norms.restype = ctypes.c_int
+    L.aspis_clip_rows.argtypes = [P, i64, i64, i64, ctypes.c_int, f64, P, i64, P, P, size, P]
+    L.aspis_clip_rows.restype = ctypes.c_int
+    L.aspis_clipped_sgd.argtypes = [P, P, P, P, i64, ctypes.POINTER(SgdOptions), P, P, P, size, P]
+    L.aspis_clipped_sgd.restype = ctypes.c_int
+    L.aspis_clipped_adamw.argtypes = [P, P, P, P, P, i64, ctypes.POINTER(AdamwOptions), P, P, P,
+                                      size, P]
+    L.aspis_clipped_adamw.restype = ctypes.c_int
     L.aspis_last_error.argtypes = []
     L.aspis_last_error.restype = ctypes.c_char_p
     _lib = L
@@ -448,3 +496,375 @@ def read_probe(buf, sink=None) -> float:
     nbytes -= nbytes % 16
     _check(lib().aspis_read_probe(buf.data_ptr(), nbytes, sink.data_ptr(), _stream_ptr()))
     return sink
+
+
+# ------------------------------------- norms, clipping and the model update
+
+def _dtype_code(dtype) -> int:
+    torch = _torch()
+    code = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}.get(dtype)
+    if code is None:
+        raise AspisError(ERR_INVALID_ARG, f"unsupported type {dtype}: float32, bfloat16 or float16")
+    return code
+
+
+def _layout(t):
+    """Shape and strides of a tensor whose elements fill one span of memory
+    without gaps or overlaps, None otherwise (strides of dimensions of one
+    element say nothing and read 0)."""
+    shape = tuple(t.shape)
+    strides = tuple(0 if n == 1 else st for n, st in zip(shape, t.stride()))
+    want = 1
+    if t.numel() > 0:
+        for st, n in sorted((st, n) for st, n in zip(strides, shape) if n > 1):
+            if st != want:
+                return None
+            want *= n
+    return shape, strides
+
+
+def _on(device):
+    """Makes `device` current for a launch, where it is not."""
+    torch = _torch()
+    if device.index is None or device.index == torch.cuda.current_device():
+        return contextlib.nullcontext()
+    return torch.cuda.device(device)
+
+
+class TensorList:
+    """A list of CUDA tensors as the norm, clipping and update calls take it
+    (aspis_tensor_table): made once for tensors that stay, or by the call
+    itself from any sequence of tensors.
+
+    Tensors are float32, bfloat16 or float16 (types may mix), on one device,
+    of any shape, also empty; each must fill one span of memory (any order of
+    its dimensions, no gaps).  The list holds the tensors and looks at every
+    call whether they still are where they were, so that a tensor whose
+    storage was replaced (`t.data = ...`) is read where it is now."""
+
+    def __init__(self, tensors, device=None):
+        torch = _torch()
+        self.tensors = [tensors] if isinstance(tensors, torch.Tensor) else list(tensors)
+        for i, t in enumerate(self.tensors):
+            if not isinstance(t, torch.Tensor) or not t.is_cuda or t.layout != torch.strided:
+                raise AspisError(ERR_INVALID_ARG, f"tensor {i} of the list must be a strided cuda "
+                                                  f"tensor")
+        if device is None:
+            device = self.tensors[0].device if self.tensors else \
+                torch.device("cuda", torch.cuda.current_device())
+        self.device = torch.device(device)
+        self._read()
+
+    def __len__(self):
+        return len(self.tensors)
+
+    def _read(self):
+        """Looks the tensors over and uploads their table."""
+        torch = _torch()
+        ts = self.tensors
+        n = len(ts)
+        self._where = self._now()
+        self.numels = [t.numel() for t in ts]
+        self.dtypes = [t.dtype for t in ts]
+        codes = np.array([_dtype_code(d) for d in self.dtypes], dtype=np.int32)
+        self.layouts = [_layout(t) for t in ts]
+        for i, t in enumerate(ts):
+            if self.layouts[i] is None:
+                raise AspisError(ERR_INVALID_ARG, f"tensor {i} of the list has gaps or overlaps in "
+                                                  f"memory: shape {tuple(t.shape)}, strides "
+                                                  f"{t.stride()}")
+            if t.device != self.device:
+                raise AspisError(ERR_INVALID_ARG, f"tensor {i} of the list is on {t.device}, the "
+                                                  f"list on {self.device}")
+        self.contiguous = all(t.is_contiguous() for t in ts)
+        spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size())
+                       for t in ts if t.numel() > 0)
+        self.disjoint = all(a[1] <= b[0] for a, b in zip(spans, spans[1:]))
+        ptrs = np.array([t.data_ptr() for t in ts], dtype=np.uint64)
+        numels = np.array(self.numels, dtype=np.int64)
+        self.n_chunks = int(lib().aspis_tensor_chunks(numels.ctypes.data, n))
+        entries = int(lib().aspis_tensor_entries(numels.ctypes.data, n))
+        if entries < 0:
+            raise AspisError(ERR_OVERFLOW, "too many elements in the list")
+        host = np.zeros((max(entries, 1), 2), dtype=np.uint64)
+        _check(lib().aspis_tensor_table(ptrs.ctypes.data, numels.ctypes.data, codes.ctypes.data, n,
+                                        host.ctypes.data, entries))
+        # a copy from pageable memory returns when it is done: the table is
+        # there for any stream
+        self._table = torch.from_numpy(host.view(np.int64)).to(self.device)
+        self._stream = torch.cuda.current_stream(self.device)
+
+    def _now(self):
+        return [(t.data_ptr(), t.numel()) for t in self.tensors]
+
+    def table(self) -> int:
+        """Device address of the table, brought up to date."""
+        if self._now() != self._where:
+            self._read()
+        stream = _torch().cuda.current_stream(self.device)
+        if stream != self._stream:
+            self._table.record_stream(stream)
+        return self._table.data_ptr()
+
+
+def _list(x) -> TensorList:
+    return x if isinstance(x, TensorList) else TensorList(x)
+
+
+def _check_match(name: str, a: TensorList, ref: TensorList, same_types: bool = False,
+                 float32: bool = False):
+    """`a` lists tensors of the sizes, order of elements and device of ref's."""
+    if a.numels != ref.numels or a.device != ref.device:
+        raise AspisError(ERR_INVALID_ARG, f"{name} must list tensors of the gradients' sizes, in "
+                                          f"their order, on their device")
+    if not (a.contiguous and ref.contiguous) and a.layouts != ref.layouts:
+        raise AspisError(ERR_INVALID_ARG, f"{name}: tensors that are not contiguous must have the "
+                                          f"gradients' shapes and strides")
+    if same_types and a.dtypes != ref.dtypes:
+        raise AspisError(ERR_INVALID_ARG, f"{name} must have the gradients' types")
+    if float32:
+        torch = _torch()
+        if any(d != torch.float32 for d in a.dtypes):
+            raise AspisError(ERR_INVALID_ARG, f"{name} must be float32")
+
+
+def _check_written(name: str, a: TensorList):
+    if not a.disjoint:
+        raise AspisError(ERR_INVALID_ARG, f"{name} is written and lists overlapping tensors")
+
+
+@dataclass
+class NormBuffers:
+    """What the norm of a list leaves on the device: norm float32 [1], sumsq
+    float64 [1] and, when asked for, each float32 [n] (every tensor's own)."""
+    norm: object
+    sumsq: object
+    each: object = None
+
+    @classmethod
+    def empty(cls, device, each: int = 0):
+        torch = _torch()
+        return cls(torch.empty(1, dtype=torch.float32, device=device),
+                   torch.empty(1, dtype=torch.float64, device=device),
+                   torch.empty(each, dtype=torch.float32, device=device) if each else None)
+
+
+def norm_workspace(grads):
+    """Workspace of grad_norm, clip_grads and the updates for a list."""
+    torch = _torch()
+    grads = _list(grads)
+    grads.table()
+    n = int(lib().aspis_norm_workspace(grads.n_chunks))
+    return torch.empty(n, dtype=torch.uint8, device=grads.device)
+
+
+def _norm_buffers(grads: TensorList, bufs, ws, sumsq, each: int = 0):
+    """Checked or new buffers of a call, and the flags they ask for."""
+    torch = _torch()
+    dev = grads.device
+    if bufs is None:
+        bufs = NormBuffers.empty(dev, each)
+    else:
+        _check_buffer("bufs.norm", bufs.norm, torch.float32, 1, dev)
+        _check_buffer("bufs.sumsq", bufs.sumsq, torch.float64, 1, dev)
+        if each:
+            _check_buffer("bufs.each", bufs.each, torch.float32, each, dev)
+    if sumsq is not None:
+        _check_buffer("sumsq", sumsq, torch.float64, 1, dev)
+    need = int(lib().aspis_norm_workspace(grads.n_chunks))
+    if ws is None:
+        ws = torch.empty(need, dtype=torch.uint8, device=dev)
+    else:
+        _check_buffer("ws", ws, torch.uint8, need, dev)
+    return bufs, ws, bufs.sumsq if sumsq is None else sumsq, \
+        0 if sumsq is None else CLIP_HAVE_SUMSQ
+
+
+def grad_norm(grads, each: bool = False, bufs: NormBuffers | None = None, ws=None) -> NormBuffers:
+    """The global L2 norm of a list of tensors (aspis_grad_norm), with every
+    tensor's own norm when `each`.  Nothing is synchronised: the results are
+    on the device.  Where ranks hold shards of one model, all-reduce
+    bufs.sumsq and hand it to clip_grads or an update as sumsq."""
+    grads = _list(grads)
+    table = grads.table()
+    bufs, ws, sumsq, _ = _norm_buffers(grads, bufs, ws, None, len(grads) if each else 0)
+    with _on(grads.device):
+        _check(lib().aspis_grad_norm(table, grads.n_chunks, len(grads), sumsq.data_ptr(),
+                                     bufs.norm.data_ptr(),
+                                     bufs.each.data_ptr() if each and len(grads) else None,
+                                     ws.data_ptr(), ws.numel(), _stream_ptr()))
+    return bufs
+
+
+def clip_grads(grads, max_norm: float, out=None, sumsq=None, bufs: NormBuffers | None = None,
+               ws=None) -> NormBuffers:
+    """Scales a list of tensors so that its global norm is at most max_norm
+    (aspis_clip_grads): in place, or into the tensors of `out`.  Returns the
+    norm before clipping.  sumsq: the sum of squares to clip by (of all
+    ranks), instead of this list's own."""
+    grads = _list(grads)
+    table = grads.table()
+    bufs, ws, total, flags = _norm_buffers(grads, bufs, ws, sumsq)
+    if out is None:
+        _check_written("grads", grads)
+        out_table = None
+    else:
+        out = _list(out)
+        out_table = out.table()
+        _check_match("out", out, grads, same_types=True)
+        _check_written("out", out)
+    with _on(grads.device):
+        _check(lib().aspis_clip_grads(table, out_table, grads.n_chunks, max_norm, total.data_ptr(),
+                                      bufs.norm.data_ptr(), flags, ws.data_ptr(), ws.numel(),
+                                      _stream_ptr()))
+    return bufs
+
+
+def _rows(name: str, x):
+    """rows, d, elements between rows' starts and type of a tensor of rows."""
+    torch = _torch()
+    if not isinstance(x, torch.Tensor) or not x.is_cuda or x.dim() < 1:
+        raise AspisError(ERR_INVALID_ARG, f"{name} must be a cuda tensor of rows [..., d]")
+    code = _dtype_code(x.dtype)
+    d = x.shape[-1]
+    rows = 1
+    for n in x.shape[:-1]:
+        rows *= n
+    if rows * d == 0:
+        return rows, d, d, code
+    # the leading dimensions have to be one series of rows, equally far apart
+    ld, run = None, 1
+    for n, st in zip(reversed(x.shape[:-1]), reversed(x.stride()[:-1])):
+        if n == 1:
+            continue
+        if ld is None:
+            ld = st
+        elif st != ld * run:
+            ld = -1
+            break
+        run *= n
+    ld = d if ld is None else ld
+    if ld < d or (d > 1 and x.stride(-1) != 1):
+        raise AspisError(ERR_INVALID_ARG, f"{name} must hold rows of contiguous elements, equally "
+                                          f"far apart: shape {tuple(x.shape)}, strides "
+                                          f"{x.stride()}")
+    return rows, d, ld, code
+
+
+def row_workspace(x):
+    """Workspace of row_norms and clip_rows for a tensor of rows."""
+    torch = _torch()
+    rows, d, _, code = _rows("x", x)
+    return torch.empty(int(lib().aspis_row_workspace(rows, d, code)), dtype=torch.uint8,
+                       device=x.device)
+
+
+def _row_buffers(x, rows: int, d: int, code: int, norms, ws):
+    torch = _torch()
+    if norms is None:
+        norms = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    else:
+        _check_buffer("norms", norms, torch.float32, rows, x.device)
+    need = int(lib().aspis_row_workspace(rows, d, code))
+    if ws is None:
+        ws = torch.empty(need, dtype=torch.uint8, device=x.device)
+    else:
+        _check_buffer("ws", ws, torch.uint8, need, x.device)
+    return norms, ws
+
+
+def row_norms(x, norms=None, ws=None):
+    """The L2 norm of every row of x [..., d] (aspis_row_norms): the replicas
+    [f][r][d] or a worker's upload [l][d]."""
+    rows, d, ld, code = _rows("x", x)
+    norms, ws = _row_buffers(x, rows, d, code, norms, ws)
+    with _on(x.device):
+        _check(lib().aspis_row_norms(x.data_ptr(), rows, d, ld, code, norms.data_ptr(),
+                                     ws.data_ptr(), ws.numel(), _stream_ptr()))
+    return norms
+
+
+def clip_rows(x, max_norm: float, out=None, norms=None, ws=None):
+    """Scales every row of x [..., d] whose norm is above max_norm down to it
+    (aspis_clip_rows): in place, or into `out`.  Returns (out, the norms before
+    clipping).  Replicas with equal bits are equal after it, so a server may
+    clip them before detection and workers before they upload."""
+    rows, d, ld, code = _rows("x", x)
+    out = x if out is None else out
+    ldo = ld
+    if out is not x:
+        _, _, ldo, out_code = _rows("out", out)
+        if out.shape != x.shape or out_code != code or out.device != x.device:
+            raise AspisError(ERR_INVALID_ARG, "out must have the shape, type and device of x")
+    norms, ws = _row_buffers(x, rows, d, code, norms, ws)
+    with _on(x.device):
+        _check(lib().aspis_clip_rows(x.data_ptr(), rows, d, ld, code, max_norm, out.data_ptr(),
+                                     ldo, norms.data_ptr(), ws.data_ptr(), ws.numel(),
+                                     _stream_ptr()))
+    return out, norms
+
+
+def _update_lists(params, grads, states: dict, copies):
+    """The lists of an update, checked against the gradients', and their
+    tables.  The caller keeps the lists until it has launched: a list made
+    for the call owns its table's memory."""
+    lists = {"params": _list(params), **{k: _list(v) for k, v in states.items()}}
+    if copies is not None:
+        lists["copies"] = _list(copies)
+    tables = [grads.table()]
+    for name, a in lists.items():
+        tables.append(a.table())
+        _check_match(name, a, grads, float32=name != "copies")
+        _check_written(name, a)
+    return lists, tables
+
+
+def clipped_sgd(params, grads, mean=None, *, lr: float, momentum: float = 0.0,
+                nesterov: bool = False, weight_decay: float = 0.0,
+                max_norm: float = float("inf"), copies=None, sumsq=None,
+                skip_nonfinite: bool = False, bufs: NormBuffers | None = None,
+                ws=None) -> NormBuffers:
+    """One SGD update in place, by the gradients clipped to max_norm
+    (aspis_clipped_sgd); the gradients stay as they are.  params and mean
+    (the momentum, needed unless it is 0) are lists of float32 tensors,
+    copies a list that receives the new parameters rounded to its types.
+    Returns the norm before clipping.  skip_nonfinite: a norm that is not
+    finite leaves parameters, state and copies as they are.
+
+    The update is not seen by autograd's version counters."""
+    if momentum and mean is None:
+        raise AspisError(ERR_INVALID_ARG, "momentum needs the list `mean`")
+    grads = _list(grads)
+    lists, tables = _update_lists(params, grads, {} if mean is None else {"mean": mean}, copies)
+    bufs, ws, total, flags = _norm_buffers(grads, bufs, ws, sumsq)
+    opt = SgdOptions(lr, momentum, weight_decay, max_norm, int(nesterov),
+                     flags | (CLIP_SKIP_NONFINITE if skip_nonfinite else 0))
+    with _on(grads.device):
+        _check(lib().aspis_clipped_sgd(tables[1], tables[0], tables[2] if mean is not None else None,
+                                       tables[-1] if copies is not None else None, grads.n_chunks,
+                                       ctypes.byref(opt), total.data_ptr(), bufs.norm.data_ptr(),
+                                       ws.data_ptr(), ws.numel(), _stream_ptr()))
+    del lists   # their tables were needed until here
+    return bufs
+
+
+def clipped_adamw(params, grads, mean, square, *, step: int, lr: float, betas=(0.9, 0.999),
+                  eps: float = 1e-8, weight_decay: float = 0.01,
+                  max_norm: float = float("inf"), copies=None, sumsq=None,
+                  skip_nonfinite: bool = False, bufs: NormBuffers | None = None,
+                  ws=None) -> NormBuffers:
+    """One AdamW update in place, by the gradients clipped to max_norm
+    (aspis_clipped_adamw); as clipped_sgd otherwise.  step counts from 1."""
+    grads = _list(grads)
+    lists, tables = _update_lists(params, grads, {"mean": mean, "square": square}, copies)
+    bufs, ws, total, flags = _norm_buffers(grads, bufs, ws, sumsq)
+    opt = AdamwOptions(lr, betas[0], betas[1], eps, weight_decay, max_norm, step,
+                       flags | (CLIP_SKIP_NONFINITE if skip_nonfinite else 0), 0)
+    with _on(grads.device):
+        _check(lib().aspis_clipped_adamw(tables[1], tables[0], tables[2], tables[3],
+                                         tables[4] if copies is not None else None,
+                                         grads.n_chunks, ctypes.byref(opt), total.data_ptr(),
+                                         bufs.norm.data_ptr(), ws.data_ptr(), ws.numel(),
+                                         _stream_ptr()))
+    del lists   # their tables were needed until here
+    return bufs

@@ -23,9 +23,9 @@ ARCH = "gfx950"
 DEVICE_FLAGS = ["-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 
 
-SOURCES = ["aspis_host.cpp", "aspis_sim.cpp", "aspis_kernels.hip", "aspis_ws_r3.hip",
-           "aspis_ws_r3_table.hip", "aspis_ws_r5.hip", "aspis_ws_r7.hip",
-           "aspis_ws_median.hip"]
+SOURCES = ["aspis_host.cpp", "aspis_sim.cpp", "aspis_clip.cpp", "aspis_clip.hip",
+           "aspis_kernels.hip", "aspis_ws_r3.hip", "aspis_ws_r3_table.hip", "aspis_ws_r5.hip",
+           "aspis_ws_r7.hip", "aspis_ws_median.hip"]
 
 
 def _run(cmd: list[str]) -> list[str]:
