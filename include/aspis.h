@@ -431,7 +431,8 @@ typedef struct {
 
 /* Entries of the table of `count` tensors with numel[i] >= 0 elements, and
  * how many of them are chunks (n_chunks of the calls below; it depends on
- * the sizes alone).  -1 on invalid arguments or more than 2^31-1 entries. */
+ * the sizes alone).  -1 on invalid arguments, more than 2^23 tensors or more
+ * than 2^38 elements. */
 int64_t aspis_tensor_chunks(const int64_t *numel, int32_t count);
 int64_t aspis_tensor_entries(const int64_t *numel, int32_t count);
 
@@ -477,7 +478,7 @@ aspis_status aspis_clip_grads(const aspis_chunk *table, const aspis_chunk *out_t
 
 /* Rows: x holds `rows` rows of d elements, ld >= d elements from one row's
  * start to the next (a replica tensor [f][r][d] has f*r rows, a worker's
- * upload [l][d] has l).  aspis_row_workspace: bytes of workspace for them
+ * upload [l][d] has l); d is at most 2^34.  aspis_row_workspace: bytes of workspace for them
  * (may be 0; SIZE_MAX on invalid arguments). */
 size_t aspis_row_workspace(int64_t rows, int64_t d, aspis_dtype dtype);
 

@@ -523,6 +523,12 @@ def _layout(t):
     return shape, strides
 
 
+def _raw_stream(device) -> int:
+    """The current stream of a device with an index, as the library takes it
+    (an order of magnitude quicker than asking for the stream object)."""
+    return _torch()._C._cuda_getCurrentRawStream(device.index)
+
+
 def _on(device):
     """Makes `device` current for a launch, where it is not."""
     torch = _torch()
@@ -553,6 +559,8 @@ class TensorList:
             device = self.tensors[0].device if self.tensors else \
                 torch.device("cuda", torch.cuda.current_device())
         self.device = torch.device(device)
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
         self._read()
 
     def __len__(self):
@@ -592,19 +600,22 @@ class TensorList:
         # a copy from pageable memory returns when it is done: the table is
         # there for any stream
         self._table = torch.from_numpy(host.view(np.int64)).to(self.device)
-        self._stream = torch.cuda.current_stream(self.device)
+        self._address = self._table.data_ptr()
+        self._stream = _raw_stream(self.device)
+        self.all_float32 = all(d == torch.float32 for d in self.dtypes)
+        self.ws_bytes = int(lib().aspis_norm_workspace(self.n_chunks))
 
     def _now(self):
-        return [(t.data_ptr(), t.numel()) for t in self.tensors]
+        Tensor = _torch().Tensor
+        return list(map(Tensor.data_ptr, self.tensors)), list(map(Tensor.numel, self.tensors))
 
     def table(self) -> int:
         """Device address of the table, brought up to date."""
         if self._now() != self._where:
             self._read()
-        stream = _torch().cuda.current_stream(self.device)
-        if stream != self._stream:
-            self._table.record_stream(stream)
-        return self._table.data_ptr()
+        if _raw_stream(self.device) != self._stream:
+            self._table.record_stream(_torch().cuda.current_stream(self.device))
+        return self._address
 
 
 def _list(x) -> TensorList:
@@ -622,10 +633,8 @@ def _check_match(name: str, a: TensorList, ref: TensorList, same_types: bool = F
                                           f"gradients' shapes and strides")
     if same_types and a.dtypes != ref.dtypes:
         raise AspisError(ERR_INVALID_ARG, f"{name} must have the gradients' types")
-    if float32:
-        torch = _torch()
-        if any(d != torch.float32 for d in a.dtypes):
-            raise AspisError(ERR_INVALID_ARG, f"{name} must be float32")
+    if float32 and not a.all_float32:
+        raise AspisError(ERR_INVALID_ARG, f"{name} must be float32")
 
 
 def _check_written(name: str, a: TensorList):
@@ -654,8 +663,7 @@ def norm_workspace(grads):
     torch = _torch()
     grads = _list(grads)
     grads.table()
-    n = int(lib().aspis_norm_workspace(grads.n_chunks))
-    return torch.empty(n, dtype=torch.uint8, device=grads.device)
+    return torch.empty(grads.ws_bytes, dtype=torch.uint8, device=grads.device)
 
 
 def _norm_buffers(grads: TensorList, bufs, ws, sumsq, each: int = 0):
@@ -671,11 +679,10 @@ def _norm_buffers(grads: TensorList, bufs, ws, sumsq, each: int = 0):
             _check_buffer("bufs.each", bufs.each, torch.float32, each, dev)
     if sumsq is not None:
         _check_buffer("sumsq", sumsq, torch.float64, 1, dev)
-    need = int(lib().aspis_norm_workspace(grads.n_chunks))
     if ws is None:
-        ws = torch.empty(need, dtype=torch.uint8, device=dev)
+        ws = torch.empty(grads.ws_bytes, dtype=torch.uint8, device=dev)
     else:
-        _check_buffer("ws", ws, torch.uint8, need, dev)
+        _check_buffer("ws", ws, torch.uint8, grads.ws_bytes, dev)
     return bufs, ws, bufs.sumsq if sumsq is None else sumsq, \
         0 if sumsq is None else CLIP_HAVE_SUMSQ
 
@@ -692,7 +699,7 @@ def grad_norm(grads, each: bool = False, bufs: NormBuffers | None = None, ws=Non
         _check(lib().aspis_grad_norm(table, grads.n_chunks, len(grads), sumsq.data_ptr(),
                                      bufs.norm.data_ptr(),
                                      bufs.each.data_ptr() if each and len(grads) else None,
-                                     ws.data_ptr(), ws.numel(), _stream_ptr()))
+                                     ws.data_ptr(), ws.numel(), _raw_stream(grads.device)))
     return bufs
 
 
@@ -716,7 +723,7 @@ def clip_grads(grads, max_norm: float, out=None, sumsq=None, bufs: NormBuffers |
     with _on(grads.device):
         _check(lib().aspis_clip_grads(table, out_table, grads.n_chunks, max_norm, total.data_ptr(),
                                       bufs.norm.data_ptr(), flags, ws.data_ptr(), ws.numel(),
-                                      _stream_ptr()))
+                                      _raw_stream(grads.device)))
     return bufs
 
 
@@ -780,7 +787,7 @@ def row_norms(x, norms=None, ws=None):
     norms, ws = _row_buffers(x, rows, d, code, norms, ws)
     with _on(x.device):
         _check(lib().aspis_row_norms(x.data_ptr(), rows, d, ld, code, norms.data_ptr(),
-                                     ws.data_ptr(), ws.numel(), _stream_ptr()))
+                                     ws.data_ptr(), ws.numel(), _raw_stream(x.device)))
     return norms
 
 
@@ -800,7 +807,7 @@ def clip_rows(x, max_norm: float, out=None, norms=None, ws=None):
     with _on(x.device):
         _check(lib().aspis_clip_rows(x.data_ptr(), rows, d, ld, code, max_norm, out.data_ptr(),
                                      ldo, norms.data_ptr(), ws.data_ptr(), ws.numel(),
-                                     _stream_ptr()))
+                                     _raw_stream(x.device)))
     return out, norms
 
 
@@ -843,7 +850,7 @@ def clipped_sgd(params, grads, mean=None, *, lr: float, momentum: float = 0.0,
         _check(lib().aspis_clipped_sgd(tables[1], tables[0], tables[2] if mean is not None else None,
                                        tables[-1] if copies is not None else None, grads.n_chunks,
                                        ctypes.byref(opt), total.data_ptr(), bufs.norm.data_ptr(),
-                                       ws.data_ptr(), ws.numel(), _stream_ptr()))
+                                       ws.data_ptr(), ws.numel(), _raw_stream(grads.device)))
     del lists   # their tables were needed until here
     return bufs
 
@@ -865,6 +872,6 @@ def clipped_adamw(params, grads, mean, square, *, step: int, lr: float, betas=(0
                                          tables[4] if copies is not None else None,
                                          grads.n_chunks, ctypes.byref(opt), total.data_ptr(),
                                          bufs.norm.data_ptr(), ws.data_ptr(), ws.numel(),
-                                         _stream_ptr()))
+                                         _raw_stream(grads.device)))
     del lists   # their tables were needed until here
     return bufs

@@ -17,11 +17,11 @@ void host_clear_error();
 
 RowSplit row_split(int64_t d, int elem_bytes) {
     if (d <= (int64_t)kRowVecs * (16 / elem_bytes)) return {0, 1};
-    // a segment of 16 sqrt(d) elements: the sums of a row's segments that
-    // each of its workgroups reads stay below 1 % of what it scales
-    int64_t seg = (int64_t)(16.0 * std::sqrt((double)d));
-    seg = (seg + 2047) / 2048 * 2048;
-    if (seg < 16384) seg = 16384;
+    // at most 1,024 segments: every workgroup that scales a piece of the row
+    // reads all its segments' sums
+    int64_t seg = (d + 1023) / 1024;
+    seg = (seg + kChunk - 1) / kChunk * kChunk;
+    if (seg < 4 * kChunk) seg = 4 * kChunk;
     return {seg, (int32_t)((d + seg - 1) / seg)};
 }
 }  // namespace aspis
@@ -53,28 +53,27 @@ int elem_bytes(int dtype) {
     return dtype == ASPIS_F32 ? 4 : dtype == ASPIS_BF16 || dtype == ASPIS_F16 ? 2 : 0;
 }
 
-// Chunks of a list: -1 on invalid sizes, -2 beyond 2^31-1 entries.
+// Chunks of a list: -1 on invalid sizes, -2 past the limits.
 int64_t count_chunks(const int64_t *numel, int32_t count) {
     if (count < 0 || (count > 0 && numel == nullptr)) return -1;
+    if (count > aspis::kMaxTensors) return -2;
     int64_t n = 0;
     for (int32_t i = 0; i < count; ++i) {
         if (numel[i] < 0) return -1;
         if (numel[i] > kMaxElements) return -2;
         n += aspis::chunks_of(numel[i]);
-        if (n + count > INT32_MAX) return -2;
+        if (n > aspis::kMaxChunks) return -2;
     }
     return n;
 }
 
-// The workspace of a list: the norm pass's partial sums, then (for every
-// tensor's own norm) one sum per chunk.
 size_t list_workspace(int64_t n_chunks) {
-    return ((size_t)aspis::norm_groups(n_chunks) + (size_t)n_chunks) * sizeof(double);
+    return (size_t)aspis::norm_doubles(n_chunks) * sizeof(double);
 }
 
 aspis_status check_list(const char *who, const void *table, int64_t n_chunks, double max_norm,
                         const double *sumsq, const float *norm, const void *ws, size_t ws_bytes) {
-    if (n_chunks < 0 || n_chunks > INT32_MAX)
+    if (n_chunks < 0 || n_chunks > aspis::kMaxChunks)
         return fail(ASPIS_ERR_INVALID_ARG, "%s: n_chunks=%lld", who, (long long)n_chunks);
     if (n_chunks > 0 && table == nullptr)
         return fail(ASPIS_ERR_INVALID_ARG, "%s: NULL table", who);
@@ -90,21 +89,6 @@ aspis_status check_list(const char *who, const void *table, int64_t n_chunks, do
     return ASPIS_OK;
 }
 
-// The norm pass of the calls that apply the norm: leaves the partial sums in
-// the workspace and says where they are.
-aspis_status start_norm(const char *who, const aspis_chunk *table, int64_t n_chunks,
-                        double max_norm, double *sumsq, float *norm, uint32_t flags, void *ws,
-                        hipStream_t s, aspis::NormIn *in) {
-    *in = {static_cast<const double *>(ws), 0, sumsq, norm, max_norm};
-    if (flags & ASPIS_CLIP_HAVE_SUMSQ) return ASPIS_OK;
-    if (n_chunks == 0) {   // writes the norm of nothing, which the caller's kernel reads
-        return launched(aspis::launch_list_norm(table, 0, 0, *in, nullptr, nullptr, s), who);
-    }
-    in->n_partial = aspis::norm_groups(n_chunks);
-    return launched(aspis::launch_list_sumsq(table, n_chunks, static_cast<double *>(ws), nullptr, s),
-                    who);
-}
-
 aspis_status check_rows(const char *who, const void *x, int64_t rows, int64_t d, int64_t ld,
                         int dtype, const void *ws, size_t ws_bytes) {
     const int size = elem_bytes(dtype);
@@ -112,8 +96,8 @@ aspis_status check_rows(const char *who, const void *x, int64_t rows, int64_t d,
     if (rows < 0 || d < 0 || ld < d)
         return fail(ASPIS_ERR_INVALID_ARG, "%s: rows=%lld d=%lld ld=%lld", who, (long long)rows,
                     (long long)d, (long long)ld);
-    if (rows > 0 && ld > kMaxElements / rows)
-        return fail(ASPIS_ERR_OVERFLOW, "%s: rows * ld overflows", who);
+    if (d > aspis::kMaxRow || (rows > 0 && ld > kMaxElements / rows))
+        return fail(ASPIS_ERR_OVERFLOW, "%s: d=%lld or rows * ld is too large", who, (long long)d);
     if (rows > 0 && d > 0 && (x == nullptr || (uintptr_t)x % size != 0))
         return fail(ASPIS_ERR_INVALID_ARG, "%s: NULL or misaligned rows", who);
     const size_t need = aspis_row_workspace(rows, d, (aspis_dtype)dtype);
@@ -173,22 +157,25 @@ aspis_status aspis_tensor_table(const void *const *ptr, const int64_t *numel,
         return fail(ASPIS_ERR_BUFFER_SMALL, "need %lld entries, buffer holds %lld",
                     (long long)(chunks + count), (long long)cap);
     int64_t k = 0;
+    int32_t filled = 0;   // tensors before this one that are not empty
     for (int32_t i = 0; i < count; ++i) {
         const int size = elem_bytes(dtype[i]);
-        table[chunks + i] = {(uint64_t)k, (int32_t)aspis::chunks_of(numel[i]), dtype[i]};
+        table[chunks + i] = {(uint64_t)k, (int32_t)aspis::chunks_of(numel[i]), filled};
         for (int64_t at = 0; at < numel[i]; at += aspis::kChunk) {
             const int64_t left = numel[i] - at;
             table[k++] = {(uint64_t)(uintptr_t)ptr[i] + (uint64_t)(at * size),
-                          (int32_t)(left < aspis::kChunk ? left : aspis::kChunk), dtype[i]};
+                          (int32_t)(left < aspis::kChunk ? left : aspis::kChunk),
+                          filled * 4 + dtype[i]};
         }
+        filled += numel[i] > 0;
     }
     aspis::host_clear_error();
     return ASPIS_OK;
 }
 
 size_t aspis_norm_workspace(int64_t n_chunks) {
-    if (n_chunks < 0 || n_chunks > INT32_MAX) return 0;
-    return list_workspace(n_chunks > 0 ? n_chunks : 1);
+    if (n_chunks < 0 || n_chunks > aspis::kMaxChunks) return 0;
+    return list_workspace(n_chunks);
 }
 
 aspis_status aspis_grad_norm(const aspis_chunk *table, int64_t n_chunks, int32_t n_tensors,
@@ -197,18 +184,11 @@ aspis_status aspis_grad_norm(const aspis_chunk *table, int64_t n_chunks, int32_t
     const char *who = "aspis_grad_norm";
     aspis_status st = check_list(who, table, n_chunks, 0.0, sumsq, norm, workspace, ws_bytes);
     if (st != ASPIS_OK) return st;
-    if (n_tensors < 0 || (each != nullptr && n_tensors > 0 && table == nullptr))
+    if (n_tensors < 0 || n_tensors > aspis::kMaxTensors || (each != nullptr && n_tensors > 0 && table == nullptr))
         return fail(ASPIS_ERR_INVALID_ARG, "%s: n_tensors=%d or NULL table", who, n_tensors);
-    const hipStream_t s = static_cast<hipStream_t>(stream);
-    double *partial = static_cast<double *>(workspace);
-    const int groups = aspis::norm_groups(n_chunks);
-    double *chunk_sums = each != nullptr && n_chunks > 0 ? partial + groups : nullptr;
-    const aspis::NormIn in{partial, groups, sumsq, norm, 0.0};
-    if (n_chunks > 0) {
-        st = launched(aspis::launch_list_sumsq(table, n_chunks, partial, chunk_sums, s), who);
-        if (st != ASPIS_OK) return st;
-    }
-    return launched(aspis::launch_list_norm(table, n_chunks, n_tensors, in, chunk_sums, each, s),
+    const aspis::NormIn in{nullptr, 0, sumsq, norm, 0.0};
+    return launched(aspis::launch_norm(table, n_chunks, n_tensors, static_cast<double *>(workspace),
+                                       in, each, static_cast<hipStream_t>(stream)),
                     who);
 }
 
@@ -222,18 +202,19 @@ aspis_status aspis_clip_grads(const aspis_chunk *table, const aspis_chunk *out_t
         return fail(ASPIS_ERR_INVALID_ARG, "%s: unknown flags 0x%x", who, flags);
     if ((uintptr_t)out_table % 16 != 0)
         return fail(ASPIS_ERR_INVALID_ARG, "%s: tables must be 16-byte aligned", who);
-    const hipStream_t s = static_cast<hipStream_t>(stream);
-    aspis::NormIn in;
-    st = start_norm(who, table, n_chunks, max_norm, sumsq, norm, flags, workspace, s, &in);
-    if (st != ASPIS_OK) return st;
-    return launched(aspis::launch_list_scale(table, out_table == table ? nullptr : out_table,
-                                             n_chunks, in, s),
+    const aspis::NormIn in{nullptr, 0, sumsq, norm, max_norm};
+    return launched(aspis::launch_clip(table, out_table == table ? nullptr : out_table, n_chunks,
+                                       (flags & ASPIS_CLIP_HAVE_SUMSQ) != 0,
+                                       static_cast<double *>(workspace), in,
+                                       static_cast<hipStream_t>(stream)),
                     who);
 }
 
 size_t aspis_row_workspace(int64_t rows, int64_t d, aspis_dtype dtype) {
     const int size = elem_bytes(dtype);
-    if (size == 0 || rows < 0 || d < 0 || (rows > 0 && d > kMaxElements / rows)) return SIZE_MAX;
+    if (size == 0 || rows < 0 || d < 0 || d > aspis::kMaxRow ||
+        (rows > 0 && d > kMaxElements / rows))
+        return SIZE_MAX;
     const aspis::RowSplit split = aspis::row_split(d, size);
     return split.seg == 0 ? 0 : (size_t)rows * (size_t)split.parts * sizeof(double);
 }
@@ -294,14 +275,14 @@ aspis_status aspis_clipped_sgd(const aspis_chunk *params, const aspis_chunk *gra
         !(opt->weight_decay >= 0.0 && std::isfinite(opt->weight_decay)))
         return fail(ASPIS_ERR_INVALID_ARG, "%s: lr=%g momentum=%g weight_decay=%g", who, opt->lr,
                     opt->momentum, opt->weight_decay);
-    const hipStream_t s = static_cast<hipStream_t>(stream);
-    aspis::NormIn in;
-    st = start_norm(who, grads, n_chunks, opt->max_norm, sumsq, norm, opt->flags, workspace, s, &in);
-    if (st != ASPIS_OK) return st;
+    const aspis::NormIn in{nullptr, 0, sumsq, norm, opt->max_norm};
     const aspis::SgdArgs a{(float)opt->lr, (float)opt->momentum, (float)opt->weight_decay,
                            opt->nesterov != 0};
-    return launched(aspis::launch_sgd(params, grads, mean, copies, n_chunks, in, a,
-                                      (opt->flags & ASPIS_CLIP_SKIP_NONFINITE) != 0, s),
+    return launched(aspis::launch_sgd(params, grads, mean, copies, n_chunks,
+                                      (opt->flags & ASPIS_CLIP_HAVE_SUMSQ) != 0,
+                                      static_cast<double *>(workspace), in, a,
+                                      (opt->flags & ASPIS_CLIP_SKIP_NONFINITE) != 0,
+                                      static_cast<hipStream_t>(stream)),
                     who);
 }
 
@@ -328,10 +309,7 @@ aspis_status aspis_clipped_adamw(const aspis_chunk *params, const aspis_chunk *g
                     "%s: lr=%g beta_one=%g beta_two=%g eps=%g weight_decay=%g step=%lld", who,
                     opt->lr, opt->beta_one, opt->beta_two, opt->eps, opt->weight_decay,
                     (long long)opt->step);
-    const hipStream_t s = static_cast<hipStream_t>(stream);
-    aspis::NormIn in;
-    st = start_norm(who, grads, n_chunks, opt->max_norm, sumsq, norm, opt->flags, workspace, s, &in);
-    if (st != ASPIS_OK) return st;
+    const aspis::NormIn in{nullptr, 0, sumsq, norm, opt->max_norm};
     // the constants of a step, each rounded to f32 once
     const double t = (double)opt->step;
     const aspis::AdamArgs a{(float)(1.0 - opt->lr * opt->weight_decay),
@@ -342,8 +320,11 @@ aspis_status aspis_clipped_adamw(const aspis_chunk *params, const aspis_chunk *g
                             (float)(opt->lr / (1.0 - std::pow(opt->beta_one, t))),
                             (float)(1.0 / std::sqrt(1.0 - std::pow(opt->beta_two, t))),
                             (float)opt->eps};
-    return launched(aspis::launch_adamw(params, grads, mean, square, copies, n_chunks, in, a,
-                                        (opt->flags & ASPIS_CLIP_SKIP_NONFINITE) != 0, s),
+    return launched(aspis::launch_adamw(params, grads, mean, square, copies, n_chunks,
+                                        (opt->flags & ASPIS_CLIP_HAVE_SUMSQ) != 0,
+                                        static_cast<double *>(workspace), in, a,
+                                        (opt->flags & ASPIS_CLIP_SKIP_NONFINITE) != 0,
+                                        static_cast<hipStream_t>(stream)),
                     who);
 }
 

@@ -11,18 +11,24 @@
 namespace aspis {
 
 // Elements per chunk of a tensor list: a workgroup's unit of work.
-constexpr int kChunk = 16384;
-// aspis_chunk.info of a chunk: the tensor's aspis_dtype.  The table's
-// n_tensors further entries give tensor t's chunks: addr = the first one's
-// index, n = their number.
+constexpr int kChunk = 4096;
+// A table holds n_chunks chunks (info: the type, plus 4 times the tensor's
+// index among those that are not empty), then an entry per tensor: addr its
+// first chunk's index, n its number of chunks, info its index among those
+// that are not empty.
 inline int64_t chunks_of(int64_t numel) { return (numel + kChunk - 1) / kChunk; }
+constexpr int64_t kMaxChunks = int64_t(1) << 26;    // of a list: 2^38 elements
+constexpr int32_t kMaxTensors = 1 << 23;            // a workgroup each (their own norms)
+constexpr int64_t kMaxRow = int64_t(1) << 34;       // elements of a row: one launch
 
-// Workgroups of the norm pass over a list, and so its partial sums: a
-// function of the list alone, since the order of the sum follows it.
-constexpr int kNormGroups = 2048;
-inline int norm_groups(int64_t n_chunks) {
-    return (int)(n_chunks < kNormGroups ? n_chunks : kNormGroups);
-}
+// Workgroups of the norm pass over a list, at most, and so its partial sums:
+// a function of the list alone, since the order of the sum follows it.
+constexpr int kNormGroups = 1024;
+// Lists of up to so many chunks are one workgroup's work.
+constexpr int kSoloChunks = 16;
+// The workspace of a list, in doubles: the partial sums, then the sums of
+// runs of chunks for the tensors' own norms.
+inline int64_t norm_doubles(int64_t n_chunks) { return kNormGroups + 2 * n_chunks; }
 
 // The global norm's inputs to a kernel that applies it: n_partial sums of
 // squares (0: the sum is in *sumsq already), and where the results go.
@@ -34,13 +40,11 @@ struct NormIn {
     double max_norm;
 };
 
-hipError_t launch_list_sumsq(const aspis_chunk *table, int64_t n_chunks, double *partial,
-                             double *chunk_sums, hipStream_t s);
-hipError_t launch_list_norm(const aspis_chunk *table, int64_t n_chunks, int32_t n_tensors,
-                            const NormIn &in, const double *chunk_sums, float *each,
-                            hipStream_t s);
-hipError_t launch_list_scale(const aspis_chunk *table, const aspis_chunk *out, int64_t n_chunks,
-                             const NormIn &in, hipStream_t s);
+// ws: norm_doubles(n_chunks) doubles.  have_sumsq: *in.sumsq is given.
+hipError_t launch_norm(const aspis_chunk *table, int64_t n_chunks, int32_t n_tensors, double *ws,
+                       NormIn in, float *each, hipStream_t s);
+hipError_t launch_clip(const aspis_chunk *table, const aspis_chunk *out, int64_t n_chunks,
+                       bool have_sumsq, double *ws, NormIn in, hipStream_t s);
 
 struct SgdArgs {
     float lr, momentum, decay;
@@ -51,11 +55,12 @@ struct AdamArgs {
 };
 hipError_t launch_sgd(const aspis_chunk *params, const aspis_chunk *grads,
                       const aspis_chunk *mean, const aspis_chunk *copies, int64_t n_chunks,
-                      const NormIn &in, const SgdArgs &a, bool skip, hipStream_t s);
+                      bool have_sumsq, double *ws, const NormIn &in, const SgdArgs &a, bool skip,
+                      hipStream_t s);
 hipError_t launch_adamw(const aspis_chunk *params, const aspis_chunk *grads,
                         const aspis_chunk *mean, const aspis_chunk *square,
-                        const aspis_chunk *copies, int64_t n_chunks, const NormIn &in,
-                        const AdamArgs &a, bool skip, hipStream_t s);
+                        const aspis_chunk *copies, int64_t n_chunks, bool have_sumsq, double *ws,
+                        const NormIn &in, const AdamArgs &a, bool skip, hipStream_t s);
 
 // Rows.  A row of up to kRowVecs 16-byte vectors is held in one workgroup's
 // registers; a longer one is cut into segments.

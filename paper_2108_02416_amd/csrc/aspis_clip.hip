@@ -104,13 +104,44 @@ using Ptr = const typename E::T GLOBAL *;
 template <typename E>
 using MutPtr = typename E::T GLOBAL *;
 
-template <typename E>
+// Once: the data is not needed again soon (non-temporal).
+enum class Use { Again, Once };
+
+template <typename E, Use USE = Use::Again>
 __device__ __forceinline__ u32x4 load_vec(Ptr<E> p) {
-    return *(const typename E::Vec GLOBAL *)p;
+    const typename E::Vec GLOBAL *q = (const typename E::Vec GLOBAL *)p;
+    if constexpr (USE == Use::Once) return __builtin_nontemporal_load(q);
+    return *q;
 }
-template <typename E>
+template <typename E, Use USE = Use::Again>
 __device__ __forceinline__ void store_vec(MutPtr<E> p, u32x4 v) {
-    *(typename E::Vec GLOBAL *)p = v;
+    typename E::Vec GLOBAL *q = (typename E::Vec GLOBAL *)p;
+    if constexpr (USE == Use::Once) __builtin_nontemporal_store((typename E::Vec)v, q);
+    else *q = v;
+}
+
+// The vector at element i of n elements, zeros past the end.
+template <typename E, Use USE>
+__device__ __forceinline__ u32x4 load_part(Ptr<E> p, int i, int n) {
+    if (i + E::V <= n) return load_vec<E, USE>(p + i);
+    u32x4 w = {0, 0, 0, 0};
+    if (i < n) {
+        float x[E::V];
+#pragma unroll
+        for (int j = 0; j < E::V; ++j) x[j] = i + j < n ? E::get(p[i + j]) : 0.0f;
+        w = E::pack(x);
+    }
+    return w;
+}
+template <typename E, Use USE>
+__device__ __forceinline__ void store_part(MutPtr<E> p, int i, int n, const float (&x)[E::V]) {
+    if (i + E::V <= n) {
+        store_vec<E, USE>(p + i, E::pack(x));
+    } else if (i < n) {
+#pragma unroll
+        for (int j = 0; j < E::V; ++j)
+            if (i + j < n) p[i + j] = E::put(x[j]);
+    }
 }
 
 // Calls f with the element type of a dtype code (uniform over the workgroup).
@@ -124,12 +155,26 @@ __device__ __forceinline__ void with_type(int dtype, F &&f) {
 // ---------------------------------------------------------------------------
 // sums
 
+// v of the lane that the DPP control names.
+template <int CTRL>
+__device__ __forceinline__ double dpp(double v) {
+    const uint64_t w = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)w, CTRL, 0xF, 0xF, true);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(w >> 32), CTRL, 0xF, 0xF, true);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+
 // Over groups of L consecutive lanes (a power of two <= 64), to every lane.
-// Each step adds the same two values on both sides, so all lanes agree.
+// Both partners of a step add the same two values, so all lanes agree.  Up
+// to 16 lanes by DPP: within quads, then the mirrors pair the quads.
 template <int L>
 __device__ __forceinline__ double lanes_sum(double v) {
-#pragma unroll
-    for (int m = 1; m < L; m <<= 1) v += __shfl_xor(v, m, 64);
+    if constexpr (L >= 2) v += dpp<0xB1>(v);    // quad_perm 1,0,3,2
+    if constexpr (L >= 4) v += dpp<0x4E>(v);    // quad_perm 2,3,0,1
+    if constexpr (L >= 8) v += dpp<0x141>(v);   // row_half_mirror
+    if constexpr (L >= 16) v += dpp<0x140>(v);  // row_mirror
+    if constexpr (L >= 32) v += __shfl_xor(v, 16, 64);
+    if constexpr (L >= 64) v += __shfl_xor(v, 32, 64);
     return v;
 }
 
@@ -170,22 +215,28 @@ __device__ __forceinline__ void add_squares(u32x4 w, double (&acc)[2]) {
     for (int j = 0; j < E::V; ++j) acc[j & 1] = add_square(x[j], acc[j & 1]);
 }
 
-// Adds the squares of n elements, split over the B threads of a workgroup.
-template <typename E, int B, int U>
-__device__ __forceinline__ void span_squares(Ptr<E> p, int n, double (&acc)[2]) {
-    const int nv = n / E::V;
-    int i = threadIdx.x;
-    for (; i + (U - 1) * B < nv; i += U * B) {
-        u32x4 w[U];
+// A chunk in the registers of 256 threads: U vectors each, thread t holding
+// vectors t, t + 256, ...
+template <typename E>
+struct Tile {
+    static constexpr int U = kChunk / E::V / 256;
+    u32x4 w[U];
+
+    template <Use USE>
+    __device__ __forceinline__ void load(Ptr<E> p, int n, int t) {
+        if (n == kChunk) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) w[u] = load_vec<E>(p + (int64_t)(i + u * B) * E::V);
+            for (int u = 0; u < U; ++u) w[u] = load_vec<E, USE>(p + (t + u * 256) * E::V);
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u) w[u] = load_part<E, USE>(p, (t + u * 256) * E::V, n);
+        }
+    }
+    __device__ __forceinline__ void squares(double (&acc)[2]) const {
 #pragma unroll
         for (int u = 0; u < U; ++u) add_squares<E>(w[u], acc);
     }
-    for (; i < nv; i += B) add_squares<E>(load_vec<E>(p + (int64_t)i * E::V), acc);
-    const int rest = nv * E::V + threadIdx.x;
-    if (rest < n) acc[0] = add_square(E::get(p[rest]), acc[0]);
-}
+};
 
 // ---------------------------------------------------------------------------
 // the coefficient
@@ -226,31 +277,19 @@ __device__ __forceinline__ double take_sumsq(const NormIn &in) {
     return s;
 }
 
-// out = c * x over n elements, split over the B threads of a workgroup; out
-// may be x.
-template <typename E, int B, int U>
-__device__ __forceinline__ void span_scale(Ptr<E> p, MutPtr<E> o, int n, Coef c) {
-    const int nv = n / E::V;
-    auto scaled = [&](u32x4 w) {
+// Writes c * the tile; the output may be the input.
+template <typename E, Use USE>
+__device__ __forceinline__ void store_scaled(const Tile<E> &tile, MutPtr<E> o, int n, int t,
+                                             Coef c) {
+#pragma unroll
+    for (int u = 0; u < Tile<E>::U; ++u) {
         float x[E::V];
-        E::unpack(w, x);
+        E::unpack(tile.w[u], x);
 #pragma unroll
         for (int j = 0; j < E::V; ++j) x[j] = c(x[j]);
-        return E::pack(x);
-    };
-    int i = threadIdx.x;
-    for (; i + (U - 1) * B < nv; i += U * B) {
-        u32x4 w[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) w[u] = load_vec<E>(p + (int64_t)(i + u * B) * E::V);
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            store_vec<E>(o + (int64_t)(i + u * B) * E::V, scaled(w[u]));
+        if (n == kChunk) store_vec<E, USE>(o + (t + u * 256) * E::V, E::pack(x));
+        else store_part<E, USE>(o, (t + u * 256) * E::V, n, x);
     }
-    for (; i < nv; i += B)
-        store_vec<E>(o + (int64_t)i * E::V, scaled(load_vec<E>(p + (int64_t)i * E::V)));
-    const int rest = nv * E::V + threadIdx.x;
-    if (rest < n) o[rest] = E::put(c(E::get(p[rest])));
 }
 
 // ---------------------------------------------------------------------------
@@ -258,33 +297,55 @@ __device__ __forceinline__ void span_scale(Ptr<E> p, MutPtr<E> o, int n, Coef c)
 
 constexpr int kListBlock = 256;
 
+__device__ __forceinline__ int chunk_type(const aspis_chunk &c) { return c.info & 3; }
+__device__ __forceinline__ int chunk_tensor(const aspis_chunk &c) { return c.info >> 2; }
+
+// Adds the squares of a chunk, split over 256 threads.
+template <Use USE>
+__device__ __forceinline__ void chunk_squares(const aspis_chunk &c, int t, double (&acc)[2]) {
+    with_type(chunk_type(c), [&](auto e) {
+        typedef decltype(e) E;
+        Tile<E> tile;
+        tile.template load<USE>((Ptr<E>)c.addr, c.n, t);
+        tile.squares(acc);
+    });
+}
+
+// The norm pass: a fixed number of workgroups over groups of `group` chunks
+// in turn, one partial sum each.  Chunks from `keep` on are read to stay in
+// the last-level cache for the pass that follows.  runs, when not NULL,
+// receives the sum of every run of one tensor's chunks in a group, at the
+// group's index plus the tensor's: of two runs one after the other at least
+// one index is one up, so no two share a place.
 __global__ __launch_bounds__(kListBlock) void
-list_sumsq_kernel(const aspis_chunk *__restrict__ table, int64_t n_chunks, double *partial,
-                  double *chunk_sums) {
+list_sumsq_kernel(const aspis_chunk *__restrict__ table, int64_t n_chunks, int group,
+                  int64_t keep, double *partial, double *runs) {
     double acc[2] = {0.0, 0.0};
     double total = 0.0;
-    for (int64_t k = blockIdx.x; k < n_chunks; k += gridDim.x) {
-        const aspis_chunk c = table[k];
-        with_type(c.info, [&](auto e) {
-            typedef decltype(e) E;
-            span_squares<E, kListBlock, 4>((Ptr<E>)c.addr, c.n, acc);
-        });
-        if (chunk_sums != nullptr) {
+    int64_t first = (int64_t)blockIdx.x * group, k = first;
+    aspis_chunk next = table[k];
+    while (k < n_chunks) {
+        const aspis_chunk c = next;
+        const int64_t now = k, now_first = first;
+        if (++k == first + group || k >= n_chunks) k = first += (int64_t)gridDim.x * group;
+        next = table[k < n_chunks ? k : now];
+        if (now < keep) chunk_squares<Use::Once>(c, threadIdx.x, acc);
+        else chunk_squares<Use::Again>(c, threadIdx.x, acc);
+        if (runs != nullptr && (first != now_first || chunk_tensor(next) != chunk_tensor(c))) {
             const double s = block_sum<kListBlock>(acc[0] + acc[1]);
-            if (threadIdx.x == 0) chunk_sums[k] = s;
+            if (threadIdx.x == 0) runs[now_first / group + chunk_tensor(c)] = s;
             total += s;
             acc[0] = acc[1] = 0.0;
         }
     }
-    if (chunk_sums == nullptr) total = block_sum<kListBlock>(acc[0] + acc[1]);
+    if (runs == nullptr) total = block_sum<kListBlock>(acc[0] + acc[1]);
     if (threadIdx.x == 0) partial[blockIdx.x] = total;
 }
 
-// Workgroup 0 joins the partial sums; the others, one wave per tensor, the
-// tensors' own chunk sums.
+// Workgroup 0 joins the partial sums, workgroup 1 + t the runs of tensor t.
 __global__ __launch_bounds__(kListBlock) void
-list_norm_kernel(const aspis_chunk *__restrict__ tensors, int32_t n_tensors, NormIn in,
-                 const double *__restrict__ chunk_sums, float *each) {
+list_norm_kernel(const aspis_chunk *__restrict__ tensors, int group, NormIn in,
+                 const double *__restrict__ runs, float *each) {
     if (blockIdx.x == 0) {
         if (in.n_partial > 0) {
             take_sumsq<kListBlock>(in);
@@ -294,40 +355,56 @@ list_norm_kernel(const aspis_chunk *__restrict__ tensors, int32_t n_tensors, Nor
         }
         return;
     }
-    const int t = (blockIdx.x - 1) * (kListBlock / 64) + threadIdx.x / 64;
-    if (t >= n_tensors) return;
-    const aspis_chunk c = tensors[t];
-    double v = 0.0;
-    for (int i = threadIdx.x % 64; i < c.n; i += 64) v += chunk_sums[c.addr + i];
-    v = lanes_sum<64>(v);
-    if (threadIdx.x % 64 == 0) each[t] = (float)sqrt(v);
+    const aspis_chunk c = tensors[blockIdx.x - 1];
+    double s = 0.0;
+    if (c.n > 0) {
+        const int64_t first = (int64_t)c.addr / group, last = ((int64_t)c.addr + c.n - 1) / group;
+        s = block_sum_of<kListBlock>(runs + first + c.info, (int)(last - first) + 1);
+    }
+    if (threadIdx.x == 0) each[blockIdx.x - 1] = (float)sqrt(s);
 }
 
+// One chunk per workgroup, the last first where the list is longer than
+// what the cache keeps of it.  The chunk is on its way while the
+// coefficient is worked out, unless that may make it unnecessary.
 __global__ __launch_bounds__(kListBlock) void
 list_scale_kernel(const aspis_chunk *__restrict__ table, const aspis_chunk *__restrict__ out,
-                  int64_t n_chunks, NormIn in) {
-    const Coef coef = coefficient(take_sumsq<kListBlock>(in), in.max_norm);
-    if (out == nullptr && coef.one()) return;   // in place: already there
-    for (int64_t k = blockIdx.x; k < n_chunks; k += gridDim.x) {
-        const aspis_chunk c = table[k];
-        const uint64_t to = out != nullptr ? out[k].addr : c.addr;
-        with_type(c.info, [&](auto e) {
+                  int64_t first, int64_t step, NormIn in) {
+    const int64_t k = first + step * blockIdx.x;
+    const aspis_chunk c = table[k];
+    const uint64_t to = out != nullptr ? out[k].addr : c.addr;
+    if (out == nullptr) {
+        const Coef coef = coefficient(take_sumsq<kListBlock>(in), in.max_norm);
+        if (coef.one()) return;   // in place: already there
+        with_type(chunk_type(c), [&](auto e) {
             typedef decltype(e) E;
-            span_scale<E, kListBlock, 4>((Ptr<E>)c.addr, (MutPtr<E>)to, c.n, coef);
+            Tile<E> tile;
+            tile.template load<Use::Once>((Ptr<E>)c.addr, c.n, threadIdx.x);
+            store_scaled<E, Use::Once>(tile, (MutPtr<E>)to, c.n, threadIdx.x, coef);
         });
+        return;
     }
+    with_type(chunk_type(c), [&](auto e) {
+        typedef decltype(e) E;
+        Tile<E> tile;
+        tile.template load<Use::Once>((Ptr<E>)c.addr, c.n, threadIdx.x);
+        const Coef coef = coefficient(take_sumsq<kListBlock>(in), in.max_norm);
+        store_scaled<E, Use::Once>(tile, (MutPtr<E>)to, c.n, threadIdx.x, coef);
+    });
 }
 
 // ---------------------------------------------------------------------------
-// the updates: four elements per lane and step, so that the f32 tensors move
-// 16 bytes and 16-bit ones 8
+// the updates: four elements per lane, so that the f32 tensors move 16 bytes
+// and 16-bit ones 8
 
-__device__ __forceinline__ void load_four(uint64_t addr, int dtype, int64_t i, float (&x)[4]) {
+template <Use USE>
+__device__ __forceinline__ void load_four(uint64_t addr, int dtype, int i, float (&x)[4]) {
     if (dtype == ASPIS_F32) {
-        F32::unpack(load_vec<F32>((Ptr<F32>)addr + i), x);
+        F32::unpack(load_vec<F32, USE>((Ptr<F32>)addr + i), x);
         return;
     }
-    const u32x2 w = *(const u32x2_at2 GLOBAL *)((const uint16_t GLOBAL *)addr + i);
+    const u32x2_at2 GLOBAL *q = (const u32x2_at2 GLOBAL *)((const uint16_t GLOBAL *)addr + i);
+    const u32x2 w = USE == Use::Once ? (u32x2)__builtin_nontemporal_load(q) : (u32x2)*q;
     float y[8];
     if (dtype == ASPIS_BF16) BF16::unpack((u32x4){w.x, w.y, 0, 0}, y);
     else F16::unpack((u32x4){w.x, w.y, 0, 0}, y);
@@ -335,23 +412,25 @@ __device__ __forceinline__ void load_four(uint64_t addr, int dtype, int64_t i, f
     for (int j = 0; j < 4; ++j) x[j] = y[j];
 }
 
-__device__ __forceinline__ void store_four(uint64_t addr, int dtype, int64_t i,
-                                           const float (&x)[4]) {
+template <Use USE>
+__device__ __forceinline__ void store_four(uint64_t addr, int dtype, int i, const float (&x)[4]) {
     if (dtype == ASPIS_F32) {
-        store_vec<F32>((MutPtr<F32>)addr + i, F32::pack(x));
+        store_vec<F32, USE>((MutPtr<F32>)addr + i, F32::pack(x));
         return;
     }
     const float y[8] = {x[0], x[1], x[2], x[3], 0, 0, 0, 0};
     const u32x4 w = dtype == ASPIS_BF16 ? BF16::pack(y) : F16::pack(y);
-    *(u32x2_at2 GLOBAL *)((uint16_t GLOBAL *)addr + i) = (u32x2){w.x, w.y};
+    u32x2_at2 GLOBAL *q = (u32x2_at2 GLOBAL *)((uint16_t GLOBAL *)addr + i);
+    if constexpr (USE == Use::Once) __builtin_nontemporal_store((u32x2_at2){w.x, w.y}, q);
+    else *q = (u32x2_at2){w.x, w.y};
 }
 
-__device__ __forceinline__ float load_one(uint64_t addr, int dtype, int64_t i) {
+__device__ __forceinline__ float load_one(uint64_t addr, int dtype, int i) {
     float x = 0.0f;
     with_type(dtype, [&](auto e) { x = decltype(e)::get(((Ptr<decltype(e)>)addr)[i]); });
     return x;
 }
-__device__ __forceinline__ void store_one(uint64_t addr, int dtype, int64_t i, float x) {
+__device__ __forceinline__ void store_one(uint64_t addr, int dtype, int i, float x) {
     with_type(dtype, [&](auto e) {
         ((MutPtr<decltype(e)>)addr)[i] = decltype(e)::put(x);
     });
@@ -391,54 +470,159 @@ struct UpdateTables {
     const aspis_chunk *params, *grads, *state[2], *copies;
 };
 
+// Chunk k of all the update's tensors.
 template <typename Rule>
-__global__ __launch_bounds__(kListBlock) void
-update_kernel(UpdateTables t, int64_t n_chunks, NormIn in, Rule rule, bool skip) {
-    constexpr int S = Rule::S, W = S > 0 ? S : 1;
-    const double sumsq = take_sumsq<kListBlock>(in);
-    if (skip && !(sumsq <= DBL_MAX)) return;
-    const Coef coef = coefficient(sumsq, in.max_norm);
-    for (int64_t k = blockIdx.x; k < n_chunks; k += gridDim.x) {
-        const aspis_chunk g = t.grads[k];
-        const uint64_t pa = t.params[k].addr;
-        uint64_t sa[W] = {};
+struct UpdateChunk {
+    static constexpr int S = Rule::S, W = S > 0 ? S : 1;
+    uint64_t p, s[W], g, copy;
+    int n, g_type, copy_type;   // copy_type < 0: no copy
+
+    __device__ __forceinline__ UpdateChunk(const UpdateTables &t, int64_t k) {
+        const aspis_chunk c = t.grads[k];
+        n = c.n;
+        g = c.addr;
+        g_type = chunk_type(c);
+        p = t.params[k].addr;
 #pragma unroll
-        for (int j = 0; j < S; ++j) sa[j] = t.state[j][k].addr;
-        const aspis_chunk copy = t.copies != nullptr ? t.copies[k] : aspis_chunk{0, 0, 0};
-        const int nv = g.n / 4;
-        for (int i = threadIdx.x; i < nv; i += kListBlock) {
-            const int64_t at = (int64_t)i * 4;
-            float x[4], p[4], s[W][4];
-            load_four(g.addr, g.info, at, x);
-            load_four(pa, ASPIS_F32, at, p);
+        for (int j = 0; j < W; ++j) s[j] = j < S ? t.state[j][k].addr : 0;
+        copy = 0;
+        copy_type = -1;
+        if (t.copies != nullptr) {
+            const aspis_chunk o = t.copies[k];
+            copy = o.addr;
+            copy_type = chunk_type(o);
+        }
+    }
+
+    // Updates elements i to i + 3, those below n; coef() is called when the
+    // loads are on their way.
+    template <Use OUT, typename C>
+    __device__ __forceinline__ void four(const Rule &rule, int i, C &&coef) const {
+        float x[4], q[4], v[W][4];
+        if (i + 4 <= n) {
+            load_four<Use::Once>(g, g_type, i, x);
+            load_four<Use::Once>(p, ASPIS_F32, i, q);
 #pragma unroll
-            for (int j = 0; j < S; ++j) load_four(sa[j], ASPIS_F32, at, s[j]);
+            for (int j = 0; j < S; ++j) load_four<Use::Once>(s[j], ASPIS_F32, i, v[j]);
+            const Coef c = coef();
 #pragma unroll
             for (int l = 0; l < 4; ++l) {
                 float one[W];
 #pragma unroll
-                for (int j = 0; j < S; ++j) one[j] = s[j][l];
-                rule(coef(x[l]), p[l], one);
+                for (int j = 0; j < S; ++j) one[j] = v[j][l];
+                rule(c(x[l]), q[l], one);
 #pragma unroll
-                for (int j = 0; j < S; ++j) s[j][l] = one[j];
+                for (int j = 0; j < S; ++j) v[j][l] = one[j];
             }
-            store_four(pa, ASPIS_F32, at, p);
+            store_four<OUT>(p, ASPIS_F32, i, q);
 #pragma unroll
-            for (int j = 0; j < S; ++j) store_four(sa[j], ASPIS_F32, at, s[j]);
-            if (copy.n > 0) store_four(copy.addr, copy.info, at, p);
+            for (int j = 0; j < S; ++j) store_four<OUT>(s[j], ASPIS_F32, i, v[j]);
+            if (copy_type >= 0) store_four<OUT>(copy, copy_type, i, q);
+            return;
         }
-        const int i = nv * 4 + threadIdx.x;
-        if (i < g.n) {
-            float one[W], p = load_one(pa, ASPIS_F32, i);
+        const Coef c = coef();
+        for (; i < n; ++i) {
+            float one[W], y = load_one(p, ASPIS_F32, i);
 #pragma unroll
-            for (int j = 0; j < S; ++j) one[j] = load_one(sa[j], ASPIS_F32, i);
-            rule(coef(load_one(g.addr, g.info, i)), p, one);
-            store_one(pa, ASPIS_F32, i, p);
+            for (int j = 0; j < S; ++j) one[j] = load_one(s[j], ASPIS_F32, i);
+            rule(c(load_one(g, g_type, i)), y, one);
+            store_one(p, ASPIS_F32, i, y);
 #pragma unroll
-            for (int j = 0; j < S; ++j) store_one(sa[j], ASPIS_F32, i, one[j]);
-            if (copy.n > 0) store_one(copy.addr, copy.info, i, p);
+            for (int j = 0; j < S; ++j) store_one(s[j], ASPIS_F32, i, one[j]);
+            if (copy_type >= 0) store_one(copy, copy_type, i, y);
         }
     }
+};
+
+// One wave and one step of four elements per lane: the memory system sees
+// each tensor's lines in order, 1 KB at a time.
+constexpr int kUpdateBlock = 64;
+constexpr int kUpdateParts = kChunk / (4 * kUpdateBlock);
+
+template <typename Rule, Use OUT>
+__global__ __launch_bounds__(kUpdateBlock) void
+update_kernel(UpdateTables t, int64_t first, int64_t step, NormIn in, Rule rule, bool skip) {
+    const double sumsq = *in.sumsq;
+    if (blockIdx.x == 0 && threadIdx.x == 0) *in.norm = (float)sqrt(sumsq);
+    if (skip && !(sumsq <= DBL_MAX)) return;
+    const UpdateChunk<Rule> c(t, first + step * (blockIdx.x / kUpdateParts));
+    const int i = ((int)(blockIdx.x % kUpdateParts) * kUpdateBlock + (int)threadIdx.x) * 4;
+    if (i < c.n)
+        c.template four<OUT>(rule, i, [&] { return coefficient(sumsq, in.max_norm); });
+}
+
+// ---------------------------------------------------------------------------
+// short lists: everything in one workgroup and one launch
+
+struct NoApply {
+    __device__ void operator()(int64_t, int, double) const {}
+};
+struct Scale {
+    const aspis_chunk *table, *out;
+    double max_norm;
+    __device__ void operator()(int64_t k, int t, double sumsq) const {
+        const Coef coef = coefficient(sumsq, max_norm);
+        if (out == nullptr && coef.one()) return;
+        const aspis_chunk c = table[k];
+        const uint64_t to = out != nullptr ? out[k].addr : c.addr;
+        with_type(chunk_type(c), [&](auto e) {
+            typedef decltype(e) E;
+            Tile<E> tile;
+            tile.template load<Use::Again>((Ptr<E>)c.addr, c.n, t);
+            store_scaled<E, Use::Again>(tile, (MutPtr<E>)to, c.n, t, coef);
+        });
+    }
+};
+template <typename Rule>
+struct Update {
+    UpdateTables tables;
+    Rule rule;
+    double max_norm;
+    bool skip;
+    __device__ void operator()(int64_t k, int t, double sumsq) const {
+        if (skip && !(sumsq <= DBL_MAX)) return;
+        const Coef coef = coefficient(sumsq, max_norm);
+        const UpdateChunk<Rule> c(tables, k);
+        for (int i = t * 4; i < c.n; i += 4 * 256)
+            c.template four<Use::Again>(rule, i, [&] { return coef; });
+    }
+};
+
+// Four groups of 256 threads take the chunks in turn: their sums (one per
+// wave), the norm, then what is applied to them.
+constexpr int kSoloBlock = 1024;
+static_assert(kSoloChunks * 4 == 64, "a wave holds all the waves' sums");
+
+template <typename Apply>
+__global__ __launch_bounds__(kSoloBlock) void
+solo_kernel(const aspis_chunk *__restrict__ table, int n_chunks, const aspis_chunk *tensors,
+            int n_tensors, bool have_sumsq, NormIn in, float *each, Apply apply) {
+    __shared__ double sums[kSoloChunks * 4];
+    const int t = threadIdx.x % 256, group = threadIdx.x / 256;
+    double total;
+    if (have_sumsq) {
+        total = *in.sumsq;
+    } else {
+        for (int k = group; k < n_chunks; k += kSoloBlock / 256) {
+            double acc[2] = {0.0, 0.0};
+            chunk_squares<Use::Again>(table[k], t, acc);
+            const double s = lanes_sum<64>(acc[0] + acc[1]);
+            if (t % 64 == 0) sums[k * 4 + t / 64] = s;
+        }
+        __syncthreads();
+        const int lane = threadIdx.x % 64;
+        total = lanes_sum<64>(lane < n_chunks * 4 ? sums[lane] : 0.0);
+        if (threadIdx.x == 0) *in.sumsq = total;
+        if (each != nullptr)
+            for (int i = threadIdx.x; i < n_tensors; i += kSoloBlock) {
+                const aspis_chunk c = tensors[i];
+                double s = 0.0;
+                for (int j = 0; j < c.n * 4; ++j) s += sums[c.addr * 4 + j];
+                each[i] = (float)sqrt(s);
+            }
+    }
+    if (threadIdx.x == 0) *in.norm = (float)sqrt(total);
+    for (int k = group; k < n_chunks; k += kSoloBlock / 256) apply(k, t, total);
 }
 
 // ---------------------------------------------------------------------------
@@ -456,18 +640,7 @@ __global__ __launch_bounds__(B) void row_kernel(RowArgs a) {
         const Ptr<E> p = (Ptr<E>)a.x + row * a.ld;
         u32x4 w[R];
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const int i = (lane + r * L) * V;
-            w[r] = (u32x4){0, 0, 0, 0};
-            if (i + V <= d) {
-                w[r] = load_vec<E>(p + i);
-            } else if (i < d) {
-                float x[V];
-#pragma unroll
-                for (int j = 0; j < V; ++j) x[j] = i + j < d ? E::get(p[i + j]) : 0.0f;
-                w[r] = E::pack(x);
-            }
-        }
+        for (int r = 0; r < R; ++r) w[r] = load_part<E, Use::Once>(p, (lane + r * L) * V, d);
         double acc[2] = {0.0, 0.0};
 #pragma unroll
         for (int r = 0; r < R; ++r) add_squares<E>(w[r], acc);
@@ -481,18 +654,11 @@ __global__ __launch_bounds__(B) void row_kernel(RowArgs a) {
         const MutPtr<E> o = (MutPtr<E>)a.out + row * a.ldo;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const int i = (lane + r * L) * V;
             float x[V];
             E::unpack(w[r], x);
 #pragma unroll
             for (int j = 0; j < V; ++j) x[j] = c(x[j]);
-            if (i + V <= d) {
-                store_vec<E>(o + i, E::pack(x));
-            } else if (i < d) {
-#pragma unroll
-                for (int j = 0; j < V; ++j)
-                    if (i + j < d) o[i + j] = E::put(x[j]);
-            }
+            store_part<E, Use::Once>(o, (lane + r * L) * V, d, x);
         }
     }
 }
@@ -503,48 +669,52 @@ __global__ __launch_bounds__(kListBlock) void empty_rows_kernel(float *norms, in
         norms[i] = 0.0f;
 }
 
-// Segments of long rows.  One launch scales the segments of rows
-// [scale0, scale0 + n_scale) whose sums are there, and sums those of rows
-// [sum0, sum0 + n_sum); the two kinds of work alternate over the workgroups.
+// Segments of long rows.  One launch sums the segments of rows
+// [sum0, sum0 + ...) and scales those of the rows before, whose sums are
+// there and which the last-level cache still holds; the two kinds of
+// workgroups are spread evenly over the launch.
 struct SegArgs {
     RowArgs a;
     int64_t seg;
-    int32_t parts;
+    int32_t parts;    // segments of a row, summed by a workgroup each
+    int32_t tiles;    // chunks of a row, scaled by a workgroup each
     int64_t scale0, sum0;
-    int64_t n_scale, n_sum;   // segments
+    int64_t n_scale, n_sum;   // workgroups of each kind
 };
 
 template <typename E>
 __global__ __launch_bounds__(kListBlock) void segment_kernel(SegArgs g) {
-    const int64_t both = g.n_scale < g.n_sum ? g.n_scale : g.n_sum;
-    const int64_t b = blockIdx.x;
-    bool scale;
-    int64_t item;
-    if (b < 2 * both) {
-        scale = (b & 1) != 0;
-        item = b >> 1;
-    } else {
-        scale = g.n_scale > g.n_sum;
-        item = b - both;
-    }
-    const int64_t row = (scale ? g.scale0 : g.sum0) + item / g.parts;
-    const int part = (int)(item % g.parts);
-    const int64_t first = part * g.seg;
-    const int n = (int)(g.a.d - first < g.seg ? g.a.d - first : g.seg);
-    const Ptr<E> p = (Ptr<E>)g.a.x + row * g.a.ld + first;
-    double *sums = g.a.partial + row * g.parts;
-    if (!scale) {
+    const int64_t b = blockIdx.x, all = g.n_scale + g.n_sum;
+    const int64_t before = b * g.n_sum / all;
+    if ((b + 1) * g.n_sum / all > before) {
+        const int64_t row = g.sum0 + before / g.parts;
+        const int part = (int)(before % g.parts);
+        int64_t at = part * g.seg;
+        const int64_t end = at + g.seg < g.a.d ? at + g.seg : g.a.d;
+        const Ptr<E> p = (Ptr<E>)g.a.x + row * g.a.ld;
         double acc[2] = {0.0, 0.0};
-        span_squares<E, kListBlock, 4>(p, n, acc);
+        for (; at < end; at += kChunk) {
+            Tile<E> tile;
+            const int n = (int)(end - at < kChunk ? end - at : kChunk);
+            if (g.a.out == nullptr) tile.template load<Use::Once>(p + at, n, threadIdx.x);
+            else tile.template load<Use::Again>(p + at, n, threadIdx.x);
+            tile.squares(acc);
+        }
         const double s = block_sum<kListBlock>(acc[0] + acc[1]);
-        if (threadIdx.x == 0) sums[part] = s;
+        if (threadIdx.x == 0) g.a.partial[row * g.parts + part] = s;
         return;
     }
-    const double s = block_sum_of<kListBlock>(sums, g.parts);
-    if (part == 0 && threadIdx.x == 0 && g.a.norms != nullptr) g.a.norms[row] = (float)sqrt(s);
+    const int64_t item = b - before;
+    const int64_t row = g.scale0 + item / g.tiles;
+    const int64_t at = item % g.tiles * kChunk;
+    const int n = (int)(g.a.d - at < kChunk ? g.a.d - at : kChunk);
+    const double s = block_sum_of<kListBlock>(g.a.partial + row * g.parts, g.parts);
+    if (at == 0 && threadIdx.x == 0 && g.a.norms != nullptr) g.a.norms[row] = (float)sqrt(s);
     const Coef c = coefficient(s, g.a.max_norm);
     if (g.a.out == g.a.x && c.one()) return;
-    span_scale<E, kListBlock, 4>(p, (MutPtr<E>)g.a.out + row * g.a.ldo + first, n, c);
+    Tile<E> tile;
+    tile.template load<Use::Once>((Ptr<E>)g.a.x + row * g.a.ld + at, n, threadIdx.x);
+    store_scaled<E, Use::Once>(tile, (MutPtr<E>)g.a.out + row * g.a.ldo + at, n, threadIdx.x, c);
 }
 
 // The norms alone of long rows, from their segments' sums.
@@ -553,6 +723,9 @@ __global__ __launch_bounds__(kListBlock) void segment_norm_kernel(const double *
     const double s = block_sum_of<kListBlock>(sums + (int64_t)blockIdx.x * parts, parts);
     if (threadIdx.x == 0) norms[blockIdx.x] = (float)sqrt(s);
 }
+
+constexpr int64_t kMaxGrid = int64_t(1) << 23;   // workgroups of one launch
+constexpr int64_t kRowGroupBytes = 64 << 20;
 
 template <typename E, int L, int B, int R>
 void start_rows(const RowArgs &a, hipStream_t s) {
@@ -578,82 +751,159 @@ hipError_t rows_of(const RowArgs &a, hipStream_t s) {
         return hipGetLastError();
     }
     const RowSplit split = row_split(a.d, (int)sizeof(typename E::T));
+    SegArgs g{};
+    g.a = a;
+    g.seg = split.seg;
+    g.parts = split.parts;
+    g.tiles = (int32_t)chunks_of(a.d);
     // rows per launch: what stays in the last-level cache until the next
     // launch scales it
     const int64_t bytes = a.d * (int64_t)sizeof(typename E::T);
-    int64_t step = (int64_t)(64 << 20) / bytes;
+    int64_t step = a.out != nullptr ? kRowGroupBytes / bytes : kMaxGrid / split.parts;
+    const int64_t most = kMaxGrid / ((int64_t)g.tiles + g.parts);
+    if (step > most) step = most;
     if (step < 1) step = 1;
-    if (a.out == nullptr) step = a.rows;
-    while (step * split.parts > (1 << 20) && step > 1) step = (step + 1) / 2;
     for (int64_t r = 0; r < a.rows + (a.out != nullptr ? step : 0); r += step) {
-        SegArgs g{};
-        g.a = a;
-        g.seg = split.seg;
-        g.parts = split.parts;
+        auto group = [&](int64_t first) {   // rows of the group that begins there
+            if (first < 0 || first >= a.rows) return (int64_t)0;
+            return a.rows - first < step ? a.rows - first : step;
+        };
         g.sum0 = r;
-        const int64_t sum_rows = r < a.rows ? (a.rows - r < step ? a.rows - r : step) : 0;
-        g.n_sum = sum_rows * split.parts;
-        if (a.out != nullptr && r > 0) {
-            g.scale0 = r - step;
-            g.n_scale = (a.rows - g.scale0 < step ? a.rows - g.scale0 : step) * split.parts;
-        }
-        if (g.n_sum + g.n_scale == 0) continue;
+        g.scale0 = r - step;
+        g.n_sum = group(r) * g.parts;
+        g.n_scale = a.out != nullptr ? group(r - step) * g.tiles : 0;
         segment_kernel<E><<<(unsigned)(g.n_sum + g.n_scale), kListBlock, 0, s>>>(g);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     if (a.out == nullptr)
-        segment_norm_kernel<<<(unsigned)a.rows, kListBlock, 0, s>>>(a.partial, split.parts,
-                                                                    a.norms);
+        for (int64_t r = 0; r < a.rows; r += kMaxGrid) {
+            const int64_t n = a.rows - r < kMaxGrid ? a.rows - r : kMaxGrid;
+            segment_norm_kernel<<<(unsigned)n, kListBlock, 0, s>>>(a.partial + r * split.parts,
+                                                                   split.parts, a.norms + r);
+        }
     return hipGetLastError();
 }
 
-unsigned list_grid(int64_t n_chunks) { return n_chunks > 0 ? (unsigned)norm_groups(n_chunks) : 1u; }
+// Chunks at the end of a list that the last-level cache (256 MB) keeps from
+// one pass to the next: 192 MB of f32.
+constexpr int64_t kKeepChunks = (int64_t)192 * 1024 * 1024 / (4 * kChunk);
+// From here on the partial sums are joined by a launch of their own; below,
+// by every workgroup that scales a chunk.
+constexpr int64_t kJoinChunks = 8192;
+// Written f32 bytes up to which an update leaves its results in the cache.
+constexpr int64_t kKeepWritten = (int64_t)128 << 20;
+
+// Chunks of one launch that takes them all: its threads stay below 2^32.
+constexpr int64_t kLaunchChunks = int64_t(1) << 21;
+
+// Calls launch(first chunk, step, chunks) over a list: forwards, or the last
+// chunk first where the list is longer than what the cache keeps of it.
+template <typename F>
+hipError_t over_chunks(int64_t n_chunks, F &&launch) {
+    const bool backwards = n_chunks > kKeepChunks;
+    for (int64_t done = 0; done < n_chunks; done += kLaunchChunks) {
+        const int64_t n = n_chunks - done < kLaunchChunks ? n_chunks - done : kLaunchChunks;
+        launch(backwards ? n_chunks - 1 - done : done, backwards ? int64_t(-1) : int64_t(1),
+               (unsigned)n);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+template <typename Apply>
+hipError_t start_solo(const aspis_chunk *table, int64_t n_chunks, int32_t n_tensors,
+                      bool have_sumsq, const NormIn &in, float *each, const Apply &apply,
+                      hipStream_t s) {
+    solo_kernel<<<1, kSoloBlock, 0, s>>>(table, (int)n_chunks, table + n_chunks, n_tensors,
+                                         have_sumsq, in, each, apply);
+    return hipGetLastError();
+}
+
+// The norm pass and, when asked, its joining; afterwards in says where the
+// sum is.
+hipError_t start_sumsq(const aspis_chunk *table, int64_t n_chunks, double *ws, bool read_again,
+                       bool join, int32_t n_tensors, float *each, NormIn *in, hipStream_t s) {
+    const int groups = (int)(n_chunks < kNormGroups ? n_chunks : kNormGroups);
+    const int group = (int)(n_chunks / (4 * kNormGroups) < 1    ? 1
+                            : n_chunks / (4 * kNormGroups) > 16 ? 16
+                                                                : n_chunks / (4 * kNormGroups));
+    const int64_t keep = !read_again ? n_chunks : n_chunks > kKeepChunks ? n_chunks - kKeepChunks : 0;
+    double *runs = each != nullptr ? ws + kNormGroups : nullptr;
+    list_sumsq_kernel<<<groups, kListBlock, 0, s>>>(table, n_chunks, group, keep, ws, runs);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    in->partial = ws;
+    in->n_partial = groups;
+    if (!join) return hipSuccess;
+    list_norm_kernel<<<each != nullptr ? 1u + (unsigned)n_tensors : 1u, kListBlock, 0, s>>>(
+        table + n_chunks, group, *in, runs, each);
+    in->n_partial = 0;
+    return hipGetLastError();
+}
+
+template <typename Rule>
+hipError_t update_list(const UpdateTables &t, int64_t n_chunks, bool have_sumsq, double *ws,
+                       NormIn in, const Rule &rule, bool skip, hipStream_t s) {
+    if (n_chunks <= kSoloChunks)
+        return start_solo(t.grads, n_chunks, 0, have_sumsq, in, nullptr,
+                          Update<Rule>{t, rule, in.max_norm, skip}, s);
+    if (!have_sumsq) {
+        const hipError_t e = start_sumsq(t.grads, n_chunks, ws, true, true, 0, nullptr, &in, s);
+        if (e != hipSuccess) return e;
+    }
+    const bool again = n_chunks * kChunk * 4 * (1 + Rule::S) <= kKeepWritten;
+    return over_chunks(n_chunks, [&](int64_t first, int64_t step, unsigned n) {
+        const unsigned grid = n * kUpdateParts;
+        if (again)
+            update_kernel<Rule, Use::Again><<<grid, kUpdateBlock, 0, s>>>(t, first, step, in, rule,
+                                                                          skip);
+        else
+            update_kernel<Rule, Use::Once><<<grid, kUpdateBlock, 0, s>>>(t, first, step, in, rule,
+                                                                         skip);
+    });
+}
 
 }  // namespace
 
-hipError_t launch_list_sumsq(const aspis_chunk *table, int64_t n_chunks, double *partial,
-                             double *chunk_sums, hipStream_t s) {
-    list_sumsq_kernel<<<list_grid(n_chunks), kListBlock, 0, s>>>(table, n_chunks, partial,
-                                                                 chunk_sums);
-    return hipGetLastError();
+hipError_t launch_norm(const aspis_chunk *table, int64_t n_chunks, int32_t n_tensors, double *ws,
+                       NormIn in, float *each, hipStream_t s) {
+    if (n_chunks <= kSoloChunks)
+        return start_solo(table, n_chunks, n_tensors, false, in, each, NoApply{}, s);
+    return start_sumsq(table, n_chunks, ws, false, true, n_tensors, each, &in, s);
 }
 
-hipError_t launch_list_norm(const aspis_chunk *table, int64_t n_chunks, int32_t n_tensors,
-                            const NormIn &in, const double *chunk_sums, float *each,
-                            hipStream_t s) {
-    const int waves = kListBlock / 64;
-    const unsigned grid = 1u + (each != nullptr ? (unsigned)((n_tensors + waves - 1) / waves) : 0u);
-    list_norm_kernel<<<grid, kListBlock, 0, s>>>(table + n_chunks, n_tensors, in, chunk_sums,
-                                                 each);
-    return hipGetLastError();
-}
-
-hipError_t launch_list_scale(const aspis_chunk *table, const aspis_chunk *out, int64_t n_chunks,
-                             const NormIn &in, hipStream_t s) {
-    list_scale_kernel<<<list_grid(n_chunks), kListBlock, 0, s>>>(table, out, n_chunks, in);
-    return hipGetLastError();
+hipError_t launch_clip(const aspis_chunk *table, const aspis_chunk *out, int64_t n_chunks,
+                       bool have_sumsq, double *ws, NormIn in, hipStream_t s) {
+    if (n_chunks <= kSoloChunks)
+        return start_solo(table, n_chunks, 0, have_sumsq, in, nullptr,
+                          Scale{table, out, in.max_norm}, s);
+    if (!have_sumsq) {
+        const hipError_t e = start_sumsq(table, n_chunks, ws, true, n_chunks >= kJoinChunks, 0,
+                                         nullptr, &in, s);
+        if (e != hipSuccess) return e;
+    }
+    return over_chunks(n_chunks, [&](int64_t first, int64_t step, unsigned n) {
+        list_scale_kernel<<<n, kListBlock, 0, s>>>(table, out, first, step, in);
+    });
 }
 
 hipError_t launch_sgd(const aspis_chunk *params, const aspis_chunk *grads,
                       const aspis_chunk *mean, const aspis_chunk *copies, int64_t n_chunks,
-                      const NormIn &in, const SgdArgs &a, bool skip, hipStream_t s) {
+                      bool have_sumsq, double *ws, const NormIn &in, const SgdArgs &a, bool skip,
+                      hipStream_t s) {
     const UpdateTables t{params, grads, {mean, nullptr}, copies};
-    if (mean != nullptr)
-        update_kernel<<<list_grid(n_chunks), kListBlock, 0, s>>>(t, n_chunks, in, Sgd{a}, skip);
-    else
-        update_kernel<<<list_grid(n_chunks), kListBlock, 0, s>>>(t, n_chunks, in, PlainSgd{a},
-                                                                 skip);
-    return hipGetLastError();
+    if (mean != nullptr) return update_list(t, n_chunks, have_sumsq, ws, in, Sgd{a}, skip, s);
+    return update_list(t, n_chunks, have_sumsq, ws, in, PlainSgd{a}, skip, s);
 }
 
 hipError_t launch_adamw(const aspis_chunk *params, const aspis_chunk *grads,
                         const aspis_chunk *mean, const aspis_chunk *square,
-                        const aspis_chunk *copies, int64_t n_chunks, const NormIn &in,
-                        const AdamArgs &a, bool skip, hipStream_t s) {
-    const UpdateTables t{params, grads, {mean, square}, copies};
-    update_kernel<<<list_grid(n_chunks), kListBlock, 0, s>>>(t, n_chunks, in, AdamW{a}, skip);
-    return hipGetLastError();
+                        const aspis_chunk *copies, int64_t n_chunks, bool have_sumsq, double *ws,
+                        const NormIn &in, const AdamArgs &a, bool skip, hipStream_t s) {
+    return update_list(UpdateTables{params, grads, {mean, square}, copies}, n_chunks, have_sumsq,
+                       ws, in, AdamW{a}, skip, s);
 }
 
 hipError_t launch_rows(const RowArgs &a, hipStream_t s) {
