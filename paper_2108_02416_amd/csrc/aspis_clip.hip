@@ -120,30 +120,6 @@ __device__ __forceinline__ void store_vec(MutPtr<E> p, u32x4 v) {
     else *q = v;
 }
 
-// The vector at element i of n elements, zeros past the end.
-template <typename E, Use USE>
-__device__ __forceinline__ u32x4 load_part(Ptr<E> p, int i, int n) {
-    if (i + E::V <= n) return load_vec<E, USE>(p + i);
-    u32x4 w = {0, 0, 0, 0};
-    if (i < n) {
-        float x[E::V];
-#pragma unroll
-        for (int j = 0; j < E::V; ++j) x[j] = i + j < n ? E::get(p[i + j]) : 0.0f;
-        w = E::pack(x);
-    }
-    return w;
-}
-template <typename E, Use USE>
-__device__ __forceinline__ void store_part(MutPtr<E> p, int i, int n, const float (&x)[E::V]) {
-    if (i + E::V <= n) {
-        store_vec<E, USE>(p + i, E::pack(x));
-    } else if (i < n) {
-#pragma unroll
-        for (int j = 0; j < E::V; ++j)
-            if (i + j < n) p[i + j] = E::put(x[j]);
-    }
-}
-
 // Calls f with the element type of a dtype code (uniform over the workgroup).
 template <typename F>
 __device__ __forceinline__ void with_type(int dtype, F &&f) {
@@ -215,28 +191,68 @@ __device__ __forceinline__ void add_squares(u32x4 w, double (&acc)[2]) {
     for (int j = 0; j < E::V; ++j) acc[j & 1] = add_square(x[j], acc[j & 1]);
 }
 
-// A chunk in the registers of 256 threads: U vectors each, thread t holding
-// vectors t, t + 256, ...
-template <typename E>
-struct Tile {
-    static constexpr int U = kChunk / E::V / 256;
-    u32x4 w[U];
+// n elements in the registers of L lanes: vectors lane, lane + L, ..., R at
+// most, and of the n % V elements after the last whole vector, elements lane,
+// lane + L, ...; zeros past the end.
+template <typename E, int L, int R>
+struct Span {
+    static constexpr int V = E::V, Q = (V - 2 + L) / L;
+    u32x4 w[R];
+    float tail[Q];
 
     template <Use USE>
-    __device__ __forceinline__ void load(Ptr<E> p, int n, int t) {
-        if (n == kChunk) {
+    __device__ __forceinline__ void load(Ptr<E> p, int n, int lane) {
+        if (n == R * L * V) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) w[u] = load_vec<E, USE>(p + (t + u * 256) * E::V);
-        } else {
+            for (int r = 0; r < R; ++r) w[r] = load_vec<E, USE>(p + (lane + r * L) * V);
 #pragma unroll
-            for (int u = 0; u < U; ++u) w[u] = load_part<E, USE>(p, (t + u * 256) * E::V, n);
+            for (int q = 0; q < Q; ++q) tail[q] = 0.0f;
+            return;
+        }
+        const int nv = n / V;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            w[r] = (u32x4){0, 0, 0, 0};
+            if (lane + r * L < nv) w[r] = load_vec<E, USE>(p + (lane + r * L) * V);
+        }
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            const int i = nv * V + lane + q * L;
+            tail[q] = i < n ? E::get(p[i]) : 0.0f;
         }
     }
-    __device__ __forceinline__ void squares(double (&acc)[2]) const {
+    __device__ __forceinline__ double squares() const {
+        double acc[2] = {0.0, 0.0};
 #pragma unroll
-        for (int u = 0; u < U; ++u) add_squares<E>(w[u], acc);
+        for (int r = 0; r < R; ++r) add_squares<E>(w[r], acc);
+#pragma unroll
+        for (int q = 0; q < Q; ++q) acc[q & 1] = add_square(tail[q], acc[q & 1]);
+        return acc[0] + acc[1];
+    }
+    // Writes c times the elements; o may be where they came from.
+    template <Use USE, typename C>
+    __device__ __forceinline__ void store(MutPtr<E> o, int n, int lane, C c) const {
+        const int nv = n / V;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            if (n != R * L * V && lane + r * L >= nv) continue;
+            float x[V];
+            E::unpack(w[r], x);
+#pragma unroll
+            for (int j = 0; j < V; ++j) x[j] = c(x[j]);
+            store_vec<E, USE>(o + (lane + r * L) * V, E::pack(x));
+        }
+        if (n == R * L * V) return;
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            const int i = nv * V + lane + q * L;
+            if (i < n) o[i] = E::put(c(tail[q]));
+        }
     }
 };
+// A chunk in the registers of 256 threads.
+template <typename E>
+using Tile = Span<E, 256, kChunk / E::V / 256>;
 
 // ---------------------------------------------------------------------------
 // the coefficient
@@ -277,21 +293,6 @@ __device__ __forceinline__ double take_sumsq(const NormIn &in) {
     return s;
 }
 
-// Writes c * the tile; the output may be the input.
-template <typename E, Use USE>
-__device__ __forceinline__ void store_scaled(const Tile<E> &tile, MutPtr<E> o, int n, int t,
-                                             Coef c) {
-#pragma unroll
-    for (int u = 0; u < Tile<E>::U; ++u) {
-        float x[E::V];
-        E::unpack(tile.w[u], x);
-#pragma unroll
-        for (int j = 0; j < E::V; ++j) x[j] = c(x[j]);
-        if (n == kChunk) store_vec<E, USE>(o + (t + u * 256) * E::V, E::pack(x));
-        else store_part<E, USE>(o, (t + u * 256) * E::V, n, x);
-    }
-}
-
 // ---------------------------------------------------------------------------
 // lists of tensors
 
@@ -300,15 +301,17 @@ constexpr int kListBlock = 256;
 __device__ __forceinline__ int chunk_type(const aspis_chunk &c) { return c.info & 3; }
 __device__ __forceinline__ int chunk_tensor(const aspis_chunk &c) { return c.info >> 2; }
 
-// Adds the squares of a chunk, split over 256 threads.
+// The squares of a chunk, split over 256 threads.
 template <Use USE>
-__device__ __forceinline__ void chunk_squares(const aspis_chunk &c, int t, double (&acc)[2]) {
+__device__ __forceinline__ double chunk_squares(const aspis_chunk &c, int t) {
+    double s = 0.0;
     with_type(chunk_type(c), [&](auto e) {
         typedef decltype(e) E;
         Tile<E> tile;
         tile.template load<USE>((Ptr<E>)c.addr, c.n, t);
-        tile.squares(acc);
+        s = tile.squares();
     });
+    return s;
 }
 
 // The norm pass: a fixed number of workgroups over groups of `group` chunks
@@ -320,8 +323,7 @@ __device__ __forceinline__ void chunk_squares(const aspis_chunk &c, int t, doubl
 __global__ __launch_bounds__(kListBlock) void
 list_sumsq_kernel(const aspis_chunk *__restrict__ table, int64_t n_chunks, int group,
                   int64_t keep, double *partial, double *runs) {
-    double acc[2] = {0.0, 0.0};
-    double total = 0.0;
+    double acc = 0.0, total = 0.0;
     int64_t first = (int64_t)blockIdx.x * group, k = first;
     aspis_chunk next = table[k];
     while (k < n_chunks) {
@@ -329,16 +331,16 @@ list_sumsq_kernel(const aspis_chunk *__restrict__ table, int64_t n_chunks, int g
         const int64_t now = k, now_first = first;
         if (++k == first + group || k >= n_chunks) k = first += (int64_t)gridDim.x * group;
         next = table[k < n_chunks ? k : now];
-        if (now < keep) chunk_squares<Use::Once>(c, threadIdx.x, acc);
-        else chunk_squares<Use::Again>(c, threadIdx.x, acc);
+        acc += now < keep ? chunk_squares<Use::Once>(c, threadIdx.x)
+                          : chunk_squares<Use::Again>(c, threadIdx.x);
         if (runs != nullptr && (first != now_first || chunk_tensor(next) != chunk_tensor(c))) {
-            const double s = block_sum<kListBlock>(acc[0] + acc[1]);
+            const double s = block_sum<kListBlock>(acc);
             if (threadIdx.x == 0) runs[now_first / group + chunk_tensor(c)] = s;
             total += s;
-            acc[0] = acc[1] = 0.0;
+            acc = 0.0;
         }
     }
-    if (runs == nullptr) total = block_sum<kListBlock>(acc[0] + acc[1]);
+    if (runs == nullptr) total = block_sum<kListBlock>(acc);
     if (threadIdx.x == 0) partial[blockIdx.x] = total;
 }
 
@@ -380,7 +382,7 @@ list_scale_kernel(const aspis_chunk *__restrict__ table, const aspis_chunk *__re
             typedef decltype(e) E;
             Tile<E> tile;
             tile.template load<Use::Once>((Ptr<E>)c.addr, c.n, threadIdx.x);
-            store_scaled<E, Use::Once>(tile, (MutPtr<E>)to, c.n, threadIdx.x, coef);
+            tile.template store<Use::Once>((MutPtr<E>)to, c.n, threadIdx.x, coef);
         });
         return;
     }
@@ -389,7 +391,7 @@ list_scale_kernel(const aspis_chunk *__restrict__ table, const aspis_chunk *__re
         Tile<E> tile;
         tile.template load<Use::Once>((Ptr<E>)c.addr, c.n, threadIdx.x);
         const Coef coef = coefficient(take_sumsq<kListBlock>(in), in.max_norm);
-        store_scaled<E, Use::Once>(tile, (MutPtr<E>)to, c.n, threadIdx.x, coef);
+        tile.template store<Use::Once>((MutPtr<E>)to, c.n, threadIdx.x, coef);
     });
 }
 
@@ -569,7 +571,7 @@ struct Scale {
             typedef decltype(e) E;
             Tile<E> tile;
             tile.template load<Use::Again>((Ptr<E>)c.addr, c.n, t);
-            store_scaled<E, Use::Again>(tile, (MutPtr<E>)to, c.n, t, coef);
+            tile.template store<Use::Again>((MutPtr<E>)to, c.n, t, coef);
         });
     }
 };
@@ -604,9 +606,7 @@ solo_kernel(const aspis_chunk *__restrict__ table, int n_chunks, const aspis_chu
         total = *in.sumsq;
     } else {
         for (int k = group; k < n_chunks; k += kSoloBlock / 256) {
-            double acc[2] = {0.0, 0.0};
-            chunk_squares<Use::Again>(table[k], t, acc);
-            const double s = lanes_sum<64>(acc[0] + acc[1]);
+            const double s = lanes_sum<64>(chunk_squares<Use::Again>(table[k], t));
             if (t % 64 == 0) sums[k * 4 + t / 64] = s;
         }
         __syncthreads();
@@ -632,34 +632,21 @@ solo_kernel(const aspis_chunk *__restrict__ table, int n_chunks, const aspis_chu
 // written once.  L <= 64: B / L rows per workgroup; L == B: one.
 template <typename E, int L, int B, int R>
 __global__ __launch_bounds__(B) void row_kernel(RowArgs a) {
-    constexpr int V = E::V, G = B / L;
+    constexpr int G = B / L;
     const int lane = threadIdx.x % L;
     for (int64_t row0 = (int64_t)blockIdx.x * G; row0 < a.rows; row0 += (int64_t)gridDim.x * G) {
         const int64_t row = row0 + threadIdx.x / L;
         const int d = row < a.rows ? (int)a.d : 0;
-        const Ptr<E> p = (Ptr<E>)a.x + row * a.ld;
-        u32x4 w[R];
-#pragma unroll
-        for (int r = 0; r < R; ++r) w[r] = load_part<E, Use::Once>(p, (lane + r * L) * V, d);
-        double acc[2] = {0.0, 0.0};
-#pragma unroll
-        for (int r = 0; r < R; ++r) add_squares<E>(w[r], acc);
-        double s;
-        if constexpr (L == B) s = block_sum<B>(acc[0] + acc[1]);
-        else s = lanes_sum<L>(acc[0] + acc[1]);
+        Span<E, L, R> span;
+        span.template load<Use::Once>((Ptr<E>)a.x + row * a.ld, d, lane);
+        double s = span.squares();
+        if constexpr (L == B) s = block_sum<B>(s);
+        else s = lanes_sum<L>(s);
         if (d > 0 && lane == 0 && a.norms != nullptr) a.norms[row] = (float)sqrt(s);
         if (a.out == nullptr) continue;
         const Coef c = coefficient(s, a.max_norm);
         if (a.out == a.x && c.one()) continue;
-        const MutPtr<E> o = (MutPtr<E>)a.out + row * a.ldo;
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            float x[V];
-            E::unpack(w[r], x);
-#pragma unroll
-            for (int j = 0; j < V; ++j) x[j] = c(x[j]);
-            store_part<E, Use::Once>(o, (lane + r * L) * V, d, x);
-        }
+        span.template store<Use::Once>((MutPtr<E>)a.out + row * a.ldo, d, lane, c);
     }
 }
 
@@ -692,15 +679,15 @@ __global__ __launch_bounds__(kListBlock) void segment_kernel(SegArgs g) {
         int64_t at = part * g.seg;
         const int64_t end = at + g.seg < g.a.d ? at + g.seg : g.a.d;
         const Ptr<E> p = (Ptr<E>)g.a.x + row * g.a.ld;
-        double acc[2] = {0.0, 0.0};
+        double acc = 0.0;
         for (; at < end; at += kChunk) {
             Tile<E> tile;
             const int n = (int)(end - at < kChunk ? end - at : kChunk);
             if (g.a.out == nullptr) tile.template load<Use::Once>(p + at, n, threadIdx.x);
             else tile.template load<Use::Again>(p + at, n, threadIdx.x);
-            tile.squares(acc);
+            acc += tile.squares();
         }
-        const double s = block_sum<kListBlock>(acc[0] + acc[1]);
+        const double s = block_sum<kListBlock>(acc);
         if (threadIdx.x == 0) g.a.partial[row * g.parts + part] = s;
         return;
     }
@@ -714,7 +701,7 @@ __global__ __launch_bounds__(kListBlock) void segment_kernel(SegArgs g) {
     if (g.a.out == g.a.x && c.one()) return;
     Tile<E> tile;
     tile.template load<Use::Once>((Ptr<E>)g.a.x + row * g.a.ld + at, n, threadIdx.x);
-    store_scaled<E, Use::Once>(tile, (MutPtr<E>)g.a.out + row * g.a.ldo + at, n, threadIdx.x, c);
+    tile.template store<Use::Once>((MutPtr<E>)g.a.out + row * g.a.ldo + at, n, threadIdx.x, c);
 }
 
 // The norms alone of long rows, from their segments' sums.
