@@ -466,6 +466,8 @@ aspis_status aspis_grad_norm(const aspis_chunk *table, int64_t n_chunks,
                                          all ranks): no norm pass          */
 #define ASPIS_CLIP_SKIP_NONFINITE 2u  /* updates: leave everything as it is
                                          where the norm is not finite      */
+#define ASPIS_CLIP_NO_WAIT 4u         /* rows: no workgroup waits for another
+                                         inside a kernel                   */
 
 /* Clips a list of tensors by its global norm: out = c * x, rounded to the
  * type.  out_table NULL (or table itself) clips in place; otherwise it lists
@@ -490,11 +492,16 @@ aspis_status aspis_row_norms(const void *x, int64_t rows, int64_t d, int64_t ld,
 /* Clips every row by its own norm: out_i = c_i * x_i, rounded to the type.
  * out: rows of ldo >= d elements of the same type; x itself (with ldo = ld)
  * clips in place, anything else must not overlap x.  norms: device float
- * [rows], the norms before clipping, or NULL. */
+ * [rows], the norms before clipping, or NULL.
+ * A row too long for one workgroup's registers is held by several, which
+ * wait for each other's sums, each at most 0.1 ms; what did not fit the
+ * device together is read again.  ASPIS_CLIP_NO_WAIT leaves the waiting out
+ * (for calls that share the device with other long-running kernels).  The
+ * results are the same. */
 aspis_status aspis_clip_rows(const void *x, int64_t rows, int64_t d, int64_t ld,
                              aspis_dtype dtype, double max_norm, void *out,
-                             int64_t ldo, float *norms, void *workspace,
-                             size_t ws_bytes, void *stream);
+                             int64_t ldo, float *norms, uint32_t flags,
+                             void *workspace, size_t ws_bytes, void *stream);
 
 /* The model update with the clip applied as the gradient is read:
  * g = c * grad in f32 (c of the global norm of `grads`), then

@@ -28,6 +28,7 @@ FLAG_HALF_KEYS = 8
 FLAG_PROBE_PREFIX = 16
 CLIP_HAVE_SUMSQ = 1
 CLIP_SKIP_NONFINITE = 2
+CLIP_NO_WAIT = 4
 
 EXPORTED = (
     "aspis_num_files", "aspis_assign", "aspis_detect", "aspis_clique",
@@ -204,7 +205,7 @@ def lib():
     L.aspis_row_workspace.restype = size
     L.aspis_row_norms.argtypes = [P, i64, i64, i64, ctypes.c_int, P, P, size, P]
     L.aspis_row_norms.restype = ctypes.c_int
-    L.aspis_clip_rows.argtypes = [P, i64, i64, i64, ctypes.c_int, f64, P, i64, P, P, size, P]
+    L.aspis_clip_rows.argtypes = [P, i64, i64, i64, ctypes.c_int, f64, P, i64, P, u32, P, size, P]
     L.aspis_clip_rows.restype = ctypes.c_int
     L.aspis_clipped_sgd.argtypes = [P, P, P, P, i64, ctypes.POINTER(SgdOptions), P, P, P, size, P]
     L.aspis_clipped_sgd.restype = ctypes.c_int
@@ -791,11 +792,12 @@ def row_norms(x, norms=None, ws=None):
     return norms
 
 
-def clip_rows(x, max_norm: float, out=None, norms=None, ws=None):
+def clip_rows(x, max_norm: float, out=None, norms=None, ws=None, flags: int = 0):
     """Scales every row of x [..., d] whose norm is above max_norm down to it
     (aspis_clip_rows): in place, or into `out`.  Returns (out, the norms before
     clipping).  Replicas with equal bits are equal after it, so a server may
-    clip them before detection and workers before they upload."""
+    clip them before detection and workers before they upload.  flags may
+    hold CLIP_NO_WAIT."""
     rows, d, ld, code = _rows("x", x)
     out = x if out is None else out
     ldo = ld
@@ -806,7 +808,7 @@ def clip_rows(x, max_norm: float, out=None, norms=None, ws=None):
     norms, ws = _row_buffers(x, rows, d, code, norms, ws)
     with _on(x.device):
         _check(lib().aspis_clip_rows(x.data_ptr(), rows, d, ld, code, max_norm, out.data_ptr(),
-                                     ldo, norms.data_ptr(), ws.data_ptr(), ws.numel(),
+                                     ldo, norms.data_ptr(), flags, ws.data_ptr(), ws.numel(),
                                      _raw_stream(x.device)))
     return out, norms
 

@@ -62,14 +62,22 @@ hipError_t launch_adamw(const aspis_chunk *params, const aspis_chunk *grads,
                         const aspis_chunk *copies, int64_t n_chunks, bool have_sumsq, double *ws,
                         const NormIn &in, const AdamArgs &a, bool skip, hipStream_t s);
 
-// Rows.  A row of up to kRowVecs 16-byte vectors is held in one workgroup's
-// registers; a longer one is cut into segments.
-constexpr int kRowVecs = 8192;
-struct RowSplit {
-    int64_t seg;     // elements per segment (0: the row is not cut)
-    int32_t parts;   // segments per row
+// Rows.  How a row is summed depends on its length alone (parts of `length`
+// elements), so that its norm does; which kernel clips it also on how many
+// there are.
+constexpr int kRowVecs = 8192;   // 16-byte vectors of a row that one workgroup holds
+enum class RowKind {
+    Registers,   // in one workgroup's registers
+    Parts,       // in several workgroups' (vecs vectors a thread)
+    Segments     // read twice, the second time from the last-level cache
 };
-RowSplit row_split(int64_t d, int elem_bytes);
+struct RowPlan {
+    RowKind kind;
+    int32_t vecs;            // vectors of a part per thread
+    int32_t parts, length;   // of a row; elements of a part
+    int64_t scratch;         // doubles of workspace
+};
+RowPlan row_plan(int64_t rows, int64_t d, int elem_bytes);
 struct RowArgs {
     const void *x;
     void *out;       // nullptr: norms only
@@ -77,7 +85,8 @@ struct RowArgs {
     int64_t rows, d, ld, ldo;
     int dtype;
     double max_norm;
-    double *partial; // [rows][parts], long rows only
+    double *scratch; // row_plan's, 16-byte aligned
+    bool wait;       // workgroups may wait for one another
 };
 hipError_t launch_rows(const RowArgs &a, hipStream_t s);
 

@@ -11,6 +11,7 @@
 // atomics, so equal inputs give equal bits wherever they lie.
 #include "aspis_clip.h"
 
+#include <atomic>
 #include <cfloat>
 
 namespace aspis {
@@ -221,12 +222,17 @@ struct Span {
             tail[q] = i < n ? E::get(p[i]) : 0.0f;
         }
     }
-    __device__ __forceinline__ double squares() const {
-        double acc[2] = {0.0, 0.0};
+    // Adds the squares to two sums, vector after vector: spans one behind the
+    // other add up as one long span does.
+    __device__ __forceinline__ void squares(double (&acc)[2]) const {
 #pragma unroll
         for (int r = 0; r < R; ++r) add_squares<E>(w[r], acc);
 #pragma unroll
         for (int q = 0; q < Q; ++q) acc[q & 1] = add_square(tail[q], acc[q & 1]);
+    }
+    __device__ __forceinline__ double squares() const {
+        double acc[2] = {0.0, 0.0};
+        squares(acc);
         return acc[0] + acc[1];
     }
     // Writes c times the elements; o may be where they came from.
@@ -236,8 +242,12 @@ struct Span {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             if (n != R * L * V && lane + r * L >= nv) continue;
+            // unpacked anew: kept from squares() on, 16-bit elements would
+            // take twice the registers
+            u32x4 v = w[r];
+            if constexpr (V == 8) asm volatile("" : "+v"(v));
             float x[V];
-            E::unpack(w[r], x);
+            E::unpack(v, x);
 #pragma unroll
             for (int j = 0; j < V; ++j) x[j] = c(x[j]);
             store_vec<E, USE>(o + (lane + r * L) * V, E::pack(x));
@@ -656,15 +666,133 @@ __global__ __launch_bounds__(kListBlock) void empty_rows_kernel(float *norms, in
         norms[i] = 0.0f;
 }
 
-// Segments of long rows.  One launch sums the segments of rows
-// [sum0, sum0 + ...) and scales those of the rows before, whose sums are
-// there and which the last-level cache still holds; the two kinds of
-// workgroups are spread evenly over the launch.
+// A long row is cut into parts, each summed by 256 threads in the same order
+// whichever kernel does it, and its parts' sums are added in order: a row's
+// norm depends on its elements and length alone.
+//
+// part_kernel: a part stays in the registers of a workgroup, R vectors a
+// thread, which publishes its sum of squares, waits for the row's total and
+// writes its part, so the row crosses the memory bus once each way.
+//
+// A sum is published as one 64-bit word that is never kUnset (a NaN that
+// came from f32 or f16 has zeros in its low bits), so a reader needs no
+// other flag.  The last workgroup of a row to arrive joins the row's sums,
+// in order.  Whether a row's workgroups run together is up to the device:
+// the wait for the total is bounded, and a workgroup that gives up lists its
+// part for redo_kernel, which reads it again.  The bound changes the time
+// alone, never a result.
+constexpr uint64_t kUnset = ~uint64_t(0);
+constexpr int kLine = 16;            // 8-byte words of a 128-byte line
+constexpr int kPartBlock = 256;
+constexpr int64_t kPatience = 10000; // ticks of 10 ns
+
+struct PartArgs {
+    RowArgs a;
+    int32_t parts, length;      // of a row; elements of a part, the last one's fewer
+    int64_t patience;
+    uint64_t *sums, *totals;    // [rows][parts], [rows] lines; kUnset at the start
+    uint32_t *arrived;          // [rows] lines, 0 at the start
+    uint32_t *left;             // [0]: the number of parts given up; from [1] on: which
+};
+
+__global__ __launch_bounds__(kListBlock) void part_init_kernel(PartArgs g) {
+    const int64_t step = (int64_t)gridDim.x * kListBlock;
+    for (int64_t i = blockIdx.x * (int64_t)kListBlock + threadIdx.x; i < g.a.rows * g.parts;
+         i += step) {
+        g.sums[i] = kUnset;
+        if (i < g.a.rows) {
+            g.totals[i * kLine] = kUnset;
+            g.arrived[i * 2 * kLine] = 0;
+        }
+        if (i == 0) *g.left = 0;
+    }
+}
+
+__device__ __forceinline__ void publish(uint64_t *at, double v) {
+    __hip_atomic_store(at, __builtin_bit_cast(uint64_t, v), __ATOMIC_RELAXED,
+                       __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ uint64_t peek(const uint64_t *at) {
+    return __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+template <typename E, int R, int WAVES>
+__global__ __launch_bounds__(kPartBlock, WAVES) void part_kernel(PartArgs g) {
+    __shared__ bool last;
+    __shared__ uint64_t got;
+    const int64_t row = blockIdx.x / (uint32_t)g.parts;
+    const int part = (int)(blockIdx.x % (uint32_t)g.parts);
+    const int64_t at = (int64_t)part * g.length;
+    const int n = (int)(g.a.d - at < g.length ? g.a.d - at : g.length);
+    Span<E, kPartBlock, R> span;
+    span.template load<Use::Once>((Ptr<E>)g.a.x + row * g.a.ld + at, n, threadIdx.x);
+    const double s = block_sum<kPartBlock>(span.squares());
+    uint64_t *sums = g.sums + row * g.parts, *its_total = g.totals + row * kLine;
+    if (threadIdx.x == 0) {
+        publish(sums + part, s);
+        last = atomicAdd(g.arrived + row * 2 * kLine, 1u) == (uint32_t)g.parts - 1;
+    }
+    __syncthreads();
+    double total;
+    if (last) {   // every sum of the row has been published: no long wait
+        double v = 0.0;
+        for (int i = threadIdx.x; i < g.parts; i += kPartBlock) {
+            uint64_t w;
+            do w = peek(sums + i);
+            while (w == kUnset);
+            v += __builtin_bit_cast(double, w);
+        }
+        total = block_sum<kPartBlock>(v);
+        if (threadIdx.x == 0) {
+            publish(its_total, total);
+            if (g.a.norms != nullptr) g.a.norms[row] = (float)sqrt(total);
+        }
+    } else {
+        if (threadIdx.x == 0) {
+            const int64_t start = wall_clock64();
+            uint64_t w = peek(its_total);
+            while (w == kUnset && (int64_t)wall_clock64() - start < g.patience) {
+                __builtin_amdgcn_s_sleep(1);
+                w = peek(its_total);
+            }
+            if (w == kUnset) g.left[1 + atomicAdd(g.left, 1u)] = blockIdx.x;
+            got = w;
+        }
+        __syncthreads();
+        if (got == kUnset) return;
+        total = __builtin_bit_cast(double, got);
+    }
+    const Coef c = coefficient(total, g.a.max_norm);
+    if (g.a.out == g.a.x && c.one()) return;
+    span.template store<Use::Once>((MutPtr<E>)g.a.out + row * g.a.ldo + at, n, threadIdx.x, c);
+}
+
+// The parts that were given up; their rows' totals are all there now.
+template <typename E, int R>
+__global__ __launch_bounds__(kPartBlock) void redo_kernel(PartArgs g) {
+    const uint32_t n_left = *g.left;
+    for (uint32_t i = blockIdx.x; i < n_left; i += gridDim.x) {
+        const uint32_t item = g.left[1 + i];
+        const int64_t row = item / (uint32_t)g.parts;
+        const int64_t at = (int64_t)(item % (uint32_t)g.parts) * g.length;
+        const int n = (int)(g.a.d - at < g.length ? g.a.d - at : g.length);
+        const Coef c =
+            coefficient(__builtin_bit_cast(double, g.totals[row * kLine]), g.a.max_norm);
+        if (g.a.out == g.a.x && c.one()) continue;
+        Span<E, kPartBlock, R> span;
+        span.template load<Use::Once>((Ptr<E>)g.a.x + row * g.a.ld + at, n, threadIdx.x);
+        span.template store<Use::Once>((MutPtr<E>)g.a.out + row * g.a.ldo + at, n, threadIdx.x, c);
+    }
+}
+
+// Rows longer than the registers hold, and few short ones (two launches):
+// one launch sums the parts of rows [sum0, sum0 + ...) and scales those of the
+// rows before, whose sums are there and which the last-level cache still
+// holds; the two kinds of workgroups are spread evenly over the launch.
 struct SegArgs {
     RowArgs a;
-    int64_t seg;
-    int32_t parts;    // segments of a row, summed by a workgroup each
-    int32_t tiles;    // chunks of a row, scaled by a workgroup each
+    int32_t parts, length;    // of a row, summed by a workgroup each
+    int32_t tiles;            // chunks of a row, scaled by a workgroup each
     int64_t scale0, sum0;
     int64_t n_scale, n_sum;   // workgroups of each kind
 };
@@ -676,26 +804,26 @@ __global__ __launch_bounds__(kListBlock) void segment_kernel(SegArgs g) {
     if ((b + 1) * g.n_sum / all > before) {
         const int64_t row = g.sum0 + before / g.parts;
         const int part = (int)(before % g.parts);
-        int64_t at = part * g.seg;
-        const int64_t end = at + g.seg < g.a.d ? at + g.seg : g.a.d;
+        int64_t at = (int64_t)part * g.length;
+        const int64_t end = at + g.length < g.a.d ? at + g.length : g.a.d;
         const Ptr<E> p = (Ptr<E>)g.a.x + row * g.a.ld;
-        double acc = 0.0;
+        double acc[2] = {0.0, 0.0};
         for (; at < end; at += kChunk) {
             Tile<E> tile;
             const int n = (int)(end - at < kChunk ? end - at : kChunk);
             if (g.a.out == nullptr) tile.template load<Use::Once>(p + at, n, threadIdx.x);
             else tile.template load<Use::Again>(p + at, n, threadIdx.x);
-            acc += tile.squares();
+            tile.squares(acc);
         }
-        const double s = block_sum<kListBlock>(acc);
-        if (threadIdx.x == 0) g.a.partial[row * g.parts + part] = s;
+        const double s = block_sum<kListBlock>(acc[0] + acc[1]);
+        if (threadIdx.x == 0) g.a.scratch[row * g.parts + part] = s;
         return;
     }
     const int64_t item = b - before;
     const int64_t row = g.scale0 + item / g.tiles;
     const int64_t at = item % g.tiles * kChunk;
     const int n = (int)(g.a.d - at < kChunk ? g.a.d - at : kChunk);
-    const double s = block_sum_of<kListBlock>(g.a.partial + row * g.parts, g.parts);
+    const double s = block_sum_of<kListBlock>(g.a.scratch + row * g.parts, g.parts);
     if (at == 0 && threadIdx.x == 0 && g.a.norms != nullptr) g.a.norms[row] = (float)sqrt(s);
     const Coef c = coefficient(s, g.a.max_norm);
     if (g.a.out == g.a.x && c.one()) return;
@@ -712,7 +840,9 @@ __global__ __launch_bounds__(kListBlock) void segment_norm_kernel(const double *
 }
 
 constexpr int64_t kMaxGrid = int64_t(1) << 23;   // workgroups of one launch
-constexpr int64_t kRowGroupBytes = 64 << 20;
+// Bytes of rows per launch of segment_kernel: what the last-level cache
+// holds until the next launch scales it, next to what that one reads.
+constexpr int64_t kGroupBytes = 64 << 20;
 
 template <typename E, int L, int B, int R>
 void start_rows(const RowArgs &a, hipStream_t s) {
@@ -721,32 +851,60 @@ void start_rows(const RowArgs &a, hipStream_t s) {
     row_kernel<E, L, B, R><<<(unsigned)(blocks < cap ? blocks : cap), B, 0, s>>>(a);
 }
 
-template <typename E>
-hipError_t rows_of(const RowArgs &a, hipStream_t s) {
-    const int64_t nv = (a.d + E::V - 1) / E::V;
-    if (nv <= kRowVecs) {
-        if (nv <= 4) start_rows<E, 4, 256, 1>(a, s);
-        else if (nv <= 16) start_rows<E, 16, 256, 1>(a, s);
-        else if (nv <= 64) start_rows<E, 64, 256, 1>(a, s);
-        else if (nv <= 128) start_rows<E, 64, 256, 2>(a, s);
-        else if (nv <= 256) start_rows<E, 64, 256, 4>(a, s);
-        else if (nv <= 512) start_rows<E, 256, 256, 2>(a, s);
-        else if (nv <= 1024) start_rows<E, 256, 256, 4>(a, s);
-        else if (nv <= 2048) start_rows<E, 256, 256, 8>(a, s);
-        else if (nv <= 4096) start_rows<E, 1024, 1024, 4>(a, s);
-        else start_rows<E, 1024, 1024, 8>(a, s);
-        return hipGetLastError();
+// Workgroups of part_kernel<.., 24, 4> the device runs at once: four a
+// compute unit.  Looked up once per device (relaxed atomics: concurrent
+// first calls store the same value).
+int parts_at_once() {
+    static std::atomic<int> known[64];
+    int dev = 0, cus = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return 0;
+    cus = known[dev].load(std::memory_order_relaxed);
+    if (cus == 0) {
+        if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess)
+            return 0;
+        known[dev].store(cus, std::memory_order_relaxed);
     }
-    const RowSplit split = row_split(a.d, (int)sizeof(typename E::T));
+    return 4 * cus;
+}
+
+template <typename E, int R, int WAVES>
+hipError_t start_parts(const RowArgs &a, const RowPlan &plan, hipStream_t s) {
+    PartArgs g{};
+    g.parts = plan.parts;
+    g.length = plan.length;
+    // a row takes three quarters of the device at most: with less to run on,
+    // waiting for its other parts would be in vain
+    g.patience = a.wait && 4 * (int64_t)plan.parts <= 3 * (int64_t)parts_at_once() ? kPatience : 0;
+    const int64_t step = kMaxGrid / plan.parts;   // rows a launch
+    for (int64_t r = 0; r < a.rows; r += step) {
+        g.a = a;
+        g.a.rows = a.rows - r < step ? a.rows - r : step;
+        g.a.x = (const char *)a.x + r * a.ld * (int64_t)sizeof(typename E::T);
+        g.a.out = (char *)a.out + r * a.ldo * (int64_t)sizeof(typename E::T);
+        g.a.norms = a.norms != nullptr ? a.norms + r : nullptr;
+        g.totals = (uint64_t *)a.scratch;
+        g.arrived = (uint32_t *)(g.totals + g.a.rows * kLine);
+        g.sums = (uint64_t *)(g.arrived + g.a.rows * 2 * kLine);
+        g.left = (uint32_t *)(g.sums + g.a.rows * g.parts);
+        part_init_kernel<<<64, kListBlock, 0, s>>>(g);
+        const unsigned items = (unsigned)(g.a.rows * g.parts);
+        part_kernel<E, R, WAVES><<<items, kPartBlock, 0, s>>>(g);
+        redo_kernel<E, R><<<items < 512 ? items : 512, kPartBlock, 0, s>>>(g);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+template <typename E>
+hipError_t start_segments(const RowArgs &a, const RowPlan &plan, hipStream_t s) {
     SegArgs g{};
     g.a = a;
-    g.seg = split.seg;
-    g.parts = split.parts;
+    g.parts = plan.parts;
+    g.length = plan.length;
     g.tiles = (int32_t)chunks_of(a.d);
-    // rows per launch: what stays in the last-level cache until the next
-    // launch scales it
     const int64_t bytes = a.d * (int64_t)sizeof(typename E::T);
-    int64_t step = a.out != nullptr ? kRowGroupBytes / bytes : kMaxGrid / split.parts;
+    int64_t step = a.out != nullptr ? kGroupBytes / bytes : kMaxGrid / plan.parts;
     const int64_t most = kMaxGrid / ((int64_t)g.tiles + g.parts);
     if (step > most) step = most;
     if (step < 1) step = 1;
@@ -766,9 +924,29 @@ hipError_t rows_of(const RowArgs &a, hipStream_t s) {
     if (a.out == nullptr)
         for (int64_t r = 0; r < a.rows; r += kMaxGrid) {
             const int64_t n = a.rows - r < kMaxGrid ? a.rows - r : kMaxGrid;
-            segment_norm_kernel<<<(unsigned)n, kListBlock, 0, s>>>(a.partial + r * split.parts,
-                                                                   split.parts, a.norms + r);
+            segment_norm_kernel<<<(unsigned)n, kListBlock, 0, s>>>(a.scratch + r * plan.parts,
+                                                                   plan.parts, a.norms + r);
         }
+    return hipGetLastError();
+}
+
+template <typename E>
+hipError_t rows_of(const RowArgs &a, hipStream_t s) {
+    const RowPlan plan = row_plan(a.rows, a.d, (int)sizeof(typename E::T));
+    if (plan.kind == RowKind::Parts && a.out != nullptr)
+        return plan.vecs == 8 ? start_parts<E, 8, 6>(a, plan, s) : start_parts<E, 24, 4>(a, plan, s);
+    if (plan.kind != RowKind::Registers) return start_segments<E>(a, plan, s);
+    const int64_t nv = (a.d + E::V - 1) / E::V;
+    if (nv <= 4) start_rows<E, 4, 256, 1>(a, s);
+    else if (nv <= 16) start_rows<E, 16, 256, 1>(a, s);
+    else if (nv <= 64) start_rows<E, 64, 256, 1>(a, s);
+    else if (nv <= 128) start_rows<E, 64, 256, 2>(a, s);
+    else if (nv <= 256) start_rows<E, 64, 256, 4>(a, s);
+    else if (nv <= 512) start_rows<E, 256, 256, 2>(a, s);
+    else if (nv <= 1024) start_rows<E, 256, 256, 4>(a, s);
+    else if (nv <= 2048) start_rows<E, 256, 256, 8>(a, s);
+    else if (nv <= 4096) start_rows<E, 1024, 1024, 4>(a, s);
+    else start_rows<E, 1024, 1024, 8>(a, s);
     return hipGetLastError();
 }
 

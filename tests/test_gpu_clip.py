@@ -308,7 +308,8 @@ def test_clip_rows_counts(rows, d):
 
 
 @pytest.mark.parametrize("kind,rows,d", [("float32", 23, 1_500_001), ("float32", 9, 17_000_003),
-                                         ("bfloat16", 70, 800_003), ("float16", 1, 20_000_001)])
+                                         ("float32", 5, 25_000_003), ("bfloat16", 70, 800_003),
+                                         ("float16", 1, 20_000_001)])
 @pytest.mark.parametrize("where", ["out", "in_place"])
 def test_clip_long_rows_over_several_launches(kind, rows, d, where):
     x = _randn(rows * d, kind, seed=rows).reshape(rows, d)
@@ -319,6 +320,31 @@ def test_clip_long_rows_over_several_launches(kind, rows, d, where):
     for i in range(rows):
         _check_rows(before[i:i + 1], bound, got[i:i + 1], norms[i:i + 1], kind)
     assert bool((aspis.row_norms(before) == norms).all())
+
+
+@pytest.mark.parametrize("kind", ["float32", "bfloat16"])
+@pytest.mark.parametrize("rows,d", [(1, 40_001), (40, 140_003), (200, 70_007), (9, 1_300_003),
+                                    (3, 9_000_001)])
+def test_long_rows_have_the_same_bits_by_every_way(rows, d, kind):
+    """Alone or among others (few rows take two passes over the cache, more
+    stay in registers), with and without workgroups waiting for one another,
+    in place or not, at any alignment."""
+    import torch
+    x = _randn(rows * d, kind, seed=d).reshape(rows, d)
+    x[::2].mul_(3.0)
+    bound = 0.015 * math.sqrt(d)
+    out, norms = aspis.clip_rows(x, bound, out=torch.empty_like(x))
+    _check_rows(x, bound, out, norms, kind)
+    again, same = aspis.clip_rows(x, bound, out=torch.empty_like(x), flags=aspis.CLIP_NO_WAIT)
+    assert np.array_equal(_bits(again), _bits(out)) and bool((norms == same).all())
+    assert bool((aspis.row_norms(x) == norms).all())
+    for i in {0, rows // 2, rows - 1}:
+        one, norm = aspis.clip_rows(x[i], bound, out=torch.empty_like(x[i]))
+        assert np.array_equal(_bits(one), _bits(out[i])) and float(norm) == float(norms[i])
+    wide = torch.empty((rows, d + 3), dtype=x.dtype, device=x.device)[:, 1:d + 1]
+    wide.copy_(x)
+    aspis.clip_rows(wide, bound, flags=aspis.CLIP_NO_WAIT)
+    assert np.array_equal(_bits(wide), _bits(out))
 
 
 @pytest.mark.parametrize("d", [3, 300, 5_000, 70_000])
@@ -641,4 +667,5 @@ def test_refusals():
     refused(bad, lambda: aspis.clip_rows(x, 1.0, out=torch.ones(6, 9, device=dev)))
     refused(bad, lambda: aspis.clip_rows(x, 1.0, out=x.half()))
     refused(bad, lambda: aspis.row_norms(x, norms=torch.ones(5, device=dev)))
+    refused(bad, lambda: aspis.clip_rows(x, 1.0, flags=8))
     assert bool((x == 1).all())
