@@ -8,7 +8,6 @@ the library -- there is no fallback.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
 from dataclasses import dataclass
@@ -501,9 +500,14 @@ def read_probe(buf, sink=None) -> float:
 
 # ------------------------------------- norms, clipping and the model update
 
+_dtype_codes: dict = {}
+
+
 def _dtype_code(dtype) -> int:
-    torch = _torch()
-    code = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}.get(dtype)
+    if not _dtype_codes:
+        torch = _torch()
+        _dtype_codes.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
+    code = _dtype_codes.get(dtype)
     if code is None:
         raise AspisError(ERR_INVALID_ARG, f"unsupported type {dtype}: float32, bfloat16 or float16")
     return code
@@ -530,12 +534,15 @@ def _raw_stream(device) -> int:
     return _torch()._C._cuda_getCurrentRawStream(device.index)
 
 
-def _on(device):
-    """Makes `device` current for a launch, where it is not."""
+def _launch(device, call, *args):
+    """Calls a library function that enqueues work on `device`, and checks
+    its status."""
     torch = _torch()
-    if device.index is None or device.index == torch.cuda.current_device():
-        return contextlib.nullcontext()
-    return torch.cuda.device(device)
+    if device.index == torch.cuda.current_device():
+        _check(call(*args))
+    else:
+        with torch.cuda.device(device):
+            _check(call(*args))
 
 
 class TensorList:
@@ -696,11 +703,10 @@ def grad_norm(grads, each: bool = False, bufs: NormBuffers | None = None, ws=Non
     grads = _list(grads)
     table = grads.table()
     bufs, ws, sumsq, _ = _norm_buffers(grads, bufs, ws, None, len(grads) if each else 0)
-    with _on(grads.device):
-        _check(lib().aspis_grad_norm(table, grads.n_chunks, len(grads), sumsq.data_ptr(),
-                                     bufs.norm.data_ptr(),
-                                     bufs.each.data_ptr() if each and len(grads) else None,
-                                     ws.data_ptr(), ws.numel(), _raw_stream(grads.device)))
+    _launch(grads.device, lib().aspis_grad_norm, table, grads.n_chunks, len(grads),
+            sumsq.data_ptr(), bufs.norm.data_ptr(),
+            bufs.each.data_ptr() if each and len(grads) else None, ws.data_ptr(), ws.numel(),
+            _raw_stream(grads.device))
     return bufs
 
 
@@ -721,10 +727,9 @@ def clip_grads(grads, max_norm: float, out=None, sumsq=None, bufs: NormBuffers |
         out_table = out.table()
         _check_match("out", out, grads, same_types=True)
         _check_written("out", out)
-    with _on(grads.device):
-        _check(lib().aspis_clip_grads(table, out_table, grads.n_chunks, max_norm, total.data_ptr(),
-                                      bufs.norm.data_ptr(), flags, ws.data_ptr(), ws.numel(),
-                                      _raw_stream(grads.device)))
+    _launch(grads.device, lib().aspis_clip_grads, table, out_table, grads.n_chunks, max_norm,
+            total.data_ptr(), bufs.norm.data_ptr(), flags, ws.data_ptr(), ws.numel(),
+            _raw_stream(grads.device))
     return bufs
 
 
@@ -735,6 +740,8 @@ def _rows(name: str, x):
         raise AspisError(ERR_INVALID_ARG, f"{name} must be a cuda tensor of rows [..., d]")
     code = _dtype_code(x.dtype)
     d = x.shape[-1]
+    if d and x.is_contiguous():
+        return x.numel() // d, d, d, code
     rows = 1
     for n in x.shape[:-1]:
         rows *= n
@@ -773,11 +780,11 @@ def _row_buffers(x, rows: int, d: int, code: int, norms, ws):
         norms = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
     else:
         _check_buffer("norms", norms, torch.float32, rows, x.device)
-    need = int(lib().aspis_row_workspace(rows, d, code))
     if ws is None:
-        ws = torch.empty(need, dtype=torch.uint8, device=x.device)
-    else:
-        _check_buffer("ws", ws, torch.uint8, need, x.device)
+        ws = torch.empty(int(lib().aspis_row_workspace(rows, d, code)), dtype=torch.uint8,
+                         device=x.device)
+    else:   # its size is the library's to check
+        _check_buffer("ws", ws, torch.uint8, 0, x.device)
     return norms, ws
 
 
@@ -786,9 +793,8 @@ def row_norms(x, norms=None, ws=None):
     [f][r][d] or a worker's upload [l][d]."""
     rows, d, ld, code = _rows("x", x)
     norms, ws = _row_buffers(x, rows, d, code, norms, ws)
-    with _on(x.device):
-        _check(lib().aspis_row_norms(x.data_ptr(), rows, d, ld, code, norms.data_ptr(),
-                                     ws.data_ptr(), ws.numel(), _raw_stream(x.device)))
+    _launch(x.device, lib().aspis_row_norms, x.data_ptr(), rows, d, ld, code, norms.data_ptr(),
+            ws.data_ptr(), ws.numel(), _raw_stream(x.device))
     return norms
 
 
@@ -806,10 +812,9 @@ def clip_rows(x, max_norm: float, out=None, norms=None, ws=None, flags: int = 0)
         if out.shape != x.shape or out_code != code or out.device != x.device:
             raise AspisError(ERR_INVALID_ARG, "out must have the shape, type and device of x")
     norms, ws = _row_buffers(x, rows, d, code, norms, ws)
-    with _on(x.device):
-        _check(lib().aspis_clip_rows(x.data_ptr(), rows, d, ld, code, max_norm, out.data_ptr(),
-                                     ldo, norms.data_ptr(), flags, ws.data_ptr(), ws.numel(),
-                                     _raw_stream(x.device)))
+    _launch(x.device, lib().aspis_clip_rows, x.data_ptr(), rows, d, ld, code, max_norm,
+            out.data_ptr(), ldo, norms.data_ptr(), flags, ws.data_ptr(), ws.numel(),
+            _raw_stream(x.device))
     return out, norms
 
 
@@ -848,11 +853,10 @@ def clipped_sgd(params, grads, mean=None, *, lr: float, momentum: float = 0.0,
     bufs, ws, total, flags = _norm_buffers(grads, bufs, ws, sumsq)
     opt = SgdOptions(lr, momentum, weight_decay, max_norm, int(nesterov),
                      flags | (CLIP_SKIP_NONFINITE if skip_nonfinite else 0))
-    with _on(grads.device):
-        _check(lib().aspis_clipped_sgd(tables[1], tables[0], tables[2] if mean is not None else None,
-                                       tables[-1] if copies is not None else None, grads.n_chunks,
-                                       ctypes.byref(opt), total.data_ptr(), bufs.norm.data_ptr(),
-                                       ws.data_ptr(), ws.numel(), _raw_stream(grads.device)))
+    _launch(grads.device, lib().aspis_clipped_sgd, tables[1], tables[0],
+            tables[2] if mean is not None else None, tables[-1] if copies is not None else None,
+            grads.n_chunks, ctypes.byref(opt), total.data_ptr(), bufs.norm.data_ptr(),
+            ws.data_ptr(), ws.numel(), _raw_stream(grads.device))
     del lists   # their tables were needed until here
     return bufs
 
@@ -869,11 +873,9 @@ def clipped_adamw(params, grads, mean, square, *, step: int, lr: float, betas=(0
     bufs, ws, total, flags = _norm_buffers(grads, bufs, ws, sumsq)
     opt = AdamwOptions(lr, betas[0], betas[1], eps, weight_decay, max_norm, step,
                        flags | (CLIP_SKIP_NONFINITE if skip_nonfinite else 0), 0)
-    with _on(grads.device):
-        _check(lib().aspis_clipped_adamw(tables[1], tables[0], tables[2], tables[3],
-                                         tables[4] if copies is not None else None,
-                                         grads.n_chunks, ctypes.byref(opt), total.data_ptr(),
-                                         bufs.norm.data_ptr(), ws.data_ptr(), ws.numel(),
-                                         _raw_stream(grads.device)))
+    _launch(grads.device, lib().aspis_clipped_adamw, tables[1], tables[0], tables[2], tables[3],
+            tables[4] if copies is not None else None, grads.n_chunks, ctypes.byref(opt),
+            total.data_ptr(), bufs.norm.data_ptr(), ws.data_ptr(), ws.numel(),
+            _raw_stream(grads.device))
     del lists   # their tables were needed until here
     return bufs
