@@ -580,38 +580,41 @@ class TensorList:
         ts = self.tensors
         n = len(ts)
         self._where = self._now()
-        self.numels = [t.numel() for t in ts]
+        where, self.numels = self._where
         self.dtypes = [t.dtype for t in ts]
         codes = np.array([_dtype_code(d) for d in self.dtypes], dtype=np.int32)
-        self.layouts = [_layout(t) for t in ts]
+        self.contiguous = True
         for i, t in enumerate(ts):
-            if self.layouts[i] is None:
-                raise AspisError(ERR_INVALID_ARG, f"tensor {i} of the list has gaps or overlaps in "
-                                                  f"memory: shape {tuple(t.shape)}, strides "
-                                                  f"{t.stride()}")
+            if not t.is_contiguous():
+                self.contiguous = False
+                if _layout(t) is None:
+                    raise AspisError(ERR_INVALID_ARG,
+                                     f"tensor {i} of the list has gaps or overlaps in memory: "
+                                     f"shape {tuple(t.shape)}, strides {t.stride()}")
             if t.device != self.device:
                 raise AspisError(ERR_INVALID_ARG, f"tensor {i} of the list is on {t.device}, the "
                                                   f"list on {self.device}")
-        self.contiguous = all(t.is_contiguous() for t in ts)
-        spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size())
-                       for t in ts if t.numel() > 0)
+        spans = sorted((p, p + k * t.element_size()) for p, k, t in zip(where, self.numels, ts) if k)
         self.disjoint = all(a[1] <= b[0] for a, b in zip(spans, spans[1:]))
-        ptrs = np.array([t.data_ptr() for t in ts], dtype=np.uint64)
+        ptrs = np.array(where, dtype=np.uint64)
         numels = np.array(self.numels, dtype=np.int64)
         self.n_chunks = int(lib().aspis_tensor_chunks(numels.ctypes.data, n))
         entries = int(lib().aspis_tensor_entries(numels.ctypes.data, n))
         if entries < 0:
             raise AspisError(ERR_OVERFLOW, "too many elements in the list")
-        host = np.zeros((max(entries, 1), 2), dtype=np.uint64)
+        host = np.empty((max(entries, 1), 2), dtype=np.int64)
         _check(lib().aspis_tensor_table(ptrs.ctypes.data, numels.ctypes.data, codes.ctypes.data, n,
                                         host.ctypes.data, entries))
         # a copy from pageable memory returns when it is done: the table is
         # there for any stream
-        self._table = torch.from_numpy(host.view(np.int64)).to(self.device)
+        self._table = torch.from_numpy(host).to(self.device)
         self._address = self._table.data_ptr()
         self._stream = _raw_stream(self.device)
         self.all_float32 = all(d == torch.float32 for d in self.dtypes)
         self.ws_bytes = int(lib().aspis_norm_workspace(self.n_chunks))
+
+    def layouts(self):
+        return [_layout(t) for t in self.tensors]
 
     def _now(self):
         Tensor = _torch().Tensor
@@ -636,7 +639,7 @@ def _check_match(name: str, a: TensorList, ref: TensorList, same_types: bool = F
     if a.numels != ref.numels or a.device != ref.device:
         raise AspisError(ERR_INVALID_ARG, f"{name} must list tensors of the gradients' sizes, in "
                                           f"their order, on their device")
-    if not (a.contiguous and ref.contiguous) and a.layouts != ref.layouts:
+    if not (a.contiguous and ref.contiguous) and a.layouts() != ref.layouts():
         raise AspisError(ERR_INVALID_ARG, f"{name}: tensors that are not contiguous must have the "
                                           f"gradients' shapes and strides")
     if same_types and a.dtypes != ref.dtypes:
