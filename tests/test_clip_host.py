@@ -1,0 +1,180 @@
+"""Host side of the norm, clipping and update entry points, without a GPU:
+tensor tables, workspace sizes and every refusal of the C ABI (all of them
+come before anything is enqueued); and the host code under sanitizers."""
+import ctypes
+import math
+import os
+import shutil
+import subprocess
+
+import numpy as np
+import pytest
+
+from paper_2108_02416_amd import aspis
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+ROCM = "/opt/rocm"
+SIZE = {0: 4, 1: 2, 2: 2}
+
+
+def _table(numels, dtypes, base=1 << 40):
+    """The table of tensors laid one after another from an invented address."""
+    L = aspis.lib()
+    n = len(numels)
+    numel = np.array(numels, dtype=np.int64)
+    dtype = np.array(dtypes, dtype=np.int32)
+    ptr, at = np.zeros(n, dtype=np.uint64), base
+    for i in range(n):
+        at += -at % SIZE[dtypes[i]]
+        ptr[i] = at
+        at += numels[i] * SIZE[dtypes[i]]
+    entries = L.aspis_tensor_entries(numel.ctypes.data, n)
+    out = np.zeros((entries, 2), dtype=np.uint64)
+    st = L.aspis_tensor_table(ptr.ctypes.data, numel.ctypes.data, dtype.ctypes.data, n,
+                              out.ctypes.data, entries)
+    assert st == aspis.OK
+    chunks = [aspis.Chunk.from_buffer_copy(out[i].tobytes()) for i in range(entries)]
+    return ptr, chunks, L.aspis_tensor_chunks(numel.ctypes.data, n)
+
+
+@pytest.mark.parametrize("numels,dtypes", [
+    ([7840, 10], [0, 0]), ([], []), ([0], [1]), ([0, 5, 0, 0, 3, 0], [0, 1, 2, 0, 2, 1]),
+    ([1, 4096, 4097, 8192, 100_000], [2, 0, 1, 0, 2])])
+def test_a_table_covers_every_element_once(numels, dtypes):
+    ptr, entries, n_chunks = _table(numels, dtypes)
+    chunks, tensors = entries[:n_chunks], entries[n_chunks:]
+    assert len(tensors) == len(numels)
+    k = filled = 0
+    for i, (n, t) in enumerate(zip(numels, dtypes)):
+        assert (tensors[i].addr, tensors[i].info) == (k, filled)
+        at = 0
+        for _ in range(tensors[i].n):
+            c = chunks[k]
+            assert c.addr == int(ptr[i]) + at * SIZE[t] and 0 < c.n <= 4096
+            assert c.info == filled * 4 + t
+            at += c.n
+            k += 1
+        assert at == n
+        filled += n > 0
+    assert k == n_chunks
+
+
+def test_table_refusals():
+    L = aspis.lib()
+    one = np.array([5], dtype=np.int64)
+    kind = np.array([0], dtype=np.int32)
+    out = np.zeros((2, 2), dtype=np.uint64)
+
+    def table(ptr=4096, numel=one, dtype=kind, count=1, buf=out, cap=2):
+        p = np.array([ptr], dtype=np.uint64)
+        return L.aspis_tensor_table(p.ctypes.data, numel.ctypes.data, dtype.ctypes.data, count,
+                                    buf.ctypes.data if buf is not None else None, cap)
+
+    assert table() == aspis.OK
+    assert table(ptr=0) == aspis.ERR_INVALID_ARG
+    assert table(ptr=4098) == aspis.ERR_INVALID_ARG            # misaligned float32
+    assert table(ptr=4098, dtype=np.array([1], dtype=np.int32)) == aspis.OK
+    assert table(dtype=np.array([3], dtype=np.int32)) == aspis.ERR_INVALID_ARG
+    assert table(numel=np.array([-1], dtype=np.int64)) == aspis.ERR_INVALID_ARG
+    assert table(numel=np.array([1 << 39], dtype=np.int64)) == aspis.ERR_OVERFLOW
+    assert table(numel=np.array([1 << 62], dtype=np.int64)) == aspis.ERR_OVERFLOW
+    assert table(count=-1) == aspis.ERR_INVALID_ARG
+    assert table(buf=None) == aspis.ERR_INVALID_ARG
+    out[:] = 7
+    assert table(cap=1) == aspis.ERR_BUFFER_SMALL
+    assert (out == 7).all()
+    assert table(ptr=0, numel=np.array([0], dtype=np.int64)) == aspis.OK
+    assert L.aspis_tensor_chunks(None, 1) == -1 and L.aspis_tensor_entries(None, 0) == 0
+    assert L.aspis_norm_workspace(-1) == 0 and L.aspis_norm_workspace(0) > 0
+
+
+P = 1 << 20   # an address that nothing reads: every call below is refused
+
+
+def _list_calls():
+    L = aspis.lib()
+    sgd = lambda **k: aspis.SgdOptions(**{"lr": 0.1, "momentum": 0.9, "max_norm": 1.0, **k})
+    adam = lambda **k: aspis.AdamwOptions(**{"lr": 0.1, "beta_one": 0.9, "beta_two": 0.99,
+                                             "eps": 1e-8, "max_norm": 1.0, "step": 1, **k})
+    ws = 1 << 20
+    bad, small = aspis.ERR_INVALID_ARG, aspis.ERR_BUFFER_SMALL
+    norm = lambda t=P, n=3, k=1, s=P, o=P, w=P, b=ws: L.aspis_grad_norm(t, n, k, s, o, None, w, b, None)
+    clip = lambda t=P, out=None, n=3, m=1.0, s=P, o=P, f=0, w=P, b=ws: \
+        L.aspis_clip_grads(t, out, n, m, s, o, f, w, b, None)
+    up = lambda p=P, g=P, m=P, c=None, n=3, o=None, s=P, r=P, w=P, b=ws, **k: L.aspis_clipped_sgd(
+        p, g, m, c, n, ctypes.byref(sgd(**k) if o is None else o), s, r, w, b, None)
+    ad = lambda p=P, g=P, m=P, v=P, c=None, n=3, s=P, r=P, w=P, b=ws, **k: L.aspis_clipped_adamw(
+        p, g, m, v, c, n, ctypes.byref(adam(**k)), s, r, w, b, None)
+    nan, inf = math.nan, math.inf
+    yield from [(bad, norm, {"t": None}), (bad, norm, {"n": -1}), (bad, norm, {"n": 1 << 40}),
+                (bad, norm, {"s": None}), (bad, norm, {"o": None}), (bad, norm, {"t": P + 8}),
+                (bad, norm, {"w": P + 8}), (bad, norm, {"k": -1}), (small, norm, {"w": None}),
+                (small, norm, {"b": 16})]
+    yield from [(bad, clip, {"t": None}), (bad, clip, {"m": -1.0}), (bad, clip, {"m": nan}),
+                (bad, clip, {"out": P + 4}), (bad, clip, {"f": 2}), (small, clip, {"b": 0})]
+    yield from [(bad, up, {"p": None}), (bad, up, {"g": None}), (bad, up, {"m": None}),
+                (bad, up, {"p": P + 8}), (bad, up, {"m": P + 8}), (bad, up, {"c": P + 8}),
+                (bad, up, {"lr": nan}), (bad, up, {"lr": inf}), (bad, up, {"momentum": 1.0}),
+                (bad, up, {"momentum": -0.1}), (bad, up, {"weight_decay": -1.0}),
+                (bad, up, {"max_norm": nan}), (bad, up, {"flags": 4}), (small, up, {"b": 8})]
+    yield from [(bad, ad, {"v": None}), (bad, ad, {"m": None}), (bad, ad, {"step": 0}),
+                (bad, ad, {"beta_one": 1.0}), (bad, ad, {"beta_two": nan}), (bad, ad, {"eps": -1.0}),
+                (bad, ad, {"weight_decay": inf}), (bad, ad, {"c": P + 8}), (bad, ad, {"flags": 8})]
+    rows = lambda x=P, r=4, d=8, ld=8, t=0, n=P, w=P, b=ws: L.aspis_row_norms(x, r, d, ld, t, n, w, b, None)
+    crows = lambda x=P, r=4, d=8, ld=8, t=0, m=1.0, o=1 << 30, ldo=8, n=P, f=0, w=P, b=ws: \
+        L.aspis_clip_rows(x, r, d, ld, t, m, o, ldo, n, f, w, b, None)
+    yield from [(bad, rows, {"x": None}), (bad, rows, {"x": P + 2}), (bad, rows, {"ld": 7}),
+                (bad, rows, {"r": -1}), (bad, rows, {"d": -1}), (bad, rows, {"t": 3}),
+                (bad, rows, {"n": None}), (small, rows, {"d": 1 << 20, "ld": 1 << 20, "b": 8}),
+                (aspis.ERR_OVERFLOW, rows, {"r": 1 << 40, "ld": 1 << 40}),
+                (aspis.ERR_OVERFLOW, rows, {"d": 1 << 35, "ld": 1 << 35})]
+    yield from [(bad, crows, {"m": -1.0}), (bad, crows, {"m": nan}), (bad, crows, {"o": None}),
+                (bad, crows, {"o": (1 << 30) + 1}), (bad, crows, {"ldo": 7}), (bad, crows, {"f": 1}),
+                (bad, crows, {"o": P + 4}), (bad, crows, {"o": P + 32}),      # overlaps
+                (bad, crows, {"o": P, "ldo": 9}), (bad, crows, {"o": P - 64})]
+
+
+def test_every_refusal():
+    for status, call, args in _list_calls():
+        assert call(**args) == status, (args, aspis.lib().aspis_last_error())
+        assert aspis.lib().aspis_last_error()
+
+
+def test_workspaces_grow_with_the_work():
+    L = aspis.lib()
+    assert L.aspis_norm_workspace(1 << 20) > L.aspis_norm_workspace(1) > 0
+    assert L.aspis_row_workspace(1000, 30_000, 0) == 0        # in registers
+    assert L.aspis_row_workspace(1000, 40_000, 0) > 0
+    assert L.aspis_row_workspace(1000, 60_000, 1) == 0
+    assert L.aspis_row_workspace(0, 1 << 30, 0) == 0
+    for bad in ((-1, 5, 0), (5, -1, 0), (5, 5, 7), (1 << 40, 1 << 40, 0), (1, 1 << 35, 0)):
+        assert L.aspis_row_workspace(*bad) == 2 ** 64 - 1, bad
+
+
+def test_missing_library_raises(monkeypatch, tmp_path):
+    monkeypatch.setattr(aspis, "LIB_PATH", str(tmp_path / "libaspis.so"))
+    monkeypatch.setattr(aspis, "_lib", None)
+    import torch
+    with pytest.raises(ImportError, match="libaspis.so is missing"):
+        aspis.TensorList([], device=torch.device("cuda", 0))
+
+
+@pytest.mark.skipif(shutil.which("g++") is None
+                    or not os.path.exists(os.path.join(ROCM, "lib", "libamdhip64.so")),
+                    reason="needs g++ and the ROCm host runtime library")
+def test_host_code_under_sanitizers(tmp_path):
+    src = os.path.join(ROOT, "tests", "host_sanitize")
+    csrc = os.path.join(ROOT, "paper_2108_02416_amd", "csrc")
+    exe = tmp_path / "clip_sanitize"
+    subprocess.run(["g++", "-std=c++17", "-fsanitize=address,undefined",
+                    "-fno-sanitize-recover=undefined", "-fno-omit-frame-pointer", "-g", "-O1",
+                    "-D__HIP_PLATFORM_AMD__", "-I", os.path.join(ROCM, "include"),
+                    os.path.join(src, "clip_driver.cpp"), os.path.join(src, "device_stubs.cpp"),
+                    os.path.join(csrc, "aspis_clip.cpp"), os.path.join(csrc, "aspis_host.cpp"),
+                    "-L", os.path.join(ROCM, "lib"), f"-Wl,-rpath,{ROCM}/lib", "-lamdhip64",
+                    "-lpthread", "-o", str(exe)], check=True)
+    out = subprocess.run([str(exe)], capture_output=True, text=True, timeout=300,
+                         env=dict(os.environ, ASAN_OPTIONS="detect_leaks=0:abort_on_error=0"))
+    assert out.returncode == 0, out.stdout + out.stderr
+    assert out.stdout.strip().endswith("ok")
+    assert "runtime error" not in out.stderr and "AddressSanitizer" not in out.stderr, out.stderr

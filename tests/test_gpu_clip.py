@@ -498,6 +498,47 @@ def test_clipped_adamw(name, kind, step, wd, copy):
             _assert_copy(copies[i], params[i])
 
 
+@pytest.mark.parametrize("rule,n,kind", [("sgd", 51_000_001, "bfloat16"), ("sgd", 3_000_001, "float32"),
+                                         ("adamw", 12_000_003, "float32"),
+                                         ("adamw", 34_000_001, "float16")])
+def test_updates_of_long_lists(rule, n, kind):
+    """The kernels for lists of some thousand chunks and of more than the
+    cache keeps, against the formulas in 64 bits on the GPU."""
+    import torch
+    sizes = [n // 3, 5, n - n // 3 - 5]
+    grads = _views(sizes, kind, seed=1, offset=1)
+    params, mean = _views(sizes, seed=2, offset=2, scale=0.5), _views(sizes, seed=3, scale=0.003)
+    square = [v.square_() for v in _views(sizes, seed=4, offset=1, scale=0.003)]
+    copies = [torch.empty(k, dtype=torch.bfloat16, device=device()) for k in sizes]
+    norm = math.sqrt(sum(float(g.double().square().sum()) for g in grads))
+    bound, lr = 0.3 * norm, 3e-3
+    start = [[t.double() for t in x] for x in (params, mean, square)]
+    if rule == "sgd":
+        bufs = aspis.clipped_sgd(params, grads, mean, lr=lr, momentum=0.9, max_norm=bound,
+                                 copies=copies)
+    else:
+        bufs = aspis.clipped_adamw(params, grads, mean, square, step=3, lr=lr, betas=(0.9, 0.95),
+                                   weight_decay=0.1, max_norm=bound, copies=copies)
+    _assert_norm(bufs.norm, norm)
+    for i in range(3):
+        g = 0.3 * grads[i].double()
+        p, m, v = (x[i] for x in start)
+        if rule == "sgd":
+            m_tol = 8 * U * (g.abs() + 0.9 * m.abs() * 2)
+            m = 0.9 * m + g
+            p_tol, p = 8 * U * p.abs() + lr * m_tol, p - lr * m
+        else:
+            m_tol = 6 * U * (0.9 * m.abs() + 0.1 * g.abs())
+            m, v = 0.9 * m + 0.1 * g, 0.95 * v + 0.05 * g * g
+            rate, root = lr / (1 - 0.9 ** 3), (v / (1 - 0.95 ** 3)).sqrt() + 1e-8
+            p_tol = 4 * U * p.abs() + rate * (m_tol + 16 * U * m.abs()) / root
+            p = p * (1 - lr * 0.1) - rate * m / root
+            assert bool(((square[i].double() - v).abs() <= 8 * U * v + 1e-44).all())
+        assert bool(((mean[i].double() - m).abs() <= m_tol + 1e-44).all())
+        assert bool(((params[i].double() - p).abs() <= p_tol + 1e-44).all())
+        assert bool((copies[i] == params[i].bfloat16()).all())
+
+
 def test_unclipped_updates_use_the_gradients_bits():
     """Without a bound SGD with lr = 1 from zero gives -g to the bit."""
     import torch
