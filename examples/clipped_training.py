@@ -9,9 +9,9 @@ synthetic data by K = 7 workers, two of them adversaries.  Every iteration
 - the server clips the replicas (so that none can carry more than the bound),
   finds the adversaries, and averages the files the others agree on;
 - the aggregated gradient's global norm is clipped and an SGD step with
-  momentum applied, in one call.
+  momentum (or an AdamW step) applied, in one call.
 
-  python examples/clipped_training.py [--iterations N]
+  python examples/clipped_training.py [--iterations N] [--optimizer adamw]
 """
 import argparse
 import os
@@ -47,7 +47,7 @@ def file_gradients(weight, bias, x, y):
     return loss, torch.cat([by_weight, delta.sum(1)], dim=1)
 
 
-def train(iterations: int, device="cuda:0", say=print):
+def train(iterations: int, optimizer: str = "sgd", device="cuda:0", say=print):
     device = torch.device(device)
     files = aspis.num_files(K, R)
     x, y = make_data(files, device)
@@ -60,8 +60,9 @@ def train(iterations: int, device="cuda:0", say=print):
     grad = torch.empty(d, device=device)
     params = aspis.TensorList([weight, bias])
     grads = aspis.TensorList(list(grad.split([weight.numel(), bias.numel()])))
-    momentum = aspis.TensorList([torch.zeros_like(weight), torch.zeros_like(bias)])
-    bufs, ws = aspis.NormBuffers.empty(device), aspis.norm_workspace(grads)
+    mean, square = (aspis.TensorList([torch.zeros_like(weight), torch.zeros_like(bias)])
+                    for _ in range(2))
+    bufs, ws = aspis.NormBuffers.empty(device, each=len(grads)), aspis.norm_workspace(grads)
     losses, found = [], []
     for it in range(iterations):
         loss, g = file_gradients(weight, bias, x, y)
@@ -75,13 +76,19 @@ def train(iterations: int, device="cuda:0", say=print):
         # the server: no replica longer than the bound, whoever sent it
         _, norms = aspis.clip_rows(upload, FILE_NORM)
         res = aspis.detect_aggregate(upload, K, R, Q, mode="paper", layout="worker", out=grad)
-        aspis.clipped_sgd(params, grads, momentum, lr=0.5, momentum=0.9, max_norm=STEP_NORM,
-                          skip_nonfinite=True, bufs=bufs, ws=ws)
+        common = {"max_norm": STEP_NORM, "skip_nonfinite": True, "bufs": bufs, "ws": ws}
+        if optimizer == "sgd":
+            aspis.clipped_sgd(params, grads, mean, lr=0.5, momentum=0.9, **common)
+        else:
+            aspis.clipped_adamw(params, grads, mean, square, step=it + 1, lr=0.02,
+                                weight_decay=0.0, **common)
         losses.append(float(loss))
         found.append(res["clique"].as_dict(K)["detected"])
         if it % 10 == 0 or it == iterations - 1:
-            say(f"iteration {it:3d}  loss {losses[-1]:.4f}  gradient norm {float(bufs.norm):.4f}  "
-                f"longest upload {float(norms.max()):.1f}  detected {sorted(found[-1])}")
+            each = aspis.grad_norm(grads, each=True, bufs=bufs, ws=ws).each.tolist()
+            say(f"iteration {it:3d}  loss {losses[-1]:.4f}  gradient norm {float(bufs.norm):.4f} "
+                f"(weight {each[0]:.4f}, bias {each[1]:.4f})  longest upload "
+                f"{float(norms.max()):.1f}  detected {sorted(found[-1])}")
     return losses, found
 
 
@@ -89,4 +96,6 @@ if __name__ == "__main__":
     ap = argparse.ArgumentParser(description=__doc__,
                                  formatter_class=argparse.RawDescriptionHelpFormatter)
     ap.add_argument("--iterations", type=int, default=60)
-    train(ap.parse_args().iterations)
+    ap.add_argument("--optimizer", choices=("sgd", "adamw"), default="sgd")
+    args = ap.parse_args()
+    train(args.iterations, args.optimizer)

@@ -982,8 +982,9 @@ hipError_t rows_of(const RowArgs &a, hipStream_t s) {
 }
 
 // Chunks at the end of a list that the last-level cache (256 MB) keeps from
-// one pass to the next: 192 MB of f32.
-constexpr int64_t kKeepChunks = (int64_t)192 * 1024 * 1024 / (4 * kChunk);
+// one pass to the next, of f32.  Of 180 MB clipped: 85.7 us, with 192 MB
+// kept 87.6, with 320 MB 86.2.
+constexpr int64_t kKeepChunks = (int64_t)256 * 1024 * 1024 / (4 * kChunk);
 // From here on the partial sums are joined by a launch of their own; below,
 // by every workgroup that scales a chunk.
 constexpr int64_t kJoinChunks = 8192;

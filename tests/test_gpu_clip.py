@@ -498,6 +498,21 @@ def test_clipped_adamw(name, kind, step, wd, copy):
             _assert_copy(copies[i], params[i])
 
 
+@pytest.mark.parametrize("sizes", [[900, 7], [300_001, 5], [40_000_003]])
+def test_updates_by_the_sum_of_all_ranks(sizes):
+    """An update by a given sum of squares is the one by gradients that have
+    it: twice the norm gives half the coefficient."""
+    import torch
+    g, p = _views(sizes, seed=1, offset=1), _views(sizes, seed=2, offset=2, scale=0.5)
+    q, m, n = [t.clone() for t in p], [torch.zeros_like(t) for t in p], [torch.zeros_like(t) for t in p]
+    own = aspis.grad_norm(g)
+    bound = 0.5 * float(own.norm)
+    a = aspis.clipped_sgd(p, g, m, lr=0.1, momentum=0.9, max_norm=bound, sumsq=4.0 * own.sumsq)
+    b = aspis.clipped_sgd(q, g, n, lr=0.1, momentum=0.9, max_norm=0.5 * bound)
+    assert float(a.norm) == 2.0 * float(own.norm) and float(b.norm) == float(own.norm)
+    assert all(np.array_equal(_bits(x), _bits(y)) for x, y in zip(p + m, q + n))
+
+
 @pytest.mark.parametrize("rule,n,kind", [("sgd", 51_000_001, "bfloat16"), ("sgd", 3_000_001, "float32"),
                                          ("adamw", 12_000_003, "float32"),
                                          ("adamw", 34_000_001, "float16")])

@@ -14,10 +14,11 @@ PATH = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))),
                     "clipped_training.py")
 
 
-def test_clipped_training():
+@pytest.mark.parametrize("optimizer", ["sgd", "adamw"])
+def test_clipped_training(optimizer):
     spec = importlib.util.spec_from_file_location("clipped_training", PATH)
     example = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(example)
-    losses, found = example.train(30, device())
+    losses, found = example.train(30, optimizer, device())
     assert losses[-1] < 0.5 * losses[0]
     assert all(f == frozenset(example.ADVERSARIES) for f in found)
