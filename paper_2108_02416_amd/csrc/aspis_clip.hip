@@ -201,24 +201,56 @@ __device__ __forceinline__ void add_squares(u32x4 w, double (&acc)[2]) {
 template <typename E, int L, int R>
 struct Span {
     static constexpr int V = E::V, Q = (V - 2 + L) / L;
+    // 16-bit elements at an address that is not a multiple of four: a 16-byte
+    // load there takes the memory pipeline longer, so the vectors are loaded
+    // from one element earlier (in the same aligned word as the first
+    // element, which is never the first of an allocation) and shifted, the
+    // last element coming from the next lane.  6,900 rows of 10,007 f16: 50.8
+    // against 54.4 us; a list of 200M bf16 from an odd place: clip 203 against
+    // 218 us.  Not in a wave's rows (50,000 of 1,001: 37.7 against 36.0) nor
+    // with more vectors (24: the registers spill).
+    static constexpr bool kShift = V == 8 && L >= 256 && R >= 2 && R <= 8;
     u32x4 w[R];
     float tail[Q];
 
     template <Use USE>
     __device__ __forceinline__ void load(Ptr<E> p, int n, int lane) {
+        const bool odd = kShift && ((uint64_t)p & 2) != 0;
+        const Ptr<E> from = odd ? p - 1 : p;
+        const int nv = n / V;
         if (n == R * L * V) {
 #pragma unroll
-            for (int r = 0; r < R; ++r) w[r] = load_vec<E, USE>(p + (lane + r * L) * V);
+            for (int r = 0; r < R; ++r) w[r] = load_vec<E, USE>(from + (lane + r * L) * V);
+        } else {
 #pragma unroll
-            for (int q = 0; q < Q; ++q) tail[q] = 0.0f;
-            return;
+            for (int r = 0; r < R; ++r) {
+                w[r] = (u32x4){0, 0, 0, 0};
+                if (lane + r * L < nv) w[r] = load_vec<E, USE>(from + (lane + r * L) * V);
+            }
         }
-        const int nv = n / V;
+        if constexpr (kShift)
+            if (odd) {
+                uint32_t own[R];   // where the next lane does not load the next vector
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            w[r] = (u32x4){0, 0, 0, 0};
-            if (lane + r * L < nv) w[r] = load_vec<E, USE>(p + (lane + r * L) * V);
-        }
+                for (int r = 0; r < R; ++r) {
+                    own[r] = 0;
+                    const int i = lane + r * L;
+                    if (i < nv && (lane == L - 1 || threadIdx.x % 64 == 63 || i == nv - 1))
+                        own[r] = *(const uint16_t GLOBAL *)(p + i * V + 7);
+                }
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const int i = lane + r * L;
+                    const u32x4 a = w[r];
+                    uint32_t last = __builtin_amdgcn_update_dpp(0, (int)a.x, 0x130, 0xF, 0xF, true);
+                    if (lane == L - 1 || threadIdx.x % 64 == 63 || i == nv - 1) last = own[r];
+                    if (i < nv)
+                        w[r] = (u32x4){__builtin_amdgcn_alignbit(a.y, a.x, 16),
+                                       __builtin_amdgcn_alignbit(a.z, a.y, 16),
+                                       __builtin_amdgcn_alignbit(a.w, a.z, 16),
+                                       last << 16 | a.w >> 16};
+                }
+            }
 #pragma unroll
         for (int q = 0; q < Q; ++q) {
             const int i = nv * V + lane + q * L;
