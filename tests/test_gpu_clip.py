@@ -608,6 +608,29 @@ def test_lists_and_buffers_on_another_stream():
     _assert_norm(a.norm, _norm64(ts))
 
 
+def test_long_rows_on_two_streams_at_once():
+    """Two calls whose rows each take most of the device: workgroups that
+    wait for others that cannot start give up and their parts are read again.
+    Both results are those of a call alone."""
+    import torch
+    xs = [_randn(6 * 11_000_001, seed=s).reshape(6, 11_000_001) for s in (1, 2)]
+    bound = 0.004 * math.sqrt(11_000_001)
+    want = [aspis.clip_rows(x, bound, out=torch.empty_like(x)) for x in xs]
+    streams = [torch.cuda.Stream() for _ in xs]
+    outs = [torch.empty_like(x) for x in xs]
+    sizes = [aspis.row_workspace(x) for x in xs]
+    norms = [torch.empty(6, device=device()) for _ in xs]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for x, o, n, w, s in zip(xs, outs, norms, sizes, streams):
+            with torch.cuda.stream(s):
+                o.zero_()
+                aspis.clip_rows(x, bound, out=o, norms=n, ws=w)
+        torch.cuda.synchronize()
+        for (a, b), o, n in zip(want, outs, norms):
+            assert bool((a == o).all()) and bool((b == n).all())
+
+
 def test_in_a_graph():
     """An update and a clip of rows captured once and replayed on new
     gradients, with other work between the replays."""
