@@ -545,6 +545,24 @@ def _launch(device, call, *args):
             _check(call(*args))
 
 
+_state = None
+
+
+def _tensor_state(tensors) -> bytes:
+    """Where the tensors of a list are and how they are laid out
+    (csrc/aspis_tensors.cpp)."""
+    global _state
+    if _state is None:
+        import torch  # noqa: F401  (its libraries come first)
+        try:
+            from ._tensors import state
+        except ImportError as e:
+            raise ImportError(f"{os.path.join(HERE, '_tensors.so')} is missing or does not load "
+                              f"({e}): run python -c 'import __graft_entry__ as g; g.build()'") from e
+        _state = state
+    return _state(tensors)
+
+
 class TensorList:
     """A list of CUDA tensors as the norm, clipping and update calls take it
     (aspis_tensor_table): made once for tensors that stay, or by the call
@@ -553,8 +571,9 @@ class TensorList:
     Tensors are float32, bfloat16 or float16 (types may mix), on one device,
     of any shape, also empty; each must fill one span of memory (any order of
     its dimensions, no gaps).  The list holds the tensors and looks at every
-    call whether they still are where they were, so that a tensor whose
-    storage was replaced (`t.data = ...`) is read where it is now."""
+    call whether they still are where they were, of the types and in the
+    layouts they had, so that a tensor whose storage was replaced
+    (`t.data = ...`) is read as it is now."""
 
     def __init__(self, tensors, device=None):
         torch = _torch()
@@ -579,8 +598,8 @@ class TensorList:
         torch = _torch()
         ts = self.tensors
         n = len(ts)
-        self._where = self._now()
-        where, self.numels = self._where
+        self._where = _tensor_state(ts)
+        where, self.numels = [t.data_ptr() for t in ts], [t.numel() for t in ts]
         self.dtypes = [t.dtype for t in ts]
         codes = np.array([_dtype_code(d) for d in self.dtypes], dtype=np.int32)
         self.contiguous = True
@@ -616,13 +635,9 @@ class TensorList:
     def layouts(self):
         return [_layout(t) for t in self.tensors]
 
-    def _now(self):
-        Tensor = _torch().Tensor
-        return list(map(Tensor.data_ptr, self.tensors)), list(map(Tensor.numel, self.tensors))
-
     def table(self) -> int:
         """Device address of the table, brought up to date."""
-        if self._now() != self._where:
+        if _tensor_state(self.tensors) != self._where:
             self._read()
         if _raw_stream(self.device) != self._stream:
             self._table.record_stream(_torch().cuda.current_stream(self.device))

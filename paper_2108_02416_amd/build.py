@@ -1,19 +1,24 @@
-"""Build libaspis.so (gfx950) in-tree with hipcc.
+"""Build libaspis.so (gfx950) in-tree with hipcc, and the binding's Python
+module _tensors.so with g++.
 
 The library is the C ABI declared in include/aspis.h: host code
 (csrc/aspis_host.cpp, csrc/aspis_sim.cpp) plus the HIP kernels
 (csrc/aspis_kernels.hip, and csrc/aspis_ws_*.hip for the warp-specialised
-kernels' many instantiations).
+kernels' many instantiations).  _tensors (csrc/aspis_tensors.cpp) reads the
+addresses and layouts of torch tensors.
 """
+import importlib.util
 import os
 import subprocess
 import sys
+import sysconfig
 import tempfile
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libaspis.so")
+TENSORS = os.path.join(HERE, "_tensors.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
@@ -36,8 +41,19 @@ def _run(cmd: list[str]) -> list[str]:
             if "packed-fp32-ops" not in ln and ln.strip()]
     if r.returncode != 0:
         sys.stderr.write("\n".join(msgs) + "\n")
-        raise RuntimeError("hipcc failed building libaspis.so")
+        raise RuntimeError(f"{os.path.basename(cmd[0])} failed building {cmd[cmd.index('-o') + 1]}")
     return msgs
+
+
+def _tensors_command() -> list[str]:
+    # found without importing torch: its path is all that is needed
+    torch = importlib.util.find_spec("torch").submodule_search_locations[0]
+    return ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-Wno-unused-function",
+            "-I", os.path.join(torch, "include"),
+            "-I", os.path.join(torch, "include", "torch", "csrc", "api", "include"),
+            "-I", sysconfig.get_paths()["include"],
+            "-o", TENSORS + ".tmp", os.path.join(HERE, "csrc", "aspis_tensors.cpp"),
+            "-L", os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
 
 
 def build(verbose: bool = False) -> str:
@@ -49,6 +65,7 @@ def build(verbose: bool = False) -> str:
         for src in SOURCES:
             objs.append(os.path.join(tmp, src + ".o"))
             cmds.append([HIPCC, *flags, "-c", "-o", objs[-1], os.path.join(HERE, "csrc", src)])
+        cmds.append(_tensors_command())
         link = [HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", LIB + ".tmp", *objs]
         if verbose:
             print("\n".join(" ".join(c) for c in [*cmds, link]), flush=True)
@@ -58,6 +75,7 @@ def build(verbose: bool = False) -> str:
     if verbose and msgs:
         print("\n".join(msgs))
     os.replace(LIB + ".tmp", LIB)
+    os.replace(TENSORS + ".tmp", TENSORS)
     return LIB
 
 

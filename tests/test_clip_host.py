@@ -159,6 +159,32 @@ def test_missing_library_raises(monkeypatch, tmp_path):
         aspis.TensorList([], device=torch.device("cuda", 0))
 
 
+def test_the_state_of_a_list_of_tensors():
+    import torch
+    a, b = torch.zeros(12, dtype=torch.bfloat16), torch.zeros(5)
+    now = aspis._tensor_state([a, b])
+    assert now == aspis._tensor_state([a, b])
+    assert aspis._tensor_state([]) == b""
+    for other in ([b, a], [a], [a.view(torch.float16), b], [a[:11], b], [a[1:], b], [a, b.clone()]):
+        assert aspis._tensor_state(other) != now
+    # the same elements in another shape, but not in another order
+    assert aspis._tensor_state([a.reshape(3, 4), b]) == now
+    turned = aspis._tensor_state([a.reshape(3, 4).t(), b])
+    assert turned != now and turned != aspis._tensor_state([a.reshape(2, 6).t(), b])
+    for wrong in ((a, b), [a, 1], None):
+        with pytest.raises(TypeError):
+            aspis._tensor_state(wrong)
+
+
+def test_missing_module_raises(monkeypatch):
+    import sys
+    import torch
+    monkeypatch.setattr(aspis, "_state", None)
+    monkeypatch.setitem(sys.modules, "paper_2108_02416_amd._tensors", None)
+    with pytest.raises(ImportError, match="_tensors.so is missing"):
+        aspis.TensorList([], device=torch.device("cuda", 0))
+
+
 @pytest.mark.skipif(shutil.which("g++") is None
                     or not os.path.exists(os.path.join(ROCM, "lib", "libamdhip64.so")),
                     reason="needs g++ and the ROCm host runtime library")

@@ -748,3 +748,24 @@ def test_refusals():
     refused(bad, lambda: aspis.row_norms(x, norms=torch.ones(5, device=dev)))
     refused(bad, lambda: aspis.clip_rows(x, 1.0, flags=8))
     assert bool((x == 1).all())
+
+
+def test_a_list_sees_a_type_or_layout_that_changes_in_place():
+    """Same address, same number of elements: another type, another order."""
+    import torch
+    memory = _randn(600, "bfloat16", seed=4)
+    t = memory.reshape(20, 30)
+    handle, out = aspis.TensorList([t]), aspis.TensorList([torch.empty_like(t)])
+    _assert_norm(aspis.grad_norm(handle).norm, _norm64([t]))
+    t.data = memory.view(torch.float16).reshape(20, 30)
+    assert t.data_ptr() == memory.data_ptr()
+    _assert_norm(aspis.grad_norm(handle).norm, _norm64([t]))
+    with pytest.raises(aspis.AspisError):   # out is still bfloat16
+        aspis.clip_grads(handle, 1.0, out=out)
+    t.data = memory.reshape(30, 20).t()
+    with pytest.raises(aspis.AspisError):   # out has another order of elements
+        aspis.clip_grads(handle, 1.0, out=out)
+    same = [torch.empty_like(t)]
+    norm = _norm64([t])
+    aspis.clip_grads(handle, norm / 2, out=same)
+    _assert_scaled(same[0], t, 0.5, "bfloat16")
