@@ -26,9 +26,9 @@
  * returns a message for the calling thread's last failure.
  *
  * Asynchrony: aspis_detect, aspis_aggregate and the norm, clipping and
- * update calls only enqueue work on the stream.  aspis_clique is host code.  aspis_detect_aggregate synchronises
- * the stream (it needs the agreement graph on the host) and returns with
- * its work complete.
+ * update calls only enqueue work on the stream.  aspis_clique is host code.
+ * aspis_detect_aggregate synchronises the stream (it needs the agreement
+ * graph on the host) and returns with its work complete.
  *
  * Thread safety: re-entrant.  Global state: the per-thread error message,
  * a per-device cache of the compute-unit count (written once per device
@@ -480,8 +480,8 @@ aspis_status aspis_clip_grads(const aspis_chunk *table, const aspis_chunk *out_t
 
 /* Rows: x holds `rows` rows of d elements, ld >= d elements from one row's
  * start to the next (a replica tensor [f][r][d] has f*r rows, a worker's
- * upload [l][d] has l); d is at most 2^34.  aspis_row_workspace: bytes of workspace for them
- * (may be 0; SIZE_MAX on invalid arguments). */
+ * upload [l][d] has l); d is at most 2^34.  aspis_row_workspace: bytes of
+ * workspace for them (may be 0; SIZE_MAX on invalid arguments). */
 size_t aspis_row_workspace(int64_t rows, int64_t d, aspis_dtype dtype);
 
 /* norms[i] = the L2 norm of row i (device float [rows]). */

