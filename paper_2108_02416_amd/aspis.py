@@ -538,29 +538,42 @@ def _launch(device, call, *args):
     """Calls a library function that enqueues work on `device`, and checks
     its status."""
     torch = _torch()
-    if device.index == torch.cuda.current_device():
+    if device.index == torch._C._cuda_getDevice():
         _check(call(*args))
     else:
         with torch.cuda.device(device):
             _check(call(*args))
 
 
-_state = None
+_native = None
 
 
-def _tensor_state(tensors) -> bytes:
-    """Where the tensors of a list are and how they are laid out
-    (csrc/aspis_tensors.cpp)."""
-    global _state
-    if _state is None:
+def _tensors():
+    """The module that looks torch tensors over (csrc/aspis_tensors.cpp)."""
+    global _native
+    if _native is None:
         import torch  # noqa: F401  (its libraries come first)
         try:
-            from ._tensors import state
+            from . import _tensors as module
         except ImportError as e:
             raise ImportError(f"{os.path.join(HERE, '_tensors.so')} is missing or does not load "
                               f"({e}): run python -c 'import __graft_entry__ as g; g.build()'") from e
-        _state = state
-    return _state(tensors)
+        _native = module
+    return _native
+
+
+def _tensor_state(tensors) -> bytes:
+    """Where the tensors of a list are and how they are laid out."""
+    return _tensors().state(tensors)
+
+
+def _buffer(name: str, t, dtype, n: int, device) -> int:
+    """The address of a caller's buffer, checked as _check_buffer does."""
+    at = _tensors().buffer(t, dtype, n, device.index)
+    if at is None:
+        _check_buffer(name, t, dtype, n, device)
+        at = t.data_ptr()
+    return at
 
 
 class TensorList:
@@ -692,25 +705,23 @@ def norm_workspace(grads):
     return torch.empty(grads.ws_bytes, dtype=torch.uint8, device=grads.device)
 
 
-def _norm_buffers(grads: TensorList, bufs, ws, sumsq, each: int = 0):
-    """Checked or new buffers of a call, and the flags they ask for."""
+def _scratch(grads: TensorList, bufs, ws, sumsq, each: int = 0):
+    """Checked or new buffers of a call: bufs, the addresses of norm, sum of
+    squares and each, the workspace and its address, and the flags they ask for."""
     torch = _torch()
-    dev = grads.device
+    dev, f32, f64 = grads.device, torch.float32, torch.float64
     if bufs is None:
         bufs = NormBuffers.empty(dev, each)
-    else:
-        _check_buffer("bufs.norm", bufs.norm, torch.float32, 1, dev)
-        _check_buffer("bufs.sumsq", bufs.sumsq, torch.float64, 1, dev)
-        if each:
-            _check_buffer("bufs.each", bufs.each, torch.float32, each, dev)
+    norm = _buffer("bufs.norm", bufs.norm, f32, 1, dev)
+    total = _buffer("bufs.sumsq", bufs.sumsq, f64, 1, dev)
+    each_at = _buffer("bufs.each", bufs.each, f32, each, dev) if each else None
+    flags = 0
     if sumsq is not None:
-        _check_buffer("sumsq", sumsq, torch.float64, 1, dev)
+        total, flags = _buffer("sumsq", sumsq, f64, 1, dev), CLIP_HAVE_SUMSQ
     if ws is None:
         ws = torch.empty(grads.ws_bytes, dtype=torch.uint8, device=dev)
-    else:
-        _check_buffer("ws", ws, torch.uint8, grads.ws_bytes, dev)
-    return bufs, ws, bufs.sumsq if sumsq is None else sumsq, \
-        0 if sumsq is None else CLIP_HAVE_SUMSQ
+    ws_at = _buffer("ws", ws, torch.uint8, grads.ws_bytes, dev)
+    return bufs, norm, total, each_at, ws, ws_at, flags
 
 
 def grad_norm(grads, each: bool = False, bufs: NormBuffers | None = None, ws=None) -> NormBuffers:
@@ -720,11 +731,10 @@ def grad_norm(grads, each: bool = False, bufs: NormBuffers | None = None, ws=Non
     bufs.sumsq and hand it to clip_grads or an update as sumsq."""
     grads = _list(grads)
     table = grads.table()
-    bufs, ws, sumsq, _ = _norm_buffers(grads, bufs, ws, None, len(grads) if each else 0)
-    _launch(grads.device, lib().aspis_grad_norm, table, grads.n_chunks, len(grads),
-            sumsq.data_ptr(), bufs.norm.data_ptr(),
-            bufs.each.data_ptr() if each and len(grads) else None, ws.data_ptr(), ws.numel(),
-            _raw_stream(grads.device))
+    bufs, norm, total, each_at, ws, ws_at, _ = _scratch(grads, bufs, ws, None,
+                                                        len(grads) if each else 0)
+    _launch(grads.device, lib().aspis_grad_norm, table, grads.n_chunks, len(grads), total,
+            norm, each_at, ws_at, ws.numel(), _raw_stream(grads.device))
     return bufs
 
 
@@ -736,7 +746,7 @@ def clip_grads(grads, max_norm: float, out=None, sumsq=None, bufs: NormBuffers |
     ranks), instead of this list's own."""
     grads = _list(grads)
     table = grads.table()
-    bufs, ws, total, flags = _norm_buffers(grads, bufs, ws, sumsq)
+    bufs, norm, total, _, ws, ws_at, flags = _scratch(grads, bufs, ws, sumsq)
     if out is None:
         _check_written("grads", grads)
         out_table = None
@@ -746,20 +756,20 @@ def clip_grads(grads, max_norm: float, out=None, sumsq=None, bufs: NormBuffers |
         _check_match("out", out, grads, same_types=True)
         _check_written("out", out)
     _launch(grads.device, lib().aspis_clip_grads, table, out_table, grads.n_chunks, max_norm,
-            total.data_ptr(), bufs.norm.data_ptr(), flags, ws.data_ptr(), ws.numel(),
-            _raw_stream(grads.device))
+            total, norm, flags, ws_at, ws.numel(), _raw_stream(grads.device))
     return bufs
 
 
 def _rows(name: str, x):
     """rows, d, elements between rows' starts and type of a tensor of rows."""
+    plain = _tensors().rows(x)
+    if plain is not None:
+        return plain
     torch = _torch()
     if not isinstance(x, torch.Tensor) or not x.is_cuda or x.dim() < 1:
         raise AspisError(ERR_INVALID_ARG, f"{name} must be a cuda tensor of rows [..., d]")
     code = _dtype_code(x.dtype)
     d = x.shape[-1]
-    if d and x.is_contiguous():
-        return x.numel() // d, d, d, code
     rows = 1
     for n in x.shape[:-1]:
         rows *= n
@@ -793,26 +803,25 @@ def row_workspace(x):
 
 
 def _row_buffers(x, rows: int, d: int, code: int, norms, ws):
+    """Checked or new buffers of a call on rows, and their addresses."""
     torch = _torch()
     if norms is None:
         norms = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
-    else:
-        _check_buffer("norms", norms, torch.float32, rows, x.device)
     if ws is None:
         ws = torch.empty(int(lib().aspis_row_workspace(rows, d, code)), dtype=torch.uint8,
                          device=x.device)
-    else:   # its size is the library's to check
-        _check_buffer("ws", ws, torch.uint8, 0, x.device)
-    return norms, ws
+    # the workspace's size is the library's to check
+    return (norms, _buffer("norms", norms, torch.float32, rows, x.device),
+            ws, _buffer("ws", ws, torch.uint8, 0, x.device))
 
 
 def row_norms(x, norms=None, ws=None):
     """The L2 norm of every row of x [..., d] (aspis_row_norms): the replicas
     [f][r][d] or a worker's upload [l][d]."""
     rows, d, ld, code = _rows("x", x)
-    norms, ws = _row_buffers(x, rows, d, code, norms, ws)
-    _launch(x.device, lib().aspis_row_norms, x.data_ptr(), rows, d, ld, code, norms.data_ptr(),
-            ws.data_ptr(), ws.numel(), _raw_stream(x.device))
+    norms, norms_at, ws, ws_at = _row_buffers(x, rows, d, code, norms, ws)
+    _launch(x.device, lib().aspis_row_norms, x.data_ptr(), rows, d, ld, code, norms_at, ws_at,
+            ws.numel(), _raw_stream(x.device))
     return norms
 
 
@@ -829,10 +838,9 @@ def clip_rows(x, max_norm: float, out=None, norms=None, ws=None, flags: int = 0)
         _, _, ldo, out_code = _rows("out", out)
         if out.shape != x.shape or out_code != code or out.device != x.device:
             raise AspisError(ERR_INVALID_ARG, "out must have the shape, type and device of x")
-    norms, ws = _row_buffers(x, rows, d, code, norms, ws)
+    norms, norms_at, ws, ws_at = _row_buffers(x, rows, d, code, norms, ws)
     _launch(x.device, lib().aspis_clip_rows, x.data_ptr(), rows, d, ld, code, max_norm,
-            out.data_ptr(), ldo, norms.data_ptr(), flags, ws.data_ptr(), ws.numel(),
-            _raw_stream(x.device))
+            out.data_ptr(), ldo, norms_at, flags, ws_at, ws.numel(), _raw_stream(x.device))
     return out, norms
 
 
@@ -868,13 +876,13 @@ def clipped_sgd(params, grads, mean=None, *, lr: float, momentum: float = 0.0,
         raise AspisError(ERR_INVALID_ARG, "momentum needs the list `mean`")
     grads = _list(grads)
     lists, tables = _update_lists(params, grads, {} if mean is None else {"mean": mean}, copies)
-    bufs, ws, total, flags = _norm_buffers(grads, bufs, ws, sumsq)
+    bufs, norm, total, _, ws, ws_at, flags = _scratch(grads, bufs, ws, sumsq)
     opt = SgdOptions(lr, momentum, weight_decay, max_norm, int(nesterov),
                      flags | (CLIP_SKIP_NONFINITE if skip_nonfinite else 0))
     _launch(grads.device, lib().aspis_clipped_sgd, tables[1], tables[0],
             tables[2] if mean is not None else None, tables[-1] if copies is not None else None,
-            grads.n_chunks, ctypes.byref(opt), total.data_ptr(), bufs.norm.data_ptr(),
-            ws.data_ptr(), ws.numel(), _raw_stream(grads.device))
+            grads.n_chunks, ctypes.byref(opt), total, norm, ws_at, ws.numel(),
+            _raw_stream(grads.device))
     del lists   # their tables were needed until here
     return bufs
 
@@ -888,12 +896,11 @@ def clipped_adamw(params, grads, mean, square, *, step: int, lr: float, betas=(0
     (aspis_clipped_adamw); as clipped_sgd otherwise.  step counts from 1."""
     grads = _list(grads)
     lists, tables = _update_lists(params, grads, {"mean": mean, "square": square}, copies)
-    bufs, ws, total, flags = _norm_buffers(grads, bufs, ws, sumsq)
+    bufs, norm, total, _, ws, ws_at, flags = _scratch(grads, bufs, ws, sumsq)
     opt = AdamwOptions(lr, betas[0], betas[1], eps, weight_decay, max_norm, step,
                        flags | (CLIP_SKIP_NONFINITE if skip_nonfinite else 0), 0)
     _launch(grads.device, lib().aspis_clipped_adamw, tables[1], tables[0], tables[2], tables[3],
             tables[4] if copies is not None else None, grads.n_chunks, ctypes.byref(opt),
-            total.data_ptr(), bufs.norm.data_ptr(), ws.data_ptr(), ws.numel(),
-            _raw_stream(grads.device))
+            total, norm, ws_at, ws.numel(), _raw_stream(grads.device))
     del lists   # their tables were needed until here
     return bufs

@@ -176,10 +176,27 @@ def test_the_state_of_a_list_of_tensors():
             aspis._tensor_state(wrong)
 
 
+def test_the_native_checks_take_gpu_tensors_only():
+    """None sends the binding to the Python checks, which say what is wrong."""
+    import torch
+    t = torch.zeros(6)
+    native = aspis._tensors()
+    assert native.buffer(t, torch.float32, 6, 0) is None
+    assert native.buffer(None, torch.float32, 6, 0) is None
+    assert native.rows(t) is None and native.rows([t]) is None
+    for wrong in ((t,), (t, 0, 6, 0), (t, torch.float32, "6", 0), (t, torch.float32, 1 << 70, 0)):
+        with pytest.raises((TypeError, OverflowError)):
+            native.buffer(*wrong)
+    with pytest.raises(aspis.AspisError, match="norms"):
+        aspis._buffer("norms", t, torch.float32, 6, torch.device("cuda", 0))
+
+
 def test_missing_module_raises(monkeypatch):
     import sys
     import torch
-    monkeypatch.setattr(aspis, "_state", None)
+    monkeypatch.setattr(aspis, "_native", None)
+    import paper_2108_02416_amd
+    monkeypatch.delattr(paper_2108_02416_amd, "_tensors", raising=False)
     monkeypatch.setitem(sys.modules, "paper_2108_02416_amd._tensors", None)
     with pytest.raises(ImportError, match="_tensors.so is missing"):
         aspis.TensorList([], device=torch.device("cuda", 0))
