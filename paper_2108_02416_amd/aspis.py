@@ -628,6 +628,8 @@ class TensorList:
                                                   f"list on {self.device}")
         spans = sorted((p, p + k * t.element_size()) for p, k, t in zip(where, self.numels, ts) if k)
         self.disjoint = all(a[1] <= b[0] for a, b in zip(spans, spans[1:]))
+        ends = max((b for _, b in spans), default=0)
+        self.spans = np.array([*(x for s in spans for x in s), ends], dtype=np.uint64).tobytes()
         ptrs = np.array(where, dtype=np.uint64)
         numels = np.array(self.numels, dtype=np.int64)
         self.n_chunks = int(lib().aspis_tensor_chunks(numels.ctypes.data, n))
@@ -679,6 +681,11 @@ def _check_match(name: str, a: TensorList, ref: TensorList, same_types: bool = F
 def _check_written(name: str, a: TensorList):
     if not a.disjoint:
         raise AspisError(ERR_INVALID_ARG, f"{name} is written and lists overlapping tensors")
+
+
+def _check_apart(*lists: TensorList):
+    if not _tensors().apart(*[a.spans for a in lists]):
+        raise AspisError(ERR_INVALID_ARG, "the lists of a call overlap in memory")
 
 
 @dataclass
@@ -755,6 +762,8 @@ def clip_grads(grads, max_norm: float, out=None, sumsq=None, bufs: NormBuffers |
         out_table = out.table()
         _check_match("out", out, grads, same_types=True)
         _check_written("out", out)
+        if out._where != grads._where:   # each tensor onto itself is in place
+            _check_apart(grads, out)
     _launch(grads.device, lib().aspis_clip_grads, table, out_table, grads.n_chunks, max_norm,
             total, norm, flags, ws_at, ws.numel(), _raw_stream(grads.device))
     return bufs
@@ -856,6 +865,7 @@ def _update_lists(params, grads, states: dict, copies):
         tables.append(a.table())
         _check_match(name, a, grads, float32=name != "copies")
         _check_written(name, a)
+    _check_apart(grads, *lists.values())
     return lists, tables
 
 

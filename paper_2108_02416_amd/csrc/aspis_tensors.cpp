@@ -95,7 +95,56 @@ PyObject *rows(PyObject *, PyObject *arg) {
     }
 }
 
+// The spans of memory of a list's tensors that are not empty: their first and
+// past-the-end addresses in pairs, by the first, then the largest end.
+struct Spans {
+    const uint64_t *at;
+    Py_ssize_t n;
+    uint64_t first() const { return at[0]; }
+    uint64_t end() const { return at[2 * n]; }
+};
+
+// Whether no span of one list overlaps one of the other (spans of the same
+// list may): in order of their starts, none starts before the furthest end
+// so far of the other list.
+bool apart(const Spans &a, const Spans &b) {
+    if (a.n == 0 || b.n == 0 || a.end() <= b.first() || b.end() <= a.first()) return true;
+    uint64_t end_a = 0, end_b = 0;
+    for (Py_ssize_t i = 0, j = 0; i < a.n || j < b.n;) {
+        const bool from_a = j == b.n || (i < a.n && a.at[2 * i] <= b.at[2 * j]);
+        const uint64_t *span = from_a ? a.at + 2 * i++ : b.at + 2 * j++;
+        if (span[0] < (from_a ? end_b : end_a)) return false;
+        uint64_t &end = from_a ? end_a : end_b;
+        if (span[1] > end) end = span[1];
+    }
+    return true;
+}
+
+// apart(spans, spans, ...) -> whether the lists' tensors share no memory.
+PyObject *apart_py(PyObject *, PyObject *const *args, Py_ssize_t count) {
+    constexpr Py_ssize_t kMost = 8, kWord = sizeof(uint64_t);
+    Spans lists[kMost];
+    if (count > kMost) {
+        PyErr_SetString(PyExc_TypeError, "apart() takes up to 8 lists' spans");
+        return nullptr;
+    }
+    for (Py_ssize_t i = 0; i < count; ++i) {
+        if (!PyBytes_Check(args[i]) || PyBytes_GET_SIZE(args[i]) % (2 * kWord) != kWord) {
+            PyErr_SetString(PyExc_TypeError, "apart() takes spans as bytes");
+            return nullptr;
+        }
+        // (a bytes object's data is aligned to 8)
+        lists[i] = {reinterpret_cast<const uint64_t *>(PyBytes_AS_STRING(args[i])),
+                    PyBytes_GET_SIZE(args[i]) / (2 * kWord)};
+        for (Py_ssize_t j = 0; j < i; ++j)
+            if (!apart(lists[i], lists[j])) Py_RETURN_FALSE;
+    }
+    Py_RETURN_TRUE;
+}
+
 PyMethodDef methods[] = {
+    {"apart", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(apart_py)),
+     METH_FASTCALL, "Whether lists of spans share no memory."},
     {"rows", rows, METH_O, "Rows, length, distance and type code of a contiguous GPU tensor."},
     {"buffer", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(buffer)), METH_FASTCALL,
      "The address of a contiguous GPU tensor of a type and size, or None."},

@@ -176,6 +176,34 @@ def test_the_state_of_a_list_of_tensors():
             aspis._tensor_state(wrong)
 
 
+def test_lists_that_share_memory():
+    import itertools
+    import random
+    native = aspis._tensors()
+
+    def pack(spans):
+        spans = sorted(spans)
+        return np.array([*(x for s in spans for x in s), max((b for _, b in spans), default=0)],
+                        dtype=np.uint64).tobytes()
+    rng = random.Random(5)
+    seen = set()
+    for _ in range(3000):
+        room = rng.choice([20, 60, 400])
+        lists = []
+        for _ in range(rng.randint(1, 4)):
+            starts = [rng.randrange(room) for _ in range(rng.randint(0, 4))]
+            lists.append([(a, a + rng.randint(1, 9)) for a in starts])
+        want = all(x[1] <= y[0] or y[1] <= x[0] for p, q in itertools.combinations(lists, 2)
+                   for x in p for y in q)
+        assert native.apart(*map(pack, lists)) == want, lists
+        seen.add(want)
+    assert seen == {True, False}
+    assert native.apart()
+    for wrong in ((b"",), (b"0" * 16,), ([1],), (pack([]),) * 9):
+        with pytest.raises(TypeError):
+            native.apart(*wrong)
+
+
 def test_the_native_checks_take_gpu_tensors_only():
     """None sends the binding to the Python checks, which say what is wrong."""
     import torch

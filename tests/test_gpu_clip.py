@@ -769,3 +769,27 @@ def test_a_list_sees_a_type_or_layout_that_changes_in_place():
     norm = _norm64([t])
     aspis.clip_grads(handle, norm / 2, out=same)
     _assert_scaled(same[0], t, 0.5, "bfloat16")
+
+
+def test_lists_that_overlap_are_refused():
+    import torch
+    flat = _randn(4000, seed=6)
+    before = flat.clone()
+    g, shifted = flat[:2000], flat[1000:3000]
+    p, m, v = (_randn(2000, seed=7 + i).abs_() for i in range(3))
+    for call in (lambda: aspis.clip_grads([g], 1.0, out=[shifted]),
+                 lambda: aspis.clipped_sgd([p], [g], [p], lr=0.1, momentum=0.9),
+                 lambda: aspis.clipped_sgd([shifted], [g], [m], lr=0.1, momentum=0.9),
+                 lambda: aspis.clipped_adamw([p], [g], [m], [m], step=1, lr=0.1),
+                 lambda: aspis.clipped_adamw([p], [g], [m], [v], step=1, lr=0.1, copies=[p]),
+                 lambda: aspis.clipped_adamw([p], [g], [m], [v], step=1, lr=0.1,
+                                             copies=[shifted])):
+        with pytest.raises(aspis.AspisError, match="overlap"):
+            call()
+    assert bool((flat == before).all())
+    # onto itself, and next to each other
+    norm = _norm64([g])
+    aspis.clip_grads([g], norm / 2, out=[flat[:2000]])
+    _assert_scaled(g, before[:2000], 0.5, "float32")
+    aspis.clip_grads([flat[:1000]], 1e9, out=[flat[1000:2000]])
+    assert bool((flat[:1000] == flat[1000:2000]).all())
