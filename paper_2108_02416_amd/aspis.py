@@ -607,45 +607,51 @@ class TensorList:
         return len(self.tensors)
 
     def _read(self):
-        """Looks the tensors over and uploads their table."""
+        """Looks the tensors over and uploads their table.  The list takes
+        over what it read only when all of it is there: after a refusal or a
+        failed upload the next call reads again."""
         torch = _torch()
         ts = self.tensors
         n = len(ts)
-        self._where = _tensor_state(ts)
-        where, self.numels = [t.data_ptr() for t in ts], [t.numel() for t in ts]
-        self.dtypes = [t.dtype for t in ts]
-        codes = np.array([_dtype_code(d) for d in self.dtypes], dtype=np.int32)
-        self.contiguous = True
+        state = _tensor_state(ts)
+        self._where = None
+        where, numels = [t.data_ptr() for t in ts], [t.numel() for t in ts]
+        dtypes = [t.dtype for t in ts]
+        codes = np.array([_dtype_code(d) for d in dtypes], dtype=np.int32)
+        contiguous = True
         for i, t in enumerate(ts):
+            if t.device != self.device:
+                raise AspisError(ERR_INVALID_ARG, f"tensor {i} of the list is on {t.device}, the "
+                                                  f"list on {self.device}")
             if not t.is_contiguous():
-                self.contiguous = False
+                contiguous = False
                 if _layout(t) is None:
                     raise AspisError(ERR_INVALID_ARG,
                                      f"tensor {i} of the list has gaps or overlaps in memory: "
                                      f"shape {tuple(t.shape)}, strides {t.stride()}")
-            if t.device != self.device:
-                raise AspisError(ERR_INVALID_ARG, f"tensor {i} of the list is on {t.device}, the "
-                                                  f"list on {self.device}")
-        spans = sorted((p, p + k * t.element_size()) for p, k, t in zip(where, self.numels, ts) if k)
-        self.disjoint = all(a[1] <= b[0] for a, b in zip(spans, spans[1:]))
+        spans = sorted((p, p + k * t.element_size()) for p, k, t in zip(where, numels, ts) if k)
         ends = max((b for _, b in spans), default=0)
-        self.spans = np.array([*(x for s in spans for x in s), ends], dtype=np.uint64).tobytes()
         ptrs = np.array(where, dtype=np.uint64)
-        numels = np.array(self.numels, dtype=np.int64)
-        self.n_chunks = int(lib().aspis_tensor_chunks(numels.ctypes.data, n))
-        entries = int(lib().aspis_tensor_entries(numels.ctypes.data, n))
+        sizes = np.array(numels, dtype=np.int64)
+        n_chunks = int(lib().aspis_tensor_chunks(sizes.ctypes.data, n))
+        entries = int(lib().aspis_tensor_entries(sizes.ctypes.data, n))
         if entries < 0:
             raise AspisError(ERR_OVERFLOW, "too many elements in the list")
         host = np.empty((max(entries, 1), 2), dtype=np.int64)
-        _check(lib().aspis_tensor_table(ptrs.ctypes.data, numels.ctypes.data, codes.ctypes.data, n,
+        _check(lib().aspis_tensor_table(ptrs.ctypes.data, sizes.ctypes.data, codes.ctypes.data, n,
                                         host.ctypes.data, entries))
         # a copy from pageable memory returns when it is done: the table is
         # there for any stream
-        self._table = torch.from_numpy(host).to(self.device)
-        self._address = self._table.data_ptr()
+        table = torch.from_numpy(host).to(self.device)
+        self._table, self._address = table, table.data_ptr()
         self._stream = _raw_stream(self.device)
-        self.all_float32 = all(d == torch.float32 for d in self.dtypes)
-        self.ws_bytes = int(lib().aspis_norm_workspace(self.n_chunks))
+        self.numels, self.dtypes, self.contiguous = numels, dtypes, contiguous
+        self.disjoint = all(a[1] <= b[0] for a, b in zip(spans, spans[1:]))
+        self.spans = np.array([*(x for s in spans for x in s), ends], dtype=np.uint64).tobytes()
+        self.n_chunks = n_chunks
+        self.all_float32 = all(d == torch.float32 for d in dtypes)
+        self.ws_bytes = int(lib().aspis_norm_workspace(n_chunks))
+        self._where = state
 
     def layouts(self):
         return [_layout(t) for t in self.tensors]

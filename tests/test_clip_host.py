@@ -249,3 +249,69 @@ def test_host_code_under_sanitizers(tmp_path):
     assert out.returncode == 0, out.stdout + out.stderr
     assert out.stdout.strip().endswith("ok")
     assert "runtime error" not in out.stderr and "AddressSanitizer" not in out.stderr, out.stderr
+
+
+def _host_list(monkeypatch, tensors):
+    """A TensorList of host tensors: its reading without a GPU."""
+    import torch
+    monkeypatch.setattr(aspis, "_raw_stream", lambda device: 0)
+    handle = aspis.TensorList.__new__(aspis.TensorList)
+    handle.tensors, handle.device = list(tensors), torch.device("cpu")
+    handle._read()
+    return handle
+
+
+def _follows(handle):
+    """The table names the tensors as they are now."""
+    entries = handle._table.numpy().view(np.uint64)
+    assert handle.table() == handle._table.data_ptr()
+    sizes = [t.numel() for t in handle.tensors]
+    assert handle.numels == sizes and handle.n_chunks == sum(-(-n // 4096) for n in sizes)
+    starts = [int(entries[int(e[0]), 0]) for e in entries[handle.n_chunks:]]
+    assert starts == [t.data_ptr() for t in handle.tensors]
+
+
+def test_a_list_that_could_not_be_read_is_read_again(monkeypatch):
+    """Tensors that turn unusable are refused at every call until they are
+    usable again: never answered with the table of what they were."""
+    import torch
+    good = torch.zeros(600)
+    for wrong in (torch.zeros(600, dtype=torch.float64),           # type
+                  torch.zeros(1200)[::2],                          # gaps
+                  torch.zeros(1).expand(600),                      # overlaps
+                  torch.zeros(600, device="meta")):                # another device
+        t = torch.zeros(600)
+        t.data = good
+        handle = _host_list(monkeypatch, [t, torch.zeros(5)])
+        _follows(handle)
+        if wrong.device.type == "meta":
+            handle.tensors[0] = wrong
+        else:
+            t.data = wrong
+        for _ in range(3):
+            with pytest.raises((aspis.AspisError, RuntimeError)):
+                handle.table()
+        if wrong.device.type == "meta":
+            handle.tensors[0] = t
+        t.data = torch.zeros(200_000)
+        handle.table()
+        _follows(handle)
+
+
+def test_a_table_that_could_not_be_uploaded_is_uploaded_again(monkeypatch):
+    import torch
+    t = torch.zeros(10)
+    handle = _host_list(monkeypatch, [t])
+    address = handle.table()
+    t.data = torch.zeros(200_000)
+
+    def full(array):
+        raise torch.OutOfMemoryError("no memory for the table")
+    with monkeypatch.context() as m:
+        m.setattr(torch, "from_numpy", full)
+        for _ in range(2):
+            with pytest.raises(torch.OutOfMemoryError):
+                handle.table()
+            assert handle.n_chunks == 1 and handle._address == address
+    handle.table()
+    _follows(handle)
