@@ -697,7 +697,8 @@ def _check_apart(*lists: TensorList):
 @dataclass
 class NormBuffers:
     """What the norm of a list leaves on the device: norm float32 [1], sumsq
-    float64 [1] and, when asked for, each float32 [n] (every tensor's own)."""
+    float64 [1] (of a call by a given sum of squares: that one) and, when
+    asked for, each float32 [n] (every tensor's own)."""
     norm: object
     sumsq: object
     each: object = None
@@ -730,7 +731,10 @@ def _scratch(grads: TensorList, bufs, ws, sumsq, each: int = 0):
     each_at = _buffer("bufs.each", bufs.each, f32, each, dev) if each else None
     flags = 0
     if sumsq is not None:
-        total, flags = _buffer("sumsq", sumsq, f64, 1, dev), CLIP_HAVE_SUMSQ
+        # bufs holds the sum the call went by; given in bufs.sumsq it is there
+        if _buffer("sumsq", sumsq, f64, 1, dev) != total:
+            bufs.sumsq.view(-1)[:1].copy_(sumsq.view(-1)[:1])
+        flags = CLIP_HAVE_SUMSQ
     if ws is None:
         ws = torch.empty(grads.ws_bytes, dtype=torch.uint8, device=dev)
     ws_at = _buffer("ws", ws, torch.uint8, grads.ws_bytes, dev)
@@ -741,7 +745,8 @@ def grad_norm(grads, each: bool = False, bufs: NormBuffers | None = None, ws=Non
     """The global L2 norm of a list of tensors (aspis_grad_norm), with every
     tensor's own norm when `each`.  Nothing is synchronised: the results are
     on the device.  Where ranks hold shards of one model, all-reduce
-    bufs.sumsq and hand it to clip_grads or an update as sumsq."""
+    bufs.sumsq and hand it to clip_grads or an update as sumsq (with the same
+    bufs it is used where it is, otherwise copied)."""
     grads = _list(grads)
     table = grads.table()
     bufs, norm, total, each_at, ws, ws_at, _ = _scratch(grads, bufs, ws, None,

@@ -315,3 +315,22 @@ def test_a_table_that_could_not_be_uploaded_is_uploaded_again(monkeypatch):
             assert handle.n_chunks == 1 and handle._address == address
     handle.table()
     _follows(handle)
+
+
+def test_buffers_hold_the_sum_a_call_went_by(monkeypatch):
+    """A given sum of squares is what the call's buffers hold afterwards, new
+    ones and kept ones, and the given tensor stays the caller's."""
+    import types
+    import torch
+    monkeypatch.setattr(aspis, "_buffer", lambda name, t, dtype, n, device: t.data_ptr())
+    grads = types.SimpleNamespace(device=torch.device("cpu"), ws_bytes=64)
+    kept = aspis.NormBuffers.empty("cpu")
+    kept.sumsq.fill_(7.0)
+    for given in (torch.tensor([25.0], dtype=torch.float64), torch.tensor(36.0, dtype=torch.float64)):
+        for bufs in (None, kept):
+            got, _, total, _, _, _, flags = aspis._scratch(grads, bufs, None, given)
+            assert bufs is None or got is bufs
+            assert flags == aspis.CLIP_HAVE_SUMSQ and total == got.sumsq.data_ptr()
+            assert got.sumsq.tolist() == [float(given)] and got.sumsq.data_ptr() != given.data_ptr()
+    _, _, total, _, _, _, _ = aspis._scratch(grads, kept, None, kept.sumsq)
+    assert total == kept.sumsq.data_ptr() and kept.sumsq.tolist() == [36.0]

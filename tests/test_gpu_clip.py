@@ -793,3 +793,30 @@ def test_lists_that_overlap_are_refused():
     _assert_scaled(g, before[:2000], 0.5, "float32")
     aspis.clip_grads([flat[:1000]], 1e9, out=[flat[1000:2000]])
     assert bool((flat[:1000] == flat[1000:2000]).all())
+
+
+@pytest.mark.parametrize("sizes", [[], [900, 7], [300_001, 5]])
+@pytest.mark.parametrize("call", ["clip", "sgd", "adamw"])
+def test_the_sum_a_call_went_by_is_in_its_buffers(call, sizes):
+    """With new buffers, kept ones and the sum already there."""
+    import torch
+    dev = device()
+    as_list = lambda ts: aspis.TensorList(ts, device=dev)
+    g, p, m, v = (as_list(_views(sizes, seed=s)) if sizes else as_list([]) for s in range(4))
+    for t in v.tensors:
+        t.square_()
+    total = torch.tensor([6.25], dtype=torch.float64, device=dev)
+    kept = aspis.NormBuffers.empty(dev)
+    kept.sumsq.fill_(1e30)
+    there = aspis.NormBuffers(kept.norm.clone(), total.clone())
+    for bufs, given in ((None, total), (kept, total), (there, there.sumsq)):
+        keep = {"sumsq": given, "bufs": bufs}
+        if call == "clip":
+            got = aspis.clip_grads(g, 0.5, **keep)
+        elif call == "sgd":
+            got = aspis.clipped_sgd(p, g, m, lr=0.1, momentum=0.9, max_norm=0.5, **keep)
+        else:
+            got = aspis.clipped_adamw(p, g, m, v, step=1, lr=0.1, max_norm=0.5, **keep)
+        assert bufs is None or got is bufs
+        assert got.norm.tolist() == [2.5] and got.sumsq.tolist() == [6.25]
+        assert total.tolist() == [6.25]
