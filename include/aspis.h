@@ -465,7 +465,8 @@ aspis_status aspis_grad_norm(const aspis_chunk *table, int64_t n_chunks,
 #define ASPIS_CLIP_HAVE_SUMSQ 1u      /* sumsq holds the sum of squares (of
                                          all ranks): no norm pass          */
 #define ASPIS_CLIP_SKIP_NONFINITE 2u  /* updates: leave everything as it is
-                                         where the norm is not finite      */
+                                         where the norm written (an f32) is
+                                         not finite                        */
 #define ASPIS_CLIP_NO_WAIT 4u         /* rows: no workgroup waits for another
                                          inside a kernel                   */
 

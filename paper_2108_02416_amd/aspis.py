@@ -890,7 +890,8 @@ def clipped_sgd(params, grads, mean=None, *, lr: float, momentum: float = 0.0,
     (the momentum, needed unless it is 0) are lists of float32 tensors,
     copies a list that receives the new parameters rounded to its types.
     Returns the norm before clipping.  skip_nonfinite: a norm that is not
-    finite leaves parameters, state and copies as they are.
+    finite as the float32 it is returned in leaves parameters, state and
+    copies as they are.
 
     The update is not seen by autograd's version counters."""
     if momentum and mean is None:

@@ -323,6 +323,11 @@ __device__ __forceinline__ Coef coefficient(double sumsq, double max_norm) {
     return {m, e};
 }
 
+// Whether the norm as it is written down, in f32, is finite.
+__device__ __forceinline__ bool norm_is_finite(double sumsq) {
+    return (float)sqrt(sumsq) <= FLT_MAX;
+}
+
 // The global norm's sum, from the partial sums (every workgroup adds them
 // in the same order) or as given; workgroup 0 writes it down.
 template <int B>
@@ -602,7 +607,7 @@ __global__ __launch_bounds__(kUpdateBlock) void
 update_kernel(UpdateTables t, int64_t first, int64_t step, NormIn in, Rule rule, bool skip) {
     const double sumsq = *in.sumsq;
     if (blockIdx.x == 0 && threadIdx.x == 0) *in.norm = (float)sqrt(sumsq);
-    if (skip && !(sumsq <= DBL_MAX)) return;
+    if (skip && !norm_is_finite(sumsq)) return;
     const UpdateChunk<Rule> c(t, first + step * (blockIdx.x / kUpdateParts));
     const int i = ((int)(blockIdx.x % kUpdateParts) * kUpdateBlock + (int)threadIdx.x) * 4;
     typename UpdateChunk<Rule>::Four f;
@@ -624,7 +629,7 @@ wide_update_kernel(UpdateTables t, NormIn in, Rule rule, bool skip) {
 #pragma unroll
     for (int u = 0; u < N; ++u) c.load((u * kWideBlock + (int)threadIdx.x) * 4, f[u]);
     const double sumsq = take_sumsq<kWideBlock>(in);
-    if (skip && !(sumsq <= DBL_MAX)) return;
+    if (skip && !norm_is_finite(sumsq)) return;
     const Coef coef = coefficient(sumsq, in.max_norm);
 #pragma unroll
     for (int u = 0; u < N; ++u)
@@ -660,7 +665,7 @@ struct Update {
     double max_norm;
     bool skip;
     __device__ void operator()(int64_t k, int t, double sumsq) const {
-        if (skip && !(sumsq <= DBL_MAX)) return;
+        if (skip && !norm_is_finite(sumsq)) return;
         const Coef coef = coefficient(sumsq, max_norm);
         const UpdateChunk<Rule> c(tables, k);
         for (int i = t * 4; i < c.n; i += 4 * 256) {

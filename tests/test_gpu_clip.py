@@ -820,3 +820,31 @@ def test_the_sum_a_call_went_by_is_in_its_buffers(call, sizes):
         assert bufs is None or got is bufs
         assert got.norm.tolist() == [2.5] and got.sumsq.tolist() == [6.25]
         assert total.tolist() == [6.25]
+
+
+@pytest.mark.parametrize("rule,n", [("sgd", 4), ("sgd", 70_000), ("sgd", 34_000_001), ("adamw", 4),
+                                    ("adamw", 70_000), ("adamw", 12_000_003)])
+def test_an_update_is_skipped_where_the_norm_returned_is_not_finite(rule, n):
+    """Finite gradients whose norm passes the largest float32 are skipped,
+    the largest float32 itself as a norm is not: what is returned decides."""
+    import torch
+    dev = device()
+    top = float(np.finfo(np.float32).max)
+    g = torch.zeros(n, device=dev)
+    p, m, v = (torch.full((n,), x, device=dev) for x in (1.0, 0.5, 0.25))
+
+    def go():
+        if rule == "sgd":
+            return aspis.clipped_sgd([p], [g], [m], lr=1.0, momentum=0.5, max_norm=1.0,
+                                     skip_nonfinite=True)
+        return aspis.clipped_adamw([p], [g], [m], [v], step=1, lr=1.0, betas=(0.5, 0.5),
+                                   max_norm=1.0, skip_nonfinite=True)
+    g[0] = g[-1] = top
+    bufs = go()
+    assert float(bufs.norm) == math.inf and math.isfinite(float(bufs.sumsq))
+    assert bool((p == 1.0).all() and (m == 0.5).all() and (v == 0.25).all())
+    g[-1] = 0.0
+    bufs = go()
+    assert float(bufs.norm) == top
+    assert float(m[0]) == (1.25 if rule == "sgd" else 0.75)   # the clipped gradient is 1
+    assert bool((m[1:] == 0.25).all()) and not bool((p == 1.0).any())
