@@ -411,7 +411,9 @@ aspis_status aspis_detox(int32_t K, int32_t r, int32_t q, aspis_attack attack,
  * product c * x is rounded once to f32 and once more to a 16-bit result.
  * Results depend on the values and the sizes alone -- not on addresses,
  * alignment, strides or the device's number of compute units -- so that
- * workers clipping the same gradient upload the same bits.
+ * workers clipping the same gradient by the same call upload the same bits.
+ * A list's sum of squares has the same bits from every call that forms it,
+ * with and without `each`.
  *
  * All entry points below only enqueue work on the stream.  None allocates;
  * scratch comes through the caller's workspace, which needs no particular

@@ -8,7 +8,10 @@
 // square of any f32 fits, the sum needs no scaling pass, and the rate
 // (a conversion and an fma per element) stays above what memory delivers.
 // Every sum is split by sizes alone and joined in a fixed order, without
-// atomics, so equal inputs give equal bits wherever they lie.
+// atomics, so equal inputs give equal bits wherever they lie.  A list's order
+// is the same in every call, whichever kernels do it: a chunk's 256 threads,
+// a norm workgroup's chunks thread by thread, its lanes, its waves one after
+// the other, then the workgroups (block_sum_of).
 #include "aspis_clip.h"
 
 #include <atomic>
@@ -376,7 +379,7 @@ __device__ __forceinline__ double chunk_squares(const aspis_chunk &c, int t) {
 __global__ __launch_bounds__(kListBlock) void
 list_sumsq_kernel(const aspis_chunk *__restrict__ table, int64_t n_chunks, int group,
                   int64_t keep, double *partial, double *runs) {
-    double acc = 0.0, total = 0.0;
+    double total = 0.0, run = 0.0;
     int64_t first = (int64_t)blockIdx.x * group, k = first;
     aspis_chunk next = table[k];
     while (k < n_chunks) {
@@ -384,16 +387,18 @@ list_sumsq_kernel(const aspis_chunk *__restrict__ table, int64_t n_chunks, int g
         const int64_t now = k, now_first = first;
         if (++k == first + group || k >= n_chunks) k = first += (int64_t)gridDim.x * group;
         next = table[k < n_chunks ? k : now];
-        acc += now < keep ? chunk_squares<Use::Once>(c, threadIdx.x)
-                          : chunk_squares<Use::Again>(c, threadIdx.x);
-        if (runs != nullptr && (first != now_first || chunk_tensor(next) != chunk_tensor(c))) {
-            const double s = block_sum<kListBlock>(acc);
+        const double squares = now < keep ? chunk_squares<Use::Once>(c, threadIdx.x)
+                                          : chunk_squares<Use::Again>(c, threadIdx.x);
+        total += squares;
+        if (runs == nullptr) continue;
+        run += squares;
+        if (first != now_first || chunk_tensor(next) != chunk_tensor(c)) {
+            const double s = block_sum<kListBlock>(run);
             if (threadIdx.x == 0) runs[now_first / group + chunk_tensor(c)] = s;
-            total += s;
-            acc = 0.0;
+            run = 0.0;
         }
     }
-    if (runs == nullptr) total = block_sum<kListBlock>(acc);
+    total = block_sum<kListBlock>(total);
     if (threadIdx.x == 0) partial[blockIdx.x] = total;
 }
 
@@ -677,10 +682,11 @@ struct Update {
 };
 
 // Four groups of 256 threads take the chunks in turn: their sums (one per
-// wave), the norm, then what is applied to them.  Latency bounds it: of 7,850
+// wave), the norm (joined as list_sumsq_kernel and block_sum_of join a
+// workgroup per chunk), then what is applied to them.  Latency bounds it: of 7,850
 // elements in two tensors a norm takes 2.5 us, a clip 3.7, an SGD update 4.8.
 constexpr int kSoloBlock = 1024;
-static_assert(kSoloChunks * 4 == 64, "a wave holds all the waves' sums");
+static_assert(kSoloChunks == 16, "16 lanes hold the chunks' sums");
 
 template <typename Apply>
 __global__ __launch_bounds__(kSoloBlock) void
@@ -697,8 +703,9 @@ solo_kernel(const aspis_chunk *__restrict__ table, int n_chunks, const aspis_chu
             if (t % 64 == 0) sums[k * 4 + t / 64] = s;
         }
         __syncthreads();
-        const int lane = threadIdx.x % 64;
-        total = lanes_sum<64>(lane < n_chunks * 4 ? sums[lane] : 0.0);
+        const int k = threadIdx.x % kSoloChunks;
+        const double *of = sums + k * 4;
+        total = lanes_sum<kSoloChunks>(k < n_chunks ? of[0] + of[1] + of[2] + of[3] : 0.0);
         if (threadIdx.x == 0) *in.sumsq = total;
         if (each != nullptr)
             for (int i = threadIdx.x; i < n_tensors; i += kSoloBlock) {

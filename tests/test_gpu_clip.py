@@ -848,3 +848,29 @@ def test_an_update_is_skipped_where_the_norm_returned_is_not_finite(rule, n):
     assert float(bufs.norm) == top
     assert float(m[0]) == (1.25 if rule == "sgd" else 0.75)   # the clipped gradient is 1
     assert bool((m[1:] == 0.25).all()) and not bool((p == 1.0).any())
+
+
+@pytest.mark.parametrize("kind", ["float32", "bfloat16"])
+@pytest.mark.parametrize("chunks", [1, 2, 4, 5, 6, 8, 9, 12, 15, 16, 17, 40, 1025, 2768, 9001])
+def test_every_call_sums_a_list_alike(chunks, kind):
+    """The sum of squares has the same bits from the norm, with and without
+    the tensors' own norms, the clip and the updates, whether one workgroup
+    or many form it."""
+    n = chunks * 4096 - 7
+    part = 4096 * (chunks // 3)
+    sizes = [n] if chunks < 3 else [part, n - part - 4096, 4096]
+    ts = _views(sizes, kind, seed=chunks, offset=1)
+    for t, scale in zip(ts, (1.0, 3.0, 0.1)):
+        t.mul_(scale)
+    p, m, v = (_views(sizes, seed=s) for s in (1, 2, 3))
+    for t in v:
+        t.square_()
+    want = aspis.grad_norm(ts)
+    exact = sum(float(t.double().square().sum()) for t in ts)
+    assert abs(float(want.sumsq) - exact) <= 1e-12 * exact
+    for got in (aspis.grad_norm(ts, each=True),
+                aspis.clip_grads(ts, 1.0, out=[t.clone() for t in ts]),
+                aspis.clipped_sgd(p, ts, m, lr=0.1, momentum=0.9, max_norm=1.0),
+                aspis.clipped_adamw(p, ts, m, v, step=1, lr=0.1, max_norm=1.0),
+                aspis.clip_grads(ts, 1.0)):
+        assert float(got.sumsq) == float(want.sumsq) and float(got.norm) == float(want.norm)
