@@ -408,12 +408,7 @@ __global__ __launch_bounds__(kListBlock) void
 list_norm_kernel(const aspis_chunk *__restrict__ tensors, int group, NormIn in,
                  const double *__restrict__ runs, float *each) {
     if (blockIdx.x == 0) {
-        if (in.n_partial > 0) {
-            take_sumsq<kListBlock>(in);
-        } else if (threadIdx.x == 0) {   // an empty list
-            *in.sumsq = 0.0;
-            *in.norm = 0.0f;
-        }
+        take_sumsq<kListBlock>(in);
         return;
     }
     const aspis_chunk c = tensors[blockIdx.x - 1];
