@@ -874,3 +874,123 @@ def test_every_call_sums_a_list_alike(chunks, kind):
                 aspis.clipped_adamw(p, ts, m, v, step=1, lr=0.1, max_norm=1.0),
                 aspis.clip_grads(ts, 1.0)):
         assert float(got.sumsq) == float(want.sumsq) and float(got.norm) == float(want.norm)
+
+
+# ------------------------- lists on both sides of every switch, and past the
+# length from which they are walked from their end (16,384 chunks of 4,096)
+
+EDGE_CHUNKS = [3, 4, 5, 8, 9, 16, 17]
+PAST_THE_CACHE = 68_000_003
+
+
+def _uneven(n):
+    """Four tensors of n elements together, of very different sizes."""
+    return [n // 3, 5, n // 7, n - n // 3 - 5 - n // 7]
+
+
+def _of_chunks(chunks):
+    """Tensors that take so many chunks, none a whole number of them."""
+    return [4096 * (chunks - 2) - 7, 5, 4095] if chunks < 4 else \
+        [4096 * (chunks - 3) - 7, 5, 4095, 100]
+
+
+def _within(got, want, tol):
+    return bool(((got.double() - want).abs() <= tol + 1e-44).all())
+
+
+def _check_update_on_gpu(rule, sizes, kind, copy):
+    import torch
+    n, lr, wd = sum(sizes), 0.1, 0.01
+    grads = _views(sizes, kind, seed=1, offset=1)
+    params, mean = _views(sizes, seed=2, offset=2, scale=0.5), _views(sizes, seed=3, offset=3,
+                                                                      scale=0.003)
+    square = [v.square_() for v in _views(sizes, seed=4, offset=1, scale=0.003)]
+    copies = list(torch.full((n + 1,), 9.0, dtype=_type(copy), device=device())[1:].split(sizes))
+    norm = math.sqrt(sum(float(g.double().square().sum()) for g in grads))
+    start = [[t.clone() for t in x] for x in (params, mean, square)]
+    keep = {"lr": lr, "weight_decay": wd, "max_norm": 0.3 * norm, "copies": copies}
+    if rule == "sgd":
+        bufs = aspis.clipped_sgd(params, grads, mean, momentum=0.9, **keep)
+    elif rule == "plain":
+        bufs = aspis.clipped_sgd(params, grads, **keep)
+    else:
+        bufs = aspis.clipped_adamw(params, grads, mean, square, step=3, betas=(0.9, 0.95), **keep)
+    _assert_norm(bufs.norm, norm)
+    for i in range(len(sizes)):
+        g = 0.3 * grads[i].double()
+        p, m, v = (x[i].double() for x in start)
+        if rule == "adamw":
+            m_tol = 6 * U * (0.9 * m.abs() + 0.1 * g.abs())
+            m, v = 0.9 * m + 0.1 * g, 0.95 * v + 0.05 * g * g
+            rate, root = lr / (1 - 0.9 ** 3), (v / (1 - 0.95 ** 3)).sqrt() + 1e-8
+            p_tol = 4 * U * p.abs() + rate * (m_tol + 16 * U * m.abs()) / root
+            p = p * (1 - lr * wd) - rate * m / root
+            assert _within(square[i], v, 8 * U * v)
+            assert _within(mean[i], m, m_tol)
+        else:   # the roundings that _sgd64 counts
+            mu = 0.9 if rule == "sgd" else 0.0
+            g = g + wd * p
+            step = mu * m + g
+            size = (1 + mu) * (g.abs() + 2 * wd * p.abs() + 2 * mu * step.abs())
+            p_tol, p = 8 * U * (p.abs() + lr * size), p - lr * step
+            if mu:
+                assert _within(mean[i], step, 8 * U * size)
+        assert _within(params[i], p, p_tol)
+        assert bool((copies[i] == params[i].to(copies[i].dtype)).all())
+
+
+@pytest.mark.parametrize("chunks", EDGE_CHUNKS)
+@pytest.mark.parametrize("rule", ["sgd", "plain", "adamw"])
+@pytest.mark.parametrize("kind", ["float32", "bfloat16"])
+def test_updates_at_the_switches(rule, chunks, kind):
+    sizes = _of_chunks(chunks)
+    assert sum(-(-n // 4096) for n in sizes) == chunks
+    _check_update_on_gpu(rule, sizes, kind, "float16")
+
+
+@pytest.mark.parametrize("rule,n,kind", [("plain", 34_000_001, "float32"),
+                                         ("plain", 34_000_001, "float16"),
+                                         ("adamw", 11_000_003, "bfloat16"),
+                                         ("sgd", PAST_THE_CACHE, "float32"),
+                                         ("plain", PAST_THE_CACHE, "bfloat16"),
+                                         ("adamw", PAST_THE_CACHE, "float32"),
+                                         ("adamw", PAST_THE_CACHE, "float16")])
+def test_updates_of_lists_past_the_cache(rule, n, kind):
+    _check_update_on_gpu(rule, _uneven(n), kind, "bfloat16")
+
+
+def _check_clip_on_gpu(sizes, kind, where):
+    import torch
+    ts = _views(sizes, kind, seed=5, offset=1)
+    for t, scale in zip(ts, (1.0, 40.0, 3.0, 0.2)):
+        t.mul_(scale)
+    before = [t.clone() for t in ts]
+    squares = [float(t.double().square().sum()) for t in ts]
+    norm = math.sqrt(sum(squares))
+    each = aspis.grad_norm(ts, each=True).each.tolist()
+    for got, s in zip(each, squares):
+        _assert_norm(got, math.sqrt(s))
+    out = None if where == "in_place" else \
+        list(torch.full((sum(sizes) + 3,), 7.0, dtype=_type(kind),
+                        device=device())[3:].split(sizes))
+    _assert_norm(aspis.clip_grads(ts, 0.4 * norm, out=out).norm, norm)
+    for got, x in zip(ts if out is None else out, before):
+        want = 0.4 * x.double()
+        assert _within(got, want, want.abs() * (2 * U * (1 + 1e-6) + HALF_ULP[kind] * (1 + 1e-5))
+                       + 1.5 * TINY[kind])
+    if out is not None:
+        assert all(bool((t == b).all()) for t, b in zip(ts, before))
+
+
+@pytest.mark.parametrize("chunks", EDGE_CHUNKS)
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("where", ["in_place", "out"])
+def test_clips_at_the_switches(chunks, kind, where):
+    _check_clip_on_gpu(_of_chunks(chunks), kind, where)
+
+
+@pytest.mark.parametrize("n,kind", [(11_000_003, "float32"), (PAST_THE_CACHE, "float32"),
+                                    (PAST_THE_CACHE, "bfloat16"), (150_000_001, "float16")])
+@pytest.mark.parametrize("where", ["in_place", "out"])
+def test_clips_of_lists_past_the_cache(n, kind, where):
+    _check_clip_on_gpu(_uneven(n), kind, where)
