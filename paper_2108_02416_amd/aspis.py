@@ -545,6 +545,15 @@ def _launch(device, call, *args):
             _check(call(*args))
 
 
+def _capturing(device) -> bool:
+    """Whether the device's current stream is being captured into a graph."""
+    torch = _torch()
+    if device.type != "cuda":
+        return False
+    with torch.cuda.device(device):
+        return torch.cuda.is_current_stream_capturing()
+
+
 _native = None
 
 
@@ -586,7 +595,14 @@ class TensorList:
     its dimensions, no gaps).  The list holds the tensors and looks at every
     call whether they still are where they were, of the types and in the
     layouts they had, so that a tensor whose storage was replaced
-    (`t.data = ...`) is read as it is now."""
+    (`t.data = ...`) is read as it is now.
+
+    Making a list, or reading one again, uploads its table and waits for the
+    current stream, so that the table is there for every stream; it cannot be
+    done while a graph is captured.  A list that a call makes itself serves
+    the current stream alone and does not wait."""
+
+    _own_stream_only = False
 
     def __init__(self, tensors, device=None):
         torch = _torch()
@@ -637,12 +653,19 @@ class TensorList:
         entries = int(lib().aspis_tensor_entries(sizes.ctypes.data, n))
         if entries < 0:
             raise AspisError(ERR_OVERFLOW, "too many elements in the list")
+        if _capturing(self.device):
+            raise AspisError(ERR_INVALID_ARG, "a list's table cannot be uploaded while a graph is "
+                                              "captured: make a TensorList before, and keep its "
+                                              "tensors where they are")
         host = np.empty((max(entries, 1), 2), dtype=np.int64)
         _check(lib().aspis_tensor_table(ptrs.ctypes.data, sizes.ctypes.data, codes.ctypes.data, n,
                                         host.ctypes.data, entries))
-        # a copy from pageable memory returns when it is done: the table is
-        # there for any stream
-        table = torch.from_numpy(host).to(self.device)
+        # from pageable memory the copy returns when it is done; pinned memory
+        # is not given out again before the copy from it is done
+        table = torch.from_numpy(host)
+        if self._own_stream_only:
+            table = table.pin_memory()
+        table = table.to(self.device, non_blocking=self._own_stream_only)
         self._table, self._address = table, table.data_ptr()
         self._stream = _raw_stream(self.device)
         self.numels, self.dtypes, self.contiguous = numels, dtypes, contiguous
@@ -665,8 +688,13 @@ class TensorList:
         return self._address
 
 
+class _CallList(TensorList):
+    """A list made by a call, for the stream the call is on."""
+    _own_stream_only = True
+
+
 def _list(x) -> TensorList:
-    return x if isinstance(x, TensorList) else TensorList(x)
+    return x if isinstance(x, TensorList) else _CallList(x)
 
 
 def _check_match(name: str, a: TensorList, ref: TensorList, same_types: bool = False,

@@ -994,3 +994,65 @@ def test_clips_at_the_switches(chunks, kind, where):
 @pytest.mark.parametrize("where", ["in_place", "out"])
 def test_clips_of_lists_past_the_cache(n, kind, where):
     _check_clip_on_gpu(_uneven(n), kind, where)
+
+
+def test_calls_on_plain_sequences_do_not_wait():
+    """The host is back while the stream still works on what came before, and
+    the results are those of kept lists."""
+    import torch
+    dev = device()
+    sizes = [70_001, 5, 300]
+    a = torch.randn(8192, 8192, device=dev).bfloat16()
+    b = torch.empty_like(a)
+
+    def lists():
+        g, p, m, v = (_views(sizes, seed=s) for s in (1, 2, 3, 4))
+        for t in v:
+            t.square_()
+        return g, p, m, v
+
+    def go(wrap, g, p, m, v):
+        norm = aspis.grad_norm(wrap(g), each=True)
+        aspis.clipped_sgd(wrap(p), wrap(g), wrap(m), lr=0.1, momentum=0.9, max_norm=0.5)
+        aspis.clipped_adamw(wrap(p), wrap(g), wrap(m), wrap(v), step=2, lr=0.1, max_norm=0.5)
+        aspis.clip_grads(wrap(g), 0.25, out=wrap([t.clone() for t in g]))
+        aspis.clip_grads(wrap(g), 0.25)
+        return [norm.norm, norm.each, *g, *p, *m, *v]
+    want = go(aspis.TensorList, *lists())
+    go(list, *lists())   # memory for all of it is there
+    tensors = lists()
+    torch.cuda.synchronize()
+    for _ in range(300):   # some hundred milliseconds
+        torch.mm(a, a, out=b)
+    done = torch.cuda.Event()
+    done.record()
+    got = go(list, *tensors)
+    assert not done.query()
+    torch.cuda.synchronize()
+    assert all(np.array_equal(_bits(x), _bits(y)) for x, y in zip(got, want))
+
+
+def test_plain_sequences_are_refused_in_a_capture():
+    """... by a message, and the capture goes on; kept lists capture."""
+    import torch
+    dev = device()
+    x, y = _randn(5_000, seed=1), torch.empty(5_000, device=dev)
+    handle, out = aspis.TensorList([x]), aspis.TensorList([y])
+    bufs, ws = aspis.NormBuffers.empty(dev), aspis.norm_workspace(handle)
+    norm = _norm64([x])
+    aspis.clip_grads(handle, norm / 2, out=out, bufs=bufs, ws=ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for call in (lambda: aspis.grad_norm([x]), lambda: aspis.TensorList([x]),
+                     lambda: aspis.clip_grads(handle, 1.0, out=[y])):
+            with pytest.raises(aspis.AspisError, match="captured"):
+                call()
+        aspis.clip_grads(handle, norm / 2, out=out, bufs=bufs, ws=ws)
+    for replay in range(3):
+        x.copy_(_randn(5_000, seed=7 + replay))
+        y.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        _assert_norm(bufs.norm, _norm64([x]))
+        _assert_scaled(y, x, _coef64(_norm64([x]), norm / 2), "float32")
