@@ -198,6 +198,33 @@ __device__ __forceinline__ void add_squares(u32x4 w, double (&acc)[2]) {
     for (int j = 0; j < E::V; ++j) acc[j & 1] = add_square(x[j], acc[j & 1]);
 }
 
+// ---------------------------------------------------------------------------
+// the coefficient
+
+// c = m * 2^e with m in [1/2, 1), or m = c = 1, e = 0: x * m neither
+// overflows nor, for e = 0, loses bits, and c may be far below the smallest
+// f32 (a norm of 1e40 with a bound of 1).
+struct Coef {
+    float m;
+    int e;
+    __device__ float operator()(float x) const { return __builtin_amdgcn_ldexpf(x * m, e); }
+    __device__ bool one() const { return m == 1.0f; }
+};
+
+__device__ __forceinline__ Coef coefficient(double sumsq, double max_norm) {
+    const double norm = sqrt(sumsq);
+    if (norm <= max_norm || max_norm > DBL_MAX) return {1.0f, 0};
+    const double c = max_norm / norm;
+    int e = 0;
+    const float m = (float)frexp(c, &e);
+    // rounding may carry m to 1: the same value, one exponent up
+    if (m == 1.0f) return {0.5f, e + 1};
+    return {m, e};
+}
+
+// ---------------------------------------------------------------------------
+// elements in registers
+
 // n elements in the registers of L lanes: vectors lane, lane + L, ..., R at
 // most, and of the n % V elements after the last whole vector, elements lane,
 // lane + L, ...; zeros past the end.
@@ -214,7 +241,7 @@ struct Span {
     // with more vectors (24: the registers spill).
     static constexpr bool kShift = V == 8 && L >= 256 && R >= 2 && R <= 8;
     u32x4 w[R];
-    float tail[Q];
+    typename E::T tail[Q];
 
     template <Use USE>
     __device__ __forceinline__ void load(Ptr<E> p, int n, int lane) {
@@ -257,7 +284,7 @@ struct Span {
 #pragma unroll
         for (int q = 0; q < Q; ++q) {
             const int i = nv * V + lane + q * L;
-            tail[q] = i < n ? E::get(p[i]) : 0.0f;
+            tail[q] = i < n ? p[i] : typename E::T(0);
         }
     }
     // Adds the squares to two sums, vector after vector: spans one behind the
@@ -266,17 +293,19 @@ struct Span {
 #pragma unroll
         for (int r = 0; r < R; ++r) add_squares<E>(w[r], acc);
 #pragma unroll
-        for (int q = 0; q < Q; ++q) acc[q & 1] = add_square(tail[q], acc[q & 1]);
+        for (int q = 0; q < Q; ++q) acc[q & 1] = add_square(E::get(tail[q]), acc[q & 1]);
     }
     __device__ __forceinline__ double squares() const {
         double acc[2] = {0.0, 0.0};
         squares(acc);
         return acc[0] + acc[1];
     }
-    // Writes c times the elements; o may be where they came from.
-    template <Use USE, typename C>
-    __device__ __forceinline__ void store(MutPtr<E> o, int n, int lane, C c) const {
+    // Writes c times the elements, their own bits for c = 1 (a product would
+    // turn a signalling NaN into a quiet one); o may be where they came from.
+    template <Use USE>
+    __device__ __forceinline__ void store(MutPtr<E> o, int n, int lane, Coef c) const {
         const int nv = n / V;
+        const bool same = c.one();
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             if (n != R * L * V && lane + r * L >= nv) continue;
@@ -284,17 +313,20 @@ struct Span {
             // take twice the registers
             u32x4 v = w[r];
             if constexpr (V == 8) asm volatile("" : "+v"(v));
-            float x[V];
-            E::unpack(v, x);
+            if (!same) {
+                float x[V];
+                E::unpack(v, x);
 #pragma unroll
-            for (int j = 0; j < V; ++j) x[j] = c(x[j]);
-            store_vec<E, USE>(o + (lane + r * L) * V, E::pack(x));
+                for (int j = 0; j < V; ++j) x[j] = c(x[j]);
+                v = E::pack(x);
+            }
+            store_vec<E, USE>(o + (lane + r * L) * V, v);
         }
         if (n == R * L * V) return;
 #pragma unroll
         for (int q = 0; q < Q; ++q) {
             const int i = nv * V + lane + q * L;
-            if (i < n) o[i] = E::put(c(tail[q]));
+            if (i < n) o[i] = same ? tail[q] : E::put(c(E::get(tail[q])));
         }
     }
 };
@@ -303,28 +335,7 @@ template <typename E>
 using Tile = Span<E, 256, kChunk / E::V / 256>;
 
 // ---------------------------------------------------------------------------
-// the coefficient
-
-// c = m * 2^e with m in [1/2, 1), or m = c = 1, e = 0: x * m neither
-// overflows nor, for e = 0, loses bits, and c may be far below the smallest
-// f32 (a norm of 1e40 with a bound of 1).
-struct Coef {
-    float m;
-    int e;
-    __device__ float operator()(float x) const { return __builtin_amdgcn_ldexpf(x * m, e); }
-    __device__ bool one() const { return m == 1.0f; }
-};
-
-__device__ __forceinline__ Coef coefficient(double sumsq, double max_norm) {
-    const double norm = sqrt(sumsq);
-    if (norm <= max_norm || max_norm > DBL_MAX) return {1.0f, 0};
-    const double c = max_norm / norm;
-    int e = 0;
-    const float m = (float)frexp(c, &e);
-    // rounding may carry m to 1: the same value, one exponent up
-    if (m == 1.0f) return {0.5f, e + 1};
-    return {m, e};
-}
+// the global norm
 
 // Whether the norm as it is written down, in f32, is finite.
 __device__ __forceinline__ bool norm_is_finite(double sumsq) {

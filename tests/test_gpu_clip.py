@@ -1056,3 +1056,39 @@ def test_plain_sequences_are_refused_in_a_capture():
         torch.cuda.synchronize()
         _assert_norm(bufs.norm, _norm64([x]))
         _assert_scaled(y, x, _coef64(_norm64([x]), norm / 2), "float32")
+
+
+SIGNALLING = {"float32": 0x7F800001, "bfloat16": 0x7F81, "float16": 0x7C01}
+
+
+def _with_signalling_nans(x, kind):
+    """x with signalling NaNs in places of a 16-byte load and of a tail."""
+    import torch
+    ints = x.view(torch.int32 if kind == "float32" else torch.int16)
+    for row in ints.reshape(-1, x.shape[-1]):
+        for i in {0, row.numel() // 2, row.numel() - 1}:
+            row[i] = SIGNALLING[kind]
+    return x
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("n", [1, 7, 4_095, 70_001, 40_000_003])
+@pytest.mark.parametrize("offset", [0, 1])
+def test_no_bound_returns_a_lists_own_bits(n, kind, offset):
+    import torch
+    x = _with_signalling_nans(_randn(n + offset, kind, seed=n)[offset:], kind)
+    out = torch.zeros_like(x)
+    aspis.clip_grads([x], math.inf, out=[out])
+    assert np.array_equal(_bits(out), _bits(x))
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("rows,d", [(70, 3), (70, 50), (9, 300), (5, 1_001), (5, 10_007), (3, 32_767),
+                                    (3, 50_001), (2, 100_003), (40, 300_001), (3, 7_000_001),
+                                    (1, 25_000_003)])
+def test_no_bound_returns_the_rows_own_bits(rows, d, kind):
+    import torch
+    x = _with_signalling_nans(_randn(rows * d + 1, kind, seed=d)[1:].reshape(rows, d), kind)
+    for flags in (0, aspis.CLIP_NO_WAIT):
+        out, _ = aspis.clip_rows(x, math.inf, out=torch.zeros_like(x), flags=flags)
+        assert np.array_equal(_bits(out), _bits(x))
