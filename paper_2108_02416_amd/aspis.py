@@ -676,9 +676,6 @@ class TensorList:
         self.ws_bytes = int(lib().aspis_norm_workspace(n_chunks))
         self._where = state
 
-    def layouts(self):
-        return [_layout(t) for t in self.tensors]
-
     def table(self) -> int:
         """Device address of the table, brought up to date."""
         if _tensor_state(self.tensors) != self._where:
@@ -703,9 +700,11 @@ def _check_match(name: str, a: TensorList, ref: TensorList, same_types: bool = F
     if a.numels != ref.numels or a.device != ref.device:
         raise AspisError(ERR_INVALID_ARG, f"{name} must list tensors of the gradients' sizes, in "
                                           f"their order, on their device")
-    if not (a.contiguous and ref.contiguous) and a.layouts() != ref.layouts():
-        raise AspisError(ERR_INVALID_ARG, f"{name}: tensors that are not contiguous must have the "
-                                          f"gradients' shapes and strides")
+    if not (a.contiguous and ref.contiguous):
+        for x, y in zip(a.tensors, ref.tensors):
+            if not (x.is_contiguous() and y.is_contiguous()) and _layout(x) != _layout(y):
+                raise AspisError(ERR_INVALID_ARG, f"{name}: tensors that are not contiguous must "
+                                                  f"have the gradients' shapes and strides")
     if same_types and a.dtypes != ref.dtypes:
         raise AspisError(ERR_INVALID_ARG, f"{name} must have the gradients' types")
     if float32 and not a.all_float32:

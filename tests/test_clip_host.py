@@ -334,3 +334,20 @@ def test_buffers_hold_the_sum_a_call_went_by(monkeypatch):
             assert got.sumsq.tolist() == [float(given)] and got.sumsq.data_ptr() != given.data_ptr()
     _, _, total, _, _, _, _ = aspis._scratch(grads, kept, None, kept.sumsq)
     assert total == kept.sumsq.data_ptr() and kept.sumsq.tolist() == [36.0]
+
+
+def test_lists_match_tensor_by_tensor(monkeypatch):
+    """A contiguous tensor may have any shape, whatever its neighbours are;
+    one that is not has to have the gradient's shape and strides."""
+    import torch
+    make = lambda *ts: _host_list(monkeypatch, ts)
+    turned = lambda: torch.zeros(3, 5).t()
+    grads = make(turned(), torch.zeros(12))
+    aspis._check_match("params", make(turned(), torch.zeros(3, 4)), grads)
+    aspis._check_match("params", make(torch.zeros(15), torch.zeros(3, 4)),
+                       make(torch.zeros(5, 3), torch.zeros(12)))
+    for wrong in (make(torch.zeros(5, 3), torch.zeros(12)), make(torch.zeros(15), torch.zeros(12)),
+                  make(turned(), torch.zeros(4, 3).t()), make(torch.zeros(5, 3).t(), torch.zeros(12))):
+        for a, b in ((wrong, grads), (grads, wrong)):
+            with pytest.raises(aspis.AspisError, match="not contiguous"):
+                aspis._check_match("params", a, b)
