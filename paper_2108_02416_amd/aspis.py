@@ -778,6 +778,8 @@ def grad_norm(grads, each: bool = False, bufs: NormBuffers | None = None, ws=Non
     table = grads.table()
     bufs, norm, total, each_at, ws, ws_at, _ = _scratch(grads, bufs, ws, None,
                                                         len(grads) if each else 0)
+    if each and bufs.each is None:   # no tensors
+        bufs.each = _torch().empty(0, dtype=_torch().float32, device=grads.device)
     _launch(grads.device, lib().aspis_grad_norm, table, grads.n_chunks, len(grads), total,
             norm, each_at, ws_at, ws.numel(), _raw_stream(grads.device))
     return bufs

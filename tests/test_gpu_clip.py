@@ -1092,3 +1092,13 @@ def test_no_bound_returns_the_rows_own_bits(rows, d, kind):
     for flags in (0, aspis.CLIP_NO_WAIT):
         out, _ = aspis.clip_rows(x, math.inf, out=torch.zeros_like(x), flags=flags)
         assert np.array_equal(_bits(out), _bits(x))
+
+
+def test_the_norms_of_no_tensors_are_an_empty_tensor():
+    import torch
+    none = aspis.TensorList([], device=device())
+    for bufs in (None, aspis.NormBuffers.empty(device(), each=len(none))):
+        got = aspis.grad_norm(none, each=True, bufs=bufs)
+        assert got.each.dtype == torch.float32 and got.each.shape == (0,)
+        assert float(got.norm) == 0.0
+    assert aspis.grad_norm(none).each is None
