@@ -1102,3 +1102,48 @@ def test_the_norms_of_no_tensors_are_an_empty_tensor():
         assert got.each.dtype == torch.float32 and got.each.shape == (0,)
         assert float(got.norm) == 0.0
     assert aspis.grad_norm(none).each is None
+
+
+def test_adamw_by_a_given_sum_in_a_graph():
+    """What a call took by value is what every replay goes by (the step, and
+    so the bias correction); what it took on the device is read anew (the
+    gradients, the sum of squares)."""
+    import torch
+    dev, sizes, step = device(), [70_001, 513], 5
+    grads = aspis.TensorList(_views(sizes, "bfloat16", seed=1))
+    params, mean, square = (aspis.TensorList(_views(sizes, seed=s)) for s in (2, 3, 4))
+    for t in square.tensors:
+        t.square_()
+    copies = aspis.TensorList([torch.empty(n, dtype=torch.bfloat16, device=dev) for n in sizes])
+    bufs, ws = aspis.NormBuffers.empty(dev), aspis.norm_workspace(grads)
+    total = torch.ones(1, dtype=torch.float64, device=dev)
+
+    def go():
+        aspis.clipped_adamw(params, grads, mean, square, step=step, lr=0.1, max_norm=0.5,
+                            copies=copies, sumsq=total, bufs=bufs, ws=ws)
+    state = [t for x in (params, mean, square, copies) for t in x.tensors]
+    start = [t.clone() for t in state]
+
+    def reset():
+        for t, k in zip(state, start):
+            t.copy_(k)
+    go()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        go()
+    for replay in range(4):
+        reset()
+        for i, t in enumerate(grads.tensors):
+            t.copy_(_randn(t.numel(), "bfloat16", seed=50 + 7 * replay + i))
+        total.fill_(2.0 + replay)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in state] + [bufs.norm.clone(), bufs.sumsq.clone().float()]
+        reset()
+        go()
+        torch.cuda.synchronize()
+        want = state + [bufs.norm, bufs.sumsq.float()]
+        assert all(np.array_equal(_bits(a), _bits(b)) for a, b in zip(got, want)), replay
+        assert bufs.sumsq.tolist() == [2.0 + replay]
