@@ -407,8 +407,10 @@ aspis_status aspis_detox(int32_t K, int32_t r, int32_t q, aspis_attack attack,
  * An infinite norm gives c = 0 (finite elements become 0, infinite ones
  * NaN), a NaN norm c = NaN.  c = 1 returns every element's own bits.
  *
- * Sums of squares are held in fp64 (the square of every f32 fits), and the
- * product c * x is rounded once to f32 and once more to a 16-bit result.
+ * Sums of squares are held in fp64 (the square of every f32 fits).  c is
+ * rounded to 24 bits of mantissa (its exponent may lie below f32's), the
+ * product c * x to f32, once more where that is subnormal, and once more to a
+ * 16-bit result.
  * Results depend on the values and the sizes alone -- not on addresses,
  * alignment, strides or the device's number of compute units -- so that
  * workers clipping the same gradient by the same call upload the same bits.
@@ -417,7 +419,12 @@ aspis_status aspis_detox(int32_t K, int32_t r, int32_t q, aspis_attack attack,
  *
  * All entry points below only enqueue work on the stream.  None allocates;
  * scratch comes through the caller's workspace, which needs no particular
- * contents.  Calls that overlap must not share workspaces or outputs. */
+ * contents.  Calls that overlap must not share workspaces or outputs.
+ *
+ * Bounds and options are taken by value when the call is made: a graph that
+ * captured a call replays it with the bound, rates and step it had (AdamW's
+ * bias correction among them), on what the tensors, sumsq and the tables'
+ * memory then hold. */
 typedef enum { ASPIS_F32 = 0, ASPIS_BF16 = 1, ASPIS_F16 = 2 } aspis_dtype;
 
 /* A list of tensors, as the kernels read it: an array of aspis_chunk that
@@ -514,11 +521,12 @@ aspis_status aspis_clip_rows(const void *x, int64_t rows, int64_t d, int64_t ld,
  *          square = beta2 * square + (1 - beta2) * g * g;
  *          p -= lr / (1 - beta1^step) * mean
  *               / (sqrt(square / (1 - beta2^step)) + eps)
- * in f32.  params, mean and square are tables of f32 tensors, grads of any
- * types; copies, when not NULL, lists tensors of any type that receive the
- * new parameters, rounded (a model's low-precision weights).  All tables
- * list tensors of the same sizes in the same order, and all tensors written
- * are disjoint from the others.  SGD's mean may be NULL when momentum is 0.
+ * in f32, with the constants of a step rounded to f32 once.  params, mean and
+ * square are tables of f32 tensors, grads of any types; copies, when not
+ * NULL, lists tensors of any type that receive the new parameters, rounded (a
+ * model's low-precision weights).  All tables list tensors of the same sizes
+ * in the same order, and all tensors written are disjoint from the others.
+ * SGD's mean may be NULL when momentum is 0.
  * sumsq, norm, flags, workspace: as aspis_clip_grads. */
 typedef struct {
     double lr, momentum, weight_decay, max_norm;

@@ -595,12 +595,18 @@ class TensorList:
     its dimensions, no gaps).  The list holds the tensors and looks at every
     call whether they still are where they were, of the types and in the
     layouts they had, so that a tensor whose storage was replaced
-    (`t.data = ...`) is read as it is now.
+    (`t.data = ...`) is read as it is now.  It does not see other tensors that
+    take their place: where gradients are new objects every step (`p.grad`
+    after `zero_grad()`, which drops them by default), zero them in place
+    (`zero_grad(set_to_none=False)`) or hand each call the new sequence.
 
     Making a list, or reading one again, uploads its table and waits for the
     current stream, so that the table is there for every stream; it cannot be
     done while a graph is captured.  A list that a call makes itself serves
-    the current stream alone and does not wait."""
+    the current stream alone and does not wait.
+
+    A graph that captured a call reads the table the list had then: keep the
+    list and its tensors where they are for as long as it is replayed."""
 
     _own_stream_only = False
 
@@ -770,8 +776,8 @@ def _scratch(grads: TensorList, bufs, ws, sumsq, each: int = 0):
 
 def grad_norm(grads, each: bool = False, bufs: NormBuffers | None = None, ws=None) -> NormBuffers:
     """The global L2 norm of a list of tensors (aspis_grad_norm), with every
-    tensor's own norm when `each`.  Nothing is synchronised: the results are
-    on the device.  Where ranks hold shards of one model, all-reduce
+    tensor's own norm when `each`.  Nothing is synchronised, whether `grads`
+    is a kept list or any sequence: the results are on the device.  Where ranks hold shards of one model, all-reduce
     bufs.sumsq and hand it to clip_grads or an update as sumsq (with the same
     bufs it is used where it is, otherwise copied)."""
     grads = _list(grads)
@@ -790,7 +796,10 @@ def clip_grads(grads, max_norm: float, out=None, sumsq=None, bufs: NormBuffers |
     """Scales a list of tensors so that its global norm is at most max_norm
     (aspis_clip_grads): in place, or into the tensors of `out`.  Returns the
     norm before clipping.  sumsq: the sum of squares to clip by (of all
-    ranks), instead of this list's own."""
+    ranks), instead of this list's own.
+
+    Autograd does not see it: results carry no graph, and writing in place
+    does not count in the tensors' versions."""
     grads = _list(grads)
     table = grads.table()
     bufs, norm, total, _, ws, ws_at, flags = _scratch(grads, bufs, ws, sumsq)
@@ -866,7 +875,7 @@ def _row_buffers(x, rows: int, d: int, code: int, norms, ws):
 
 def row_norms(x, norms=None, ws=None):
     """The L2 norm of every row of x [..., d] (aspis_row_norms): the replicas
-    [f][r][d] or a worker's upload [l][d]."""
+    [f][r][d] or a worker's upload [l][d].  Results carry no autograd graph."""
     rows, d, ld, code = _rows("x", x)
     norms, norms_at, ws, ws_at = _row_buffers(x, rows, d, code, norms, ws)
     _launch(x.device, lib().aspis_row_norms, x.data_ptr(), rows, d, ld, code, norms_at, ws_at,
@@ -878,8 +887,9 @@ def clip_rows(x, max_norm: float, out=None, norms=None, ws=None, flags: int = 0)
     """Scales every row of x [..., d] whose norm is above max_norm down to it
     (aspis_clip_rows): in place, or into `out`.  Returns (out, the norms before
     clipping).  Replicas with equal bits are equal after it, so a server may
-    clip them before detection and workers before they upload.  flags may
-    hold CLIP_NO_WAIT."""
+    clip them before detection (of float32 replicas) and workers before they
+    upload.  flags may hold CLIP_NO_WAIT.  Autograd does not see it, as with
+    clip_grads."""
     rows, d, ld, code = _rows("x", x)
     out = x if out is None else out
     ldo = ld
@@ -944,7 +954,10 @@ def clipped_adamw(params, grads, mean, square, *, step: int, lr: float, betas=(0
                   skip_nonfinite: bool = False, bufs: NormBuffers | None = None,
                   ws=None) -> NormBuffers:
     """One AdamW update in place, by the gradients clipped to max_norm
-    (aspis_clipped_adamw); as clipped_sgd otherwise.  step counts from 1."""
+    (aspis_clipped_adamw); as clipped_sgd otherwise.  step counts from 1.
+
+    step, lr and the other numbers are taken when the call is made: a graph
+    that captured it replays the update of that step."""
     grads = _list(grads)
     lists, tables = _update_lists(params, grads, {"mean": mean, "square": square}, copies)
     bufs, norm, total, _, ws, ws_at, flags = _scratch(grads, bufs, ws, sumsq)

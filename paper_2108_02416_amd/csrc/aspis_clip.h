@@ -24,9 +24,11 @@ constexpr int64_t kMaxRow = int64_t(1) << 34;       // elements of a row: one la
 // Workgroups of the norm pass over a list, at most, and so its partial sums:
 // a function of the list alone, since the order of the sum follows it.
 constexpr int kNormGroups = 1024;
-// Lists of up to so many chunks are one workgroup's work: a norm of 16 chunks
-// takes 6.6 us (several workgroups and two launches 10.0), a clip of 8 7.6 us
-// (10.8; of 16 11.0 and 10.7), an AdamW update of 4 10.2 us (16.0 with three launches).
+// Lists of up to so many chunks are one workgroup's work, longer ones several
+// workgroups' in two launches.  Both ways in us, the call included: a norm of
+// 16 chunks 5.4 and 7.9; a clip of 8 7.3 and 8.7, of 12 9.6 and 8.7; an AdamW
+// update of 4 9.4 and 10.8, of 5 11.2 and 10.8 (SGD: of 4 7.4 and 10.2, of 6
+// 9.0 and 10.3, of 8 10.5 and 10.3).
 constexpr int kSoloChunks = 16, kSoloClip = 8, kSoloUpdate = 4;
 // The workspace of a list, in doubles: the partial sums, then the sums of
 // runs of chunks for the tensors' own norms.

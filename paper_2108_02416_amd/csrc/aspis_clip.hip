@@ -384,7 +384,8 @@ __device__ __forceinline__ double chunk_squares(const aspis_chunk &c, int t) {
 // receives the sum of every run of one tensor's chunks in a group, at the
 // group's index plus the tensor's: of two runs one after the other at least
 // one index is one up, so no two share a place.
-// Memory bounds it: 871M mixed elements (1.74 GB) in 257 us, 6.8 TB/s, with
+// Memory bounds it: 871M mixed elements (1.74 GB) in 257 to 264 us, 6.6 to
+// 6.8 TB/s of the 7.1 that a linear read reaches, with
 // all of a chunk's 16-byte loads in flight before the first square and the
 // next chunk's entry already there; each byte is read once.
 __global__ __launch_bounds__(kListBlock) void
@@ -434,7 +435,7 @@ list_norm_kernel(const aspis_chunk *__restrict__ tensors, int group, NormIn in,
 // One chunk per workgroup, the last first where the list is longer than
 // what the cache keeps of it.  The chunk is on its way while the
 // coefficient is worked out, unless that may make it unnecessary.
-// Memory bounds it: 871M mixed elements read and written in 553 us, 6.3 TB/s
+// Memory bounds it: 871M mixed elements read and written in 553 to 560 us, 6.3 TB/s
 // (what the norm pass left in the last-level cache included).
 __global__ __launch_bounds__(kListBlock) void
 list_scale_kernel(const aspis_chunk *__restrict__ table, const aspis_chunk *__restrict__ out,
@@ -609,7 +610,8 @@ struct UpdateChunk {
 // Long lists: one wave and four elements a lane, so that the memory system
 // sees each tensor's lines in order, 1 KB at a time.  The sum is joined
 // before.  Memory bounds it: AdamW on 871M parameters with bf16 gradients
-// and copy moves 24.4 GB in 4.01 ms, 6.1 TB/s, each byte once.
+// and copy moves 24.4 GB in 3.72 to 4.01 ms by where the tensors lie, 6.1 to
+// 6.5 TB/s, each byte once.
 constexpr int kUpdateBlock = 64;
 constexpr int kUpdateParts = kChunk / (4 * kUpdateBlock);
 
@@ -628,7 +630,7 @@ update_kernel(UpdateTables t, int64_t first, int64_t step, NormIn in, Rule rule,
 
 // Shorter ones: a chunk per workgroup, on its way while the workgroup joins
 // the partial sums; one launch less.  SGD with momentum on 11.2M f32 moves
-// 223 MB in 33.9 us, 6.6 TB/s, the gradients coming from the cache.
+// 223 MB in 32 to 34 us, 6.6 to 7.0 TB/s, the gradients coming from the cache.
 constexpr int kWideBlock = 512;
 
 template <typename Rule>
@@ -690,7 +692,7 @@ struct Update {
 // Four groups of 256 threads take the chunks in turn: their sums (one per
 // wave), the norm (joined as list_sumsq_kernel and block_sum_of join a
 // workgroup per chunk), then what is applied to them.  Latency bounds it: of 7,850
-// elements in two tensors a norm takes 2.5 us, a clip 3.7, an SGD update 4.8.
+// elements in two tensors a norm takes 2.1 us, a clip 3.4, an SGD update 4.6.
 constexpr int kSoloBlock = 1024;
 static_assert(kSoloChunks == 16, "16 lanes hold the chunks' sums");
 
@@ -730,8 +732,8 @@ solo_kernel(const aspis_chunk *__restrict__ table, int n_chunks, const aspis_chu
 
 // A row in the registers of L lanes, R vectors each: read once, its norm,
 // written once.  L <= 64: B / L rows per workgroup; L == B: one.  Memory
-// bounds it: 6,900 rows of 10,007 f16 in 48.2 us, 5.7 TB/s; few rows are
-// latency (15 of 7,850 f32: 3.7 us).
+// bounds it: 6,900 rows of 10,007 f16 in 47.2 us, 5.9 TB/s; few rows are
+// latency (15 of 7,850 f32: 3.5 us).
 template <typename E, int L, int B, int R>
 __global__ __launch_bounds__(B) void row_kernel(RowArgs a) {
     constexpr int G = B / L;
@@ -765,8 +767,10 @@ __global__ __launch_bounds__(kListBlock) void empty_rows_kernel(float *norms, in
 // part_kernel: a part stays in the registers of a workgroup, R vectors a
 // thread, which publishes its sum of squares, waits for the row's total and
 // writes its part, so the row crosses the memory bus once each way: 91 rows
-// of 11.2M f32 in 1.50 ms, 5.4 TB/s, as fast as a copy (segment_kernel, which
-// reads them twice: 2.15 ms).
+// of 11.2M f32 in 1.50 ms, 5.4 TB/s (segment_kernel, which reads them twice:
+// 2.15 ms).  The device holds two such rows at a time, and a row's workgroups
+// load, wait and store together; update_kernel, which waits for nothing, moves
+// up to 6.5 TB/s.
 //
 // A sum is published as one 64-bit word that is never kUnset (a NaN that
 // came from f32 or f16 has zeros in its low bits), so a reader needs no
@@ -1050,7 +1054,9 @@ hipError_t rows_of(const RowArgs &a, hipStream_t s) {
 // kept 87.6, with 320 MB 86.2.
 constexpr int64_t kKeepChunks = (int64_t)256 * 1024 * 1024 / (4 * kChunk);
 // From here on the partial sums are joined by a launch of their own; below,
-// by every workgroup that scales a chunk.
+// by every workgroup that scales a chunk.  Joined apart and by every workgroup,
+// us: a clip of 3,500 chunks 27.4 and 26.2, of 8,000 60.6 both ways; SGD of 5,000
+// 75.7 and 75.4, of 9,000 131 and 133, of 16,000 226 and 237.
 constexpr int64_t kJoinChunks = 8192;
 
 // Chunks of one launch that takes them all: its threads stay below 2^32.
@@ -1108,8 +1114,9 @@ hipError_t update_list(const UpdateTables &t, int64_t n_chunks, bool have_sumsq,
     if (n_chunks <= kSoloUpdate)
         return start_solo(t.grads, n_chunks, 0, have_sumsq, in, nullptr,
                           Update<Rule>{t, rule, in.max_norm, skip}, s);
-    // AdamW's seven streams gain from update_kernel's order earlier (11.2M
-    // elements: 59.4 against 61.3 us; SGD's five 46.1 against 45.1)
+    // AdamW's seven streams gain from update_kernel's order earlier: joined
+    // apart and by every workgroup, 2,000 chunks take 45.9 and 42.5 us, 2,700
+    // 59.7 and 60.6, 3,500 72.6 and 74.4, 8,000 154 and 161
     const bool join = n_chunks >= (Rule::S > 1 ? kJoinChunks / 3 : kJoinChunks);
     if (!have_sumsq) {
         const hipError_t e = start_sumsq(t.grads, n_chunks, ws, true, join, 0, nullptr, &in, s);
