@@ -581,6 +581,8 @@ def _buffer(name: str, t, dtype, n: int, device) -> int:
     at = _tensors().buffer(t, dtype, n, device.index)
     if at is None:
         _check_buffer(name, t, dtype, n, device)
+        if t.is_neg():
+            raise AspisError(ERR_INVALID_ARG, f"{name} is a negated view (resolve_neg())")
         at = t.data_ptr()
     return at
 
@@ -645,6 +647,9 @@ class TensorList:
             if t.device != self.device:
                 raise AspisError(ERR_INVALID_ARG, f"tensor {i} of the list is on {t.device}, the "
                                                   f"list on {self.device}")
+            if t.is_neg():
+                raise AspisError(ERR_INVALID_ARG, f"tensor {i} of the list is a negated view: its "
+                                                  f"memory holds other values (resolve_neg())")
             if not t.is_contiguous():
                 contiguous = False
                 if _layout(t) is None:
@@ -826,6 +831,9 @@ def _rows(name: str, x):
     torch = _torch()
     if not isinstance(x, torch.Tensor) or not x.is_cuda or x.dim() < 1:
         raise AspisError(ERR_INVALID_ARG, f"{name} must be a cuda tensor of rows [..., d]")
+    if x.is_neg():
+        raise AspisError(ERR_INVALID_ARG, f"{name} is a negated view: its memory holds other values "
+                                          f"(resolve_neg())")
     code = _dtype_code(x.dtype)
     d = x.shape[-1]
     rows = 1

@@ -12,8 +12,9 @@
 namespace {
 
 // state(list of tensors) -> bytes: of every tensor the address, number of
-// elements, type and contiguity, and of one that is not contiguous its sizes
-// and strides.
+// elements, type, contiguity and whether it is a negated view (its memory
+// holds the opposite of its values), and of one that is not contiguous its
+// sizes and strides.
 PyObject *state(PyObject *, PyObject *arg) {
     if (!PyList_Check(arg)) {
         PyErr_SetString(PyExc_TypeError, "state() takes a list of tensors");
@@ -33,7 +34,7 @@ PyObject *state(PyObject *, PyObject *arg) {
             const bool contiguous = t.is_contiguous();
             words.push_back((int64_t)(intptr_t)t.data_ptr());
             words.push_back(t.numel());
-            words.push_back((int64_t)t.scalar_type() * 2 + contiguous);
+            words.push_back((int64_t)t.scalar_type() * 4 + t.is_neg() * 2 + contiguous);
             if (contiguous) continue;
             words.push_back(t.dim());
             for (int64_t size : t.sizes()) words.push_back(size);
@@ -61,7 +62,7 @@ PyObject *buffer(PyObject *, PyObject *const *args, Py_ssize_t count) {
     try {
         const at::Tensor &t = THPVariable_Unpack(args[0]);
         if (!t.is_cuda() || t.layout() != at::kStrided || t.get_device() != index ||
-            t.numel() < n || !t.is_contiguous() ||
+            t.numel() < n || !t.is_contiguous() || t.is_neg() ||
             t.scalar_type() != reinterpret_cast<THPDtype *>(args[1])->scalar_type)
             Py_RETURN_NONE;
         return PyLong_FromUnsignedLongLong((unsigned long long)(uintptr_t)t.data_ptr());
@@ -78,7 +79,7 @@ PyObject *rows(PyObject *, PyObject *arg) {
     try {
         const at::Tensor &t = THPVariable_Unpack(arg);
         if (!t.is_cuda() || t.layout() != at::kStrided || t.dim() < 1 || t.numel() == 0 ||
-            !t.is_contiguous())
+            !t.is_contiguous() || t.is_neg())
             Py_RETURN_NONE;
         int code = 0;
         switch (t.scalar_type()) {

@@ -351,3 +351,16 @@ def test_lists_match_tensor_by_tensor(monkeypatch):
         for a, b in ((wrong, grads), (grads, wrong)):
             with pytest.raises(aspis.AspisError, match="not contiguous"):
                 aspis._check_match("params", a, b)
+
+
+def test_lists_see_negated_views(monkeypatch):
+    """The imaginary part of a conjugate shares memory that holds its
+    opposite."""
+    import torch
+    x = torch.complex(torch.tensor([3.0]), torch.tensor([4.0]))
+    turned = x.conj().imag
+    assert turned.is_neg() and turned.data_ptr() == x.imag.data_ptr()
+    assert aspis._tensor_state([turned]) != aspis._tensor_state([x.imag])
+    with pytest.raises(aspis.AspisError, match="negated"):
+        _host_list(monkeypatch, [turned])
+    _follows(_host_list(monkeypatch, [turned.resolve_neg()]))

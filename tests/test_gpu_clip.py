@@ -1147,3 +1147,25 @@ def test_adamw_by_a_given_sum_in_a_graph():
         want = state + [bufs.norm, bufs.sumsq.float()]
         assert all(np.array_equal(_bits(a), _bits(b)) for a, b in zip(got, want)), replay
         assert bufs.sumsq.tolist() == [2.0 + replay]
+
+
+def test_negated_views_are_refused():
+    """The imaginary parts of conjugates: memory that holds the opposite."""
+    import torch
+    dev = device()
+    z = torch.complex(torch.full((5, 1), 3.0, device=dev), torch.full((5, 1), 4.0, device=dev))
+    rows, one = z.conj().imag, z.conj().imag[:1, 0]
+    assert rows.is_neg() and one.is_neg() and one.is_contiguous()
+    x = torch.ones(1, device=dev)
+    total = torch.ones(1, dtype=torch.complex128, device=dev).conj().imag
+    for call in (lambda: aspis.clip_rows(rows, 1.0, out=torch.empty(5, 1, device=dev)),
+                 lambda: aspis.clip_rows(one, 1.0), lambda: aspis.row_norms(rows),
+                 lambda: aspis.clip_rows(x, 1.0, out=one), lambda: aspis.grad_norm([one]),
+                 lambda: aspis.clip_grads([x], 1.0, out=[one]),
+                 lambda: aspis.row_norms(x, norms=one.view(())),
+                 lambda: aspis.clip_grads([x], 1.0, sumsq=total)):
+        with pytest.raises(aspis.AspisError, match="negated"):
+            call()
+    assert bool((z.imag == 4.0).all()) and float(x) == 1.0
+    out, norms = aspis.clip_rows(rows.resolve_neg(), 1.0)
+    assert bool((out == -1.0).all() and (norms == 4.0).all())
