@@ -25,8 +25,8 @@
  * enqueued.  HIP failures return ASPIS_ERR_DEVICE.  aspis_last_error()
  * returns a message for the calling thread's last failure.
  *
- * Asynchrony: aspis_detect, aspis_aggregate and the norm, clipping and
- * update calls only enqueue work on the stream.  aspis_clique is host code.
+ * Asynchrony: aspis_detect, aspis_aggregate, the norm, clipping and update
+ * calls and the token operators only enqueue work on the stream.  aspis_clique is host code.
  * aspis_detect_aggregate synchronises the stream (it needs the agreement
  * graph on the host) and returns with its work complete.
  *
@@ -549,6 +549,111 @@ aspis_status aspis_clipped_adamw(const aspis_chunk *params, const aspis_chunk *g
                                  const aspis_chunk *copies, int64_t n_chunks,
                                  const aspis_adamw *opt, double *sumsq, float *norm,
                                  void *workspace, size_t ws_bytes, void *stream);
+
+/* ---- a worker's step on token data --------------------------------------
+ *
+ * The operators at both ends of a language model's step: the embedding
+ * lookup and its gradient, dropout, and the policy loss on the logits with
+ * their gradient.  Workers that hold the same file must return the same bits
+ * (aspis_detect), so results depend on the values, the sizes and dropout's
+ * seed alone: no random state of a device, no order of atomic additions.
+ *
+ * Tensors are rows as in aspis_clip_rows: ld >= d elements from one row's
+ * start to the next, elements aligned to their type.  All entry points only
+ * enqueue work; scratch comes through the caller's workspace, which needs no
+ * particular contents.  Calls that overlap must not share workspaces or
+ * outputs.  Results must not overlap inputs except where a call says so.
+ * Every result is rounded to its type once, from f32. */
+typedef enum { ASPIS_I32 = 0, ASPIS_I64 = 1 } aspis_index;
+
+/* Embedding lookup: out_i = scale * table_(t_i) for the n tokens t_i, rounded
+ * to out's type (scale to f32).  A token outside [0, vocab) -- padding, or
+ * one that another rank's part of the table holds -- gives a row of zeros.
+ * vocab is below 2^31. */
+aspis_status aspis_embed(const void *table, int64_t vocab, int64_t d, int64_t ld,
+                         aspis_dtype dtype, const void *tokens, int64_t n,
+                         aspis_index index, double scale, void *out, int64_t ldo,
+                         aspis_dtype out_dtype, void *stream);
+
+#define ASPIS_EMBED_ACCUMULATE 1u   /* add to what out holds                 */
+
+/* Its gradient: out_v = scale * (the sum of grad_i over the i with t_i = v),
+ * for every row v < vocab; rows without a token are 0.  With
+ * ASPIS_EMBED_ACCUMULATE that is added to out_v in f32, and rows without a
+ * token are neither read nor written.  Tokens outside [0, vocab) add nothing,
+ * and their rows of grad are not read.  Sums are f32, in the tokens' order,
+ * in runs joined in order.  n is at most 2^30, workspace
+ * aspis_embed_workspace(n, d) bytes, 16-aligned (SIZE_MAX on invalid
+ * arguments). */
+size_t aspis_embed_workspace(int64_t n, int64_t d);
+aspis_status aspis_embed_grad(const void *grad, int64_t n, int64_t d, int64_t ld,
+                              aspis_dtype dtype, const void *tokens, aspis_index index,
+                              double scale, void *out, int64_t vocab, int64_t ldo,
+                              aspis_dtype out_dtype, uint32_t flags, void *workspace,
+                              size_t ws_bytes, void *stream);
+
+/* Dropout: out_i = x_i * 65536 / (65536 - T) where element i is kept, 0 where
+ * it is dropped, plus residual_i where residual is not NULL; T = p * 65536
+ * rounded to the nearest integer (ties to even), 0 <= p <= 1.
+ * Element i of the rows, counted without the space between them, has the
+ * position q = offset + i (modulo 2^64).  It is kept unless the 16 bits
+ * q mod 8 (from the lowest of word 0 on) of Philox4x32-10 (Salmon, Moraes,
+ * Dror, Shaw, SC'11) with the key `seed` and the counter q div 8 are below T.
+ * The mask is never stored: the gradient by x is the same call on the
+ * incoming gradient (without the residual).
+ * seed_at, when not NULL, holds the seed on the device instead (8-aligned),
+ * read when the work runs: a replayed graph draws what it then holds.
+ * out may be x or residual itself (the same address and ld). */
+aspis_status aspis_dropout(const void *x, int64_t rows, int64_t d, int64_t ld,
+                           aspis_dtype dtype, double p, uint64_t seed,
+                           const uint64_t *seed_at, uint64_t offset,
+                           const void *residual, int64_t ldr, void *out, int64_t ldo,
+                           void *stream);
+
+/* Bytes of workspace of the two calls below, 16-aligned; SIZE_MAX on invalid
+ * arguments. */
+size_t aspis_policy_workspace(int64_t rows, int64_t vocab, aspis_dtype dtype);
+
+/* logps[i] (device float [rows]) = log p(t_i), the log-probability of token
+ * t_i under softmax(logits_i / temperature); 0 for a token outside
+ * [0, vocab), whose logits are not read.  vocab is at most 2^24, rows 2^30,
+ * the temperature between 1e-30 and 1e30.  A row with a NaN or +inf, or of
+ * -inf alone, gives NaN. */
+aspis_status aspis_token_logps(const void *logits, int64_t rows, int64_t vocab,
+                               int64_t ld, aspis_dtype dtype, const void *tokens,
+                               aspis_index index, double temperature, float *logps,
+                               void *workspace, size_t ws_bytes, void *stream);
+
+/* The clipped policy loss with a KL term, and its gradient by the logits.
+ * With lp_i as above, r = exp(lp_i - old_i), x = ref_i - lp_i, A = advantage_i
+ * and c the clip's border on the side where A raises the objective
+ * (1 + clip_high for A > 0, 1 - clip_low for A < 0):
+ *   loss_i = -min(r A, clip(r) A) + kl * k_i,   k_i = exp(x) - 1 - x
+ *   slope_i = -(r A, or 0 where r is past c) + kl * (1 - exp(x))
+ *   sums   = sum over i of weight_i * (loss_i, k_i, 1 where r is past c)
+ *   grad_iv = grad_scale * weight_i * slope_i / temperature
+ *             * ((v = t_i) - softmax(logits_i / temperature)_v)
+ * The caller divides the weights by what the loss is a mean over.  Positions
+ * of weight 0 or with a token outside [0, vocab) are left out: their logits
+ * and other inputs are not read, logps is 0 and grad a row of zeros.
+ *   old, advantage, weight   device float [rows]
+ *   ref    device float [rows], or NULL: k_i = 0, and kl must be 0
+ *   sums   device float [3], added up in fp64
+ *   logps  device float [rows]
+ *   grad   rows of ldg elements of the logits' type, the logits themselves
+ *          (the same address and ld), or NULL: none
+ * Options: clip_low in [0, 1], clip_high, kl >= 0, a temperature as above and
+ * grad_scale, all finite in f32. */
+typedef struct {
+    double clip_low, clip_high, kl, temperature, grad_scale;
+} aspis_policy;
+aspis_status aspis_policy_loss(const void *logits, int64_t rows, int64_t vocab,
+                               int64_t ld, aspis_dtype dtype, const void *tokens,
+                               aspis_index index, const float *old,
+                               const float *advantage, const float *weight,
+                               const float *ref, const aspis_policy *opt, float *sums,
+                               float *logps, void *grad, int64_t ldg, void *workspace,
+                               size_t ws_bytes, void *stream);
 
 /* Message describing the calling thread's last failure ("" if none). */
 const char *aspis_last_error(void);

@@ -28,6 +28,7 @@ FLAG_PROBE_PREFIX = 16
 CLIP_HAVE_SUMSQ = 1
 CLIP_SKIP_NONFINITE = 2
 CLIP_NO_WAIT = 4
+EMBED_ACCUMULATE = 1
 
 EXPORTED = (
     "aspis_num_files", "aspis_assign", "aspis_detect", "aspis_clique",
@@ -39,6 +40,8 @@ EXPORTED = (
     "aspis_tensor_chunks", "aspis_tensor_entries", "aspis_tensor_table", "aspis_norm_workspace",
     "aspis_grad_norm", "aspis_clip_grads", "aspis_row_workspace", "aspis_row_norms",
     "aspis_clip_rows", "aspis_clipped_sgd", "aspis_clipped_adamw",
+    "aspis_embed", "aspis_embed_workspace", "aspis_embed_grad", "aspis_dropout",
+    "aspis_policy_workspace", "aspis_token_logps", "aspis_policy_loss",
 )
 
 
@@ -130,6 +133,12 @@ class AdamwOptions(ctypes.Structure):
                 ("reserved", ctypes.c_uint32)]
 
 
+class PolicyOptions(ctypes.Structure):
+    _fields_ = [("clip_low", ctypes.c_double), ("clip_high", ctypes.c_double),
+                ("kl", ctypes.c_double), ("temperature", ctypes.c_double),
+                ("grad_scale", ctypes.c_double)]
+
+
 _lib = None
 
 
@@ -211,6 +220,23 @@ def lib():
     L.aspis_clipped_adamw.argtypes = [P, P, P, P, P, i64, ctypes.POINTER(AdamwOptions), P, P, P,
                                       size, P]
     L.aspis_clipped_adamw.restype = ctypes.c_int
+    kind, u64 = ctypes.c_int, ctypes.c_uint64
+    L.aspis_embed.argtypes = [P, i64, i64, i64, kind, P, i64, kind, f64, P, i64, kind, P]
+    L.aspis_embed.restype = ctypes.c_int
+    L.aspis_embed_workspace.argtypes = [i64, i64]
+    L.aspis_embed_workspace.restype = size
+    L.aspis_embed_grad.argtypes = [P, i64, i64, i64, kind, P, kind, f64, P, i64, i64, kind, u32, P,
+                                   size, P]
+    L.aspis_embed_grad.restype = ctypes.c_int
+    L.aspis_dropout.argtypes = [P, i64, i64, i64, kind, f64, u64, P, u64, P, i64, P, i64, P]
+    L.aspis_dropout.restype = ctypes.c_int
+    L.aspis_policy_workspace.argtypes = [i64, i64, kind]
+    L.aspis_policy_workspace.restype = size
+    L.aspis_token_logps.argtypes = [P, i64, i64, i64, kind, P, kind, f64, P, P, size, P]
+    L.aspis_token_logps.restype = ctypes.c_int
+    L.aspis_policy_loss.argtypes = [P, i64, i64, i64, kind, P, kind, P, P, P, P,
+                                    ctypes.POINTER(PolicyOptions), P, P, P, i64, P, size, P]
+    L.aspis_policy_loss.restype = ctypes.c_int
     L.aspis_last_error.argtypes = []
     L.aspis_last_error.restype = ctypes.c_char_p
     _lib = L
@@ -975,4 +1001,207 @@ def clipped_adamw(params, grads, mean, square, *, step: int, lr: float, betas=(0
             tables[4] if copies is not None else None, grads.n_chunks, ctypes.byref(opt),
             total, norm, ws_at, ws.numel(), _raw_stream(grads.device))
     del lists   # their tables were needed until here
+    return bufs
+
+
+# ------------------------------------------ a worker's step on token data
+
+def _token_buffer(tokens, n: int, device) -> tuple[int, int]:
+    """Address and type code of the n tokens of a call."""
+    torch = _torch()
+    if not isinstance(tokens, torch.Tensor) or tokens.numel() != n:
+        raise AspisError(ERR_INVALID_ARG, f"tokens must be a tensor of {n} tokens")
+    wide = tokens.dtype == torch.int64
+    if not wide and tokens.dtype != torch.int32:
+        raise AspisError(ERR_INVALID_ARG, f"tokens must be int32 or int64, not {tokens.dtype}")
+    return _buffer("tokens", tokens, tokens.dtype, n, device), int(wide)
+
+
+def _matrix(name: str, x, device=None):
+    """rows, d, elements between rows and type code of [rows, d] on a device."""
+    rows, d, ld, code = _rows(name, x)
+    if x.dim() != 2 or (device is not None and x.device != device):
+        raise AspisError(ERR_INVALID_ARG, f"{name} must be [rows, d], on the device of the others")
+    return rows, d, ld, code
+
+
+def embed(table, tokens, scale: float = 1.0, out=None):
+    """scale * table[tokens] (aspis_embed): rows of table [vocab, d] for tokens
+    (int32 or int64, any shape) into out [*tokens.shape, d], of the table's type
+    unless given.  A token outside [0, vocab) gives a row of zeros: padding, or
+    one that another rank's part of the table holds (subtract the part's first
+    token, add the ranks' results).  Its gradient is embed_grad; autograd does
+    not see either."""
+    torch = _torch()
+    vocab, d, ld, code = _matrix("table", table)
+    n = tokens.numel() if isinstance(tokens, torch.Tensor) else 0
+    at, wide = _token_buffer(tokens, n, table.device)
+    if out is None:
+        out = torch.empty((*tokens.shape, d), dtype=table.dtype, device=table.device)
+    rows, width, ldo, out_code = _rows("out", out)
+    if rows != n or width != d or out.device != table.device:
+        raise AspisError(ERR_INVALID_ARG, f"out must hold {n} rows of {d} on {table.device}")
+    _launch(table.device, lib().aspis_embed, table.data_ptr(), vocab, d, ld, code, at, n, wide,
+            scale, out.data_ptr(), ldo, out_code, _raw_stream(table.device))
+    return out
+
+
+def embed_workspace(grad, tokens, vocab: int):
+    """Workspace of embed_grad for a gradient [..., d] of these tokens (of any
+    vocabulary)."""
+    torch = _torch()
+    rows, d, _, _ = _rows("grad", grad)
+    n = int(lib().aspis_embed_workspace(rows, d))
+    if n == ctypes.c_size_t(-1).value:
+        raise AspisError(ERR_OVERFLOW, f"{rows} tokens of {d} are too many")
+    return torch.empty(n, dtype=torch.uint8, device=grad.device)
+
+
+def embed_grad(grad, tokens, vocab: int, scale: float = 1.0, out=None, accumulate: bool = False,
+               ws=None):
+    """The table's gradient of embed (aspis_embed_grad): row v of out [vocab, d]
+    (float32 unless given) is scale times the sum of the rows of grad [..., d]
+    whose token is v, in the tokens' order, so that equal inputs give equal
+    bits.  Rows without a token are zeroed; with accumulate the sums are added
+    to what out holds, and those rows are left alone."""
+    torch = _torch()
+    n, d, ld, code = _rows("grad", grad)
+    at, wide = _token_buffer(tokens, n, grad.device)
+    if out is None:
+        if accumulate:
+            raise AspisError(ERR_INVALID_ARG, "accumulate needs out")
+        out = torch.empty((vocab, d), dtype=torch.float32, device=grad.device)
+    rows, width, ldo, out_code = _matrix("out", out, grad.device)
+    if rows != vocab or width != d:
+        raise AspisError(ERR_INVALID_ARG, f"out must be [{vocab}, {d}], not {tuple(out.shape)}")
+    if ws is None:
+        ws = embed_workspace(grad, tokens, vocab)
+    # the workspace's size is the library's to check
+    ws_at = _buffer("ws", ws, torch.uint8, 0, grad.device)
+    _launch(grad.device, lib().aspis_embed_grad, grad.data_ptr(), n, d, ld, code, at, wide, scale,
+            out.data_ptr(), vocab, ldo, out_code, EMBED_ACCUMULATE if accumulate else 0, ws_at,
+            ws.numel(), _raw_stream(grad.device))
+    return out
+
+
+def dropout(x, p: float, seed, offset: int = 0, residual=None, out=None):
+    """x [..., d] with a share p of its elements dropped and the others scaled
+    by 1 / (1 - p), plus residual when given (aspis_dropout), into out (x or
+    residual themselves, another tensor, or a new one).
+
+    Which elements are dropped depends on the seed (an int) and an element's
+    position, offset + its index, alone, and is never stored: the gradient by
+    x is dropout(grad, p, seed, offset), and workers that seed by file, layer
+    and step drop the same.  Ranks with shards give the shard's first position
+    as offset.  p counts in steps of 2^-16.  A graph that captured a call
+    replays its mask; with seed a cuda int64 tensor [1] it draws what that then
+    holds.  Autograd does not see it."""
+    torch = _torch()
+    rows, d, ld, code = _rows("x", x)
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    ldo, ldr, res = ld, 0, None
+    if out is not x:
+        _, _, ldo, out_code = _rows("out", out)
+        if out.shape != x.shape or out_code != code or out.device != x.device:
+            raise AspisError(ERR_INVALID_ARG, "out must have the shape, type and device of x")
+    if residual is not None:
+        _, _, ldr, res_code = _rows("residual", residual)
+        if residual.shape != x.shape or res_code != code or residual.device != x.device:
+            raise AspisError(ERR_INVALID_ARG, "residual must have the shape, type and device of x")
+        res = residual.data_ptr()
+    seed_at = None
+    if isinstance(seed, torch.Tensor):
+        seed_at, seed = _buffer("seed", seed, torch.int64, 1, x.device), 0
+    _launch(x.device, lib().aspis_dropout, x.data_ptr(), rows, d, ld, code, p,
+            seed & 0xFFFFFFFFFFFFFFFF, seed_at, offset & 0xFFFFFFFFFFFFFFFF, res, ldr,
+            out.data_ptr(), ldo, _raw_stream(x.device))
+    return out
+
+
+@dataclass
+class PolicyBuffers:
+    """What policy_loss leaves on the device: sums float32 [3], the weighted
+    sums of the loss, of the KL term and of the positions where the clip acts;
+    logps float32 [rows], the tokens' log-probabilities."""
+    sums: object
+    logps: object
+
+    @classmethod
+    def empty(cls, rows: int, device):
+        torch = _torch()
+        return cls(torch.empty(3, dtype=torch.float32, device=device),
+                   torch.empty(rows, dtype=torch.float32, device=device))
+
+
+def policy_workspace(logits):
+    """Workspace of token_logps and policy_loss for logits [..., vocab]."""
+    torch = _torch()
+    rows, vocab, _, code = _rows("logits", logits)
+    n = int(lib().aspis_policy_workspace(rows, vocab, code))
+    if n == ctypes.c_size_t(-1).value:
+        raise AspisError(ERR_OVERFLOW, f"{rows} rows of {vocab} logits are too many")
+    return torch.empty(n, dtype=torch.uint8, device=logits.device)
+
+
+def token_logps(logits, tokens, temperature: float = 1.0, logps=None, ws=None):
+    """log p of a token per row of logits [..., vocab] under
+    softmax(logits / temperature) (aspis_token_logps), float32 of the tokens'
+    shape: what policy_loss takes as old and ref.  0 where the token is outside
+    the vocabulary.  The result carries no autograd graph."""
+    torch = _torch()
+    rows, vocab, ld, code = _rows("logits", logits)
+    device = logits.device
+    at, wide = _token_buffer(tokens, rows, device)
+    if logps is None:
+        logps = torch.empty(tokens.shape, dtype=torch.float32, device=device)
+    if ws is None:
+        ws = policy_workspace(logits)
+    to = _buffer("logps", logps, torch.float32, rows, device)
+    # the workspace's size is the library's to check
+    ws_at = _buffer("ws", ws, torch.uint8, 0, device)
+    _launch(device, lib().aspis_token_logps, logits.data_ptr(), rows, vocab, ld, code, at, wide,
+            temperature, to, ws_at, ws.numel(), _raw_stream(device))
+    return logps
+
+
+def policy_loss(logits, tokens, old, advantage, weight, ref=None, clip=(0.2, 0.2), kl: float = 0.0,
+                temperature: float = 1.0, grad=None, grad_scale: float = 1.0,
+                bufs: PolicyBuffers | None = None, ws=None) -> PolicyBuffers:
+    """The clipped policy loss of tokens under logits [..., vocab], with a KL
+    term towards a reference, and its gradient by the logits in the same call
+    (aspis_policy_loss has the formulas).  old, advantage, weight and ref are
+    float32, a number per position: log-probabilities when sampled, the
+    advantage, what the position counts (its mask over the number of
+    positions; 0 leaves it out) and log-probabilities under the reference.
+    clip is (below, above) 1.  grad receives grad_scale times the gradient: a
+    tensor like logits, or logits themselves.  Nothing is synchronised.
+
+    Autograd does not see it: hand grad to the layer below (or to autograd, as
+    torch.autograd.backward(logits, grad))."""
+    torch = _torch()
+    f32 = torch.float32
+    rows, vocab, ld, code = _rows("logits", logits)
+    device = logits.device
+    at, wide = _token_buffer(tokens, rows, device)
+    if bufs is None:
+        bufs = PolicyBuffers.empty(rows, device)
+    if ws is None:
+        ws = policy_workspace(logits)
+    to, ldg = None, 0
+    if grad is not None:
+        _, _, ldg, grad_code = _rows("grad", grad)
+        if grad.shape != logits.shape or grad_code != code or grad.device != device:
+            raise AspisError(ERR_INVALID_ARG, "grad must have the shape, type and device of logits")
+        to = grad.data_ptr()
+    opt = PolicyOptions(clip[0], clip[1], kl, temperature, grad_scale)
+    _launch(device, lib().aspis_policy_loss, logits.data_ptr(), rows, vocab, ld, code, at, wide,
+            _buffer("old", old, f32, rows, device),
+            _buffer("advantage", advantage, f32, rows, device),
+            _buffer("weight", weight, f32, rows, device),
+            _buffer("ref", ref, f32, rows, device) if ref is not None else None,
+            ctypes.byref(opt), _buffer("bufs.sums", bufs.sums, f32, 3, device),
+            _buffer("bufs.logps", bufs.logps, f32, rows, device), to, ldg,
+            # the workspace's size is the library's to check
+            _buffer("ws", ws, torch.uint8, 0, device), ws.numel(), _raw_stream(device))
     return bufs

@@ -2,8 +2,8 @@
 module _tensors.so with g++.
 
 The library is the C ABI declared in include/aspis.h: host code
-(csrc/aspis_host.cpp, csrc/aspis_sim.cpp) plus the HIP kernels
-(csrc/aspis_kernels.hip, and csrc/aspis_ws_*.hip for the warp-specialised
+(csrc/aspis_host.cpp, csrc/aspis_sim.cpp, csrc/aspis_clip.cpp, csrc/aspis_tokens.cpp) plus the HIP kernels
+(csrc/aspis_kernels.hip, csrc/aspis_clip.hip, csrc/aspis_tokens.hip, csrc/aspis_policy.hip, and csrc/aspis_ws_*.hip for the warp-specialised
 kernels' many instantiations).  _tensors (csrc/aspis_tensors.cpp) reads the
 addresses and layouts of torch tensors.
 """
@@ -29,7 +29,7 @@ DEVICE_FLAGS = ["-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 
 
 SOURCES = ["aspis_host.cpp", "aspis_sim.cpp", "aspis_clip.cpp", "aspis_clip.hip",
-           "aspis_kernels.hip", "aspis_ws_r3.hip", "aspis_ws_r3_table.hip", "aspis_ws_r5.hip",
+           "aspis_tokens.cpp", "aspis_tokens.hip", "aspis_policy.hip", "aspis_kernels.hip", "aspis_ws_r3.hip", "aspis_ws_r3_table.hip", "aspis_ws_r5.hip",
            "aspis_ws_r7.hip", "aspis_ws_median.hip"]
 
 

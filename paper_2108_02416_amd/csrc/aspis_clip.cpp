@@ -4,16 +4,13 @@
 #include <hip/hip_runtime.h>
 
 #include <cmath>
-#include <cstdarg>
 #include <cstdint>
-#include <cstdio>
 
 #include "../../include/aspis.h"
 #include "aspis_clip.h"
+#include "aspis_errors.h"
 
 namespace aspis {
-aspis_status host_fail(aspis_status st, const char *msg);   // aspis_host.cpp
-void host_clear_error();
 
 RowPlan row_plan(int64_t rows, int64_t d, int elem_bytes) {
     const int64_t per_vec = 16 / elem_bytes, nv = (d + per_vec - 1) / per_vec;
@@ -50,30 +47,10 @@ RowPlan row_plan(int64_t rows, int64_t d, int elem_bytes) {
 
 namespace {
 
-using aspis::host_fail;
-
-constexpr int64_t kMaxElements = int64_t(1) << 60;
-
-aspis_status fail(aspis_status st, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
-aspis_status fail(aspis_status st, const char *fmt, ...) {
-    char msg[400];
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(msg, sizeof msg, fmt, ap);
-    va_end(ap);
-    return host_fail(st, msg);
-}
-
-aspis_status launched(hipError_t e, const char *what) {
-    if (e != hipSuccess)
-        return fail(ASPIS_ERR_DEVICE, "%s failed: %s", what, hipGetErrorString(e));
-    aspis::host_clear_error();
-    return ASPIS_OK;
-}
-
-int elem_bytes(int dtype) {
-    return dtype == ASPIS_F32 ? 4 : dtype == ASPIS_BF16 || dtype == ASPIS_F16 ? 2 : 0;
-}
+using aspis::elem_bytes;
+using aspis::fail;
+using aspis::kMaxElements;
+using aspis::launched;
 
 // Chunks of a list: -1 on invalid sizes, -2 past the limits.
 int64_t count_chunks(const int64_t *numel, int32_t count) {

@@ -1,0 +1,128 @@
+// aspis_tokens.h -- launchers shared by the host entry points of the token
+// operators (aspis_tokens.cpp) and their kernels (aspis_tokens.hip,
+// aspis_policy.hip).  Not part of the public ABI.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <cstdint>
+
+#include "../../include/aspis.h"
+
+namespace aspis {
+
+// n tokens in memory, int32 or int64.
+struct Tokens {
+    const void *at;
+    int wide;   // int64
+#ifdef __HIPCC__
+    // Token i, or -1 where it is outside [0, vocab).
+    __device__ __forceinline__ int get(int64_t i, int64_t vocab) const {
+        const int64_t t = wide ? ((const int64_t *)at)[i] : ((const int32_t *)at)[i];
+        return t >= 0 && t < vocab ? (int)t : -1;
+    }
+#endif
+};
+
+constexpr int64_t kMaxVocab = INT32_MAX;          // rows of a table
+constexpr int64_t kMaxTokens = int64_t(1) << 30;  // of one embedding gradient
+
+struct EmbedArgs {
+    const void *table;
+    int64_t vocab, d, ld;
+    int dtype;
+    Tokens tokens;
+    int64_t n;
+    float scale;
+    void *out;
+    int64_t ldo;
+    int out_dtype;
+};
+hipError_t launch_embed(const EmbedArgs &a, hipStream_t s);
+
+// The gradient: tokens sorted in runs of kSortRun, the runs merged kMergeRuns
+// at a time, then the sorted positions cut into tiles, whose sums of segments
+// that cross a tile's border are joined afterwards.
+constexpr int kSortRun = 2048, kMergeRuns = 16;
+// Positions of a tile.  A function of n alone, since the order of a sum
+// follows it.
+inline int embed_tile(int64_t n) { return n <= 4096 ? 8 : 32; }
+inline int64_t embed_row(int64_t d) { return (d + 3) / 4 * 4; }   // floats of a partial sum
+struct EmbedGradPlan {
+    int tile;
+    int64_t tiles;
+    size_t pairs;    // bytes of one array of sorted (token, position) pairs
+    size_t bytes;    // two of them, then two partial sums a tile
+};
+inline EmbedGradPlan embed_grad_plan(int64_t n, int64_t d) {
+    EmbedGradPlan p;
+    p.tile = embed_tile(n);
+    p.tiles = (n + p.tile - 1) / p.tile;
+    p.pairs = (size_t)((n + 1) / 2 * 16);
+    p.bytes = 2 * p.pairs + (size_t)(p.tiles * 2 * embed_row(d)) * sizeof(float);
+    return p;
+}
+struct EmbedGradArgs {
+    const void *grad;
+    int64_t n, d, ld;
+    int dtype;
+    Tokens tokens;
+    float scale;
+    void *out;
+    int64_t vocab, ldo;
+    int out_dtype;
+    bool accumulate;
+    void *ws;
+};
+hipError_t launch_embed_grad(const EmbedGradArgs &a, hipStream_t s);
+
+struct DropoutArgs {
+    const void *x;
+    int64_t rows, d, ld;
+    int dtype;
+    uint32_t limit;            // kept: 16 bits >= limit
+    float scale;
+    uint64_t seed;
+    const uint64_t *seed_at;   // or nullptr
+    uint64_t offset;
+    const void *residual;      // or nullptr
+    int64_t ldr;
+    void *out;
+    int64_t ldo;
+};
+hipError_t launch_dropout(const DropoutArgs &a, hipStream_t s);
+
+// Rows of logits are cut into parts of kLogitPart elements, a workgroup each.
+constexpr int64_t kMaxLogits = int64_t(1) << 24;
+constexpr int kLogitPart = 8192;
+struct PolicyPlan {
+    int64_t parts;             // of a row
+    size_t stats, at, terms;   // offsets of the workspace's arrays
+    size_t bytes;
+};
+inline PolicyPlan policy_plan(int64_t rows, int64_t vocab) {
+    PolicyPlan p;
+    p.parts = (vocab + kLogitPart - 1) / kLogitPart;
+    p.terms = 0;                                            // double [3][rows]
+    p.stats = p.terms + (size_t)rows * 3 * sizeof(double);  // float2 [rows][parts]
+    p.at = p.stats + (size_t)(rows * p.parts) * 8;          // float [rows]
+    p.bytes = (p.at + (size_t)rows * 4 + 15) / 16 * 16;
+    return p;
+}
+struct PolicyArgs {
+    const void *logits;
+    int64_t rows, vocab, ld;
+    int dtype;
+    Tokens tokens;
+    double inv_temperature;
+    // the loss; sums == nullptr: log-probabilities alone
+    const float *old, *advantage, *weight, *ref;
+    float clip_low, clip_high, kl;   // the borders 1 - low and 1 + high
+    float grad_scale;                // over the temperature
+    float *sums, *logps;
+    void *grad;                      // or nullptr
+    int64_t ldg;
+    void *ws;
+};
+hipError_t launch_policy(const PolicyArgs &a, hipStream_t s);
+
+}  // namespace aspis
