@@ -28,6 +28,7 @@ struct F32 {
     typedef float T;
     typedef u32x4_at4 Vec;
     static constexpr int V = 4;
+    static constexpr uint32_t kLowest = 0xFF800000u;   // -inf, in every element of a word
     __device__ static float get(T x) { return x; }
     __device__ static T put(float x) { return x; }
     __device__ static void unpack(u32x4 w, float (&x)[V]) {
@@ -46,6 +47,7 @@ struct BF16 {
     typedef __bf16 T;
     typedef u32x4_at2 Vec;
     static constexpr int V = 8;
+    static constexpr uint32_t kLowest = 0xFF80FF80u;
     __device__ static float get(T x) { return (float)x; }
     __device__ static T put(float x) { return (__bf16)x; }
     __device__ static void unpack(u32x4 w, float (&x)[V]) {
@@ -70,6 +72,7 @@ struct F16 {
     typedef _Float16 T;
     typedef u32x4_at2 Vec;
     static constexpr int V = 8;
+    static constexpr uint32_t kLowest = 0xFC00FC00u;
     __device__ static float get(T x) { return (float)x; }
     __device__ static T put(float x) { return (_Float16)x; }
     __device__ static void unpack(u32x4 w, float (&x)[V]) {

@@ -3,10 +3,14 @@
 //
 // With z a row of logits, M its maximum, c = log2(e) / temperature and
 // S = sum of 2^((z_v - M) c): log p(t) = (z_t - M) / temperature - ln S, and
-// the gradient's softmax is 2^((z_v - M) c) / S.  The difference z_v - M is
-// formed before the product, so that logits at the type's lowest value (a
-// mask) cannot turn into infinities of both signs; S and its parts are f32,
-// at least 1, and joined in a fixed order.
+// the gradient's softmax is 2^((z_v - M) c) / S.
+//
+// A row's whole vectors are cut into units of 64 lanes and at most 8 vectors a
+// lane, by its length and type alone (the elements after the last vector go
+// to the first unit, one a lane): each has its own maximum and sum (a lane's
+// powers in order, then the lanes), and the units are joined in order.  So a
+// row has the same bits whichever kernel takes it and whatever other rows
+// the call has: files batched together or one by one give the same gradient.
 #include "aspis_tokens.h"
 
 #include <cfloat>
@@ -18,35 +22,64 @@ namespace aspis {
 
 namespace {
 
-constexpr int kBlock = 256;
 constexpr int64_t kMaxGrid = int64_t(1) << 22;   // workgroups of one launch
 
-// A maximum M and the sum of 2^((z - M) c) over some logits; of none, or of
-// -inf alone, M = -inf and S = 0.
+// 2^((z - m) c) as 2^(z c - k), k = m c rounded: one operation and one
+// rounding less, and the rounding of k is the same for every power of a row.
+// Where k leaves f32 (logits at the type's lowest value, a mask) the
+// difference comes first: its operands cannot be infinities of both signs.
+struct Fast {
+    float c, k;
+    __device__ float operator()(float z) const { return __builtin_amdgcn_exp2f(fmaf(z, c, -k)); }
+};
+struct Slow {
+    float c, m;   // of -inf alone, which count nothing: differences from 0
+    __device__ Slow(float c, float top) : c(c), m(top == -INFINITY ? 0.0f : top) {}
+    __device__ float operator()(float z) const { return __builtin_amdgcn_exp2f((z - m) * c); }
+};
+__device__ __forceinline__ bool is_fast(float m, float c) { return fabsf(m * c) <= FLT_MAX; }
+
+// A maximum and the sum of the powers relative to it; of -inf alone the sum
+// is 0.
 struct Stats {
     float m, s;
 };
-__device__ __forceinline__ float power(float z, float m, float c) {
-    return __builtin_amdgcn_exp2f((z - m) * c);
-}
-// What a part's sum counts in one of maximum m (its own maximum at least).
-__device__ __forceinline__ float rescaled(Stats p, float m, float c) {
-    return p.m == -INFINITY && p.s == 0.0f ? 0.0f : p.s * power(p.m, m, c);
+
+// The same of every lane's, joined in lane order.
+__device__ __forceinline__ Stats join_lanes(Stats p, float c) {
+    const float m = lanes_join<64>(p.m, Max());
+    const float by = is_fast(m, c) ? __builtin_amdgcn_exp2f(p.m * c - m * c) : Slow(c, m)(p.m);
+    return {m, lanes_join<64>(p.s == 0.0f ? 0.0f : p.s * by, Sum())};
 }
 
-// The maximum or sum of a workgroup's floats, to every thread.
-template <int B, typename Op>
-__device__ __forceinline__ float block_join(float v, Op op) {
-    v = lanes_join<64>(v, op);
-    if constexpr (B == 64) return v;
-    __shared__ float part[B / 64];
-    if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = v;
-    __syncthreads();
-    float s = part[0];
+// Of N vectors a lane, and one element.
+template <typename E, int N>
+__device__ __forceinline__ Stats unit_stats(const u32x4 *v, float tail, float c) {
+    float m = tail;
 #pragma unroll
-    for (int w = 1; w < B / 64; ++w) s = op(s, part[w]);
-    __syncthreads();
-    return s;
+    for (int r = 0; r < N; ++r) {
+        float x[E::V];
+        E::unpack(v[r], x);
+#pragma unroll
+        for (int j = 0; j < E::V; ++j) m = fmaxf(m, x[j]);
+    }
+    m = lanes_join<64>(m, Max());
+    float s = 0.0f;
+    auto add = [&](auto power) {
+#pragma unroll
+        for (int r = 0; r < N; ++r) {
+            u32x4 again = v[r];
+            asm volatile("" : "+v"(again));   // unpacked anew: kept, it takes twice the registers
+            float x[E::V];
+            E::unpack(again, x);
+#pragma unroll
+            for (int j = 0; j < E::V; ++j) s += power(x[j]);
+        }
+        s += power(tail);
+    };
+    if (__builtin_amdgcn_readfirstlane(is_fast(m, c))) add(Fast{c, m * c});
+    else add(Slow(c, m));
+    return {m, lanes_join<64>(s, Sum())};
 }
 
 // e^x - 1 - x: by its series near 0, where the difference would cancel.
@@ -90,136 +123,236 @@ __device__ __forceinline__ int take_token(const PolicyArgs &a, int64_t row, floa
 
 struct Scratch {
     double *terms;   // [3][rows]
-    Stats *stats;    // [rows][parts]
+    double *partial; // [3][sum_groups]
+    Stats *stats;    // [rows][units]
     float *at;       // [rows]: the token's logit
 };
 
-// N = E::V elements i, i + 1, ... of a row of n; fill past its end.
-template <typename E, Use USE>
-__device__ __forceinline__ void load_part(Ptr<E> row, int64_t i, int64_t n, float fill,
-                                          float (&x)[E::V]) {
-    if (i + E::V <= n) {
-        E::unpack(load_vec<E, USE>(row + i), x);
-        return;
-    }
-#pragma unroll
-    for (int j = 0; j < E::V; ++j) x[j] = i + j < n ? E::get(row[i + j]) : fill;
+// Writes down what a position adds to the sums, and its log-probability.
+__device__ __forceinline__ void put_row(const PolicyArgs &a, const Scratch &w, int64_t row,
+                                        bool used, float weight, float lp, const Terms &t) {
+    a.logps[row] = lp;
+    if (a.sums == nullptr) return;
+    w.terms[row] = used ? (double)weight * t.loss : 0.0;
+    w.terms[a.rows + row] = used ? (double)weight * t.kl : 0.0;
+    w.terms[2 * a.rows + row] = used ? (double)weight * t.cut : 0.0;
 }
 
-// Maximum and sum of every part of a row, and the token's logit.
+// The whole vectors lane, lane + step, ... of a row of nv; -inf past them.
+template <typename E, int N>
+__device__ __forceinline__ void load_logits(Ptr<E> row, int lane, int step, int nv, u32x4 *v) {
+#pragma unroll
+    for (int r = 0; r < N; ++r) {
+        v[r] = (u32x4){E::kLowest, E::kLowest, E::kLowest, E::kLowest};
+        if (lane + r * step < nv) v[r] = load_vec<E, Use::Once>(row + (lane + r * step) * E::V);
+    }
+}
+
+// What a row's gradient is made of.
+struct Grad {
+    float m, c, by, own;   // -(the factor) / S; the token's own element
+};
+
+// The gradient of those vectors, and of the element `tail` in its place.
+template <typename E, int N>
+__device__ __forceinline__ void store_grad(MutPtr<E> out, int lane, int step, int nv, const u32x4 *v,
+                                           const Grad &g) {
+    auto write = [&](auto power) {
+#pragma unroll
+        for (int r = 0; r < N; ++r) {
+            u32x4 again = v[r];
+            asm volatile("" : "+v"(again));
+            float x[E::V];
+            E::unpack(again, x);
+#pragma unroll
+            for (int j = 0; j < E::V; ++j) x[j] = power(x[j]) * g.by;
+            if (lane + r * step < nv)
+                store_vec<E, Use::Once>(out + (lane + r * step) * E::V, E::pack(x));
+        }
+    };
+    if (__builtin_amdgcn_readfirstlane(is_fast(g.m, g.c))) write(Fast{g.c, g.m * g.c});
+    else write(Slow(g.c, g.m));
+}
+// ... and of an element after them, in the first lanes.
 template <typename E>
-__global__ __launch_bounds__(kBlock) void part_stats_kernel(PolicyArgs a, Scratch w, int64_t parts,
-                                                            float c, int64_t first) {
-    constexpr int V = E::V, R = kLogitPart / (kBlock * V);
+__device__ __forceinline__ void store_tail(MutPtr<E> out, int lane, int first, int n, float tail,
+                                           const Grad &g) {
+    if (first + lane >= n) return;
+    const float p = is_fast(g.m, g.c) ? Fast{g.c, g.m * g.c}(tail) : Slow(g.c, g.m)(tail);
+    out[first + lane] = E::put(p * g.by);
+}
+
+// The end of a row's statistics: its log-probability, terms and gradient.
+__device__ __forceinline__ Grad finish_row(const PolicyArgs &a, const Scratch &w, int64_t row,
+                                           float weight, float z, Stats st, float c, bool writes) {
+    // (log2 of the power of the token, in f64: one rounding, in lp)
+    const double x = is_fast(st.m, c) ? ((double)z * c - (double)(st.m * c)) * 0.6931471805599453
+                                      : (double)(z - st.m) * a.inv_temperature;
+    const float p = (is_fast(st.m, c) ? Fast{c, st.m * c}(z) : Slow(c, st.m)(z)) / st.s;
+    float lp = (float)(x - (double)logf(st.s));
+    // where the others' share is below f32's, and where a rounding went past 1
+    if (p >= 1.0f || lp > 0.0f) lp = 0.0f;
+    Terms t{0.0f, 0.0f, 0.0f, 0.0f};
+    if (a.sums != nullptr) t = terms_of(a, row, weight, lp);
+    if (writes) put_row(a, w, row, true, weight, lp, t);
+    return {st.m, c, -t.coef / st.s, t.coef * (1.0f - p)};
+}
+
+template <typename E>
+__device__ __forceinline__ void zero_row(MutPtr<E> out, int64_t first, int64_t step, int64_t n) {
+    for (int64_t i = first; i < n / E::V; i += step)
+        store_vec<E, Use::Once>(out + i * E::V, (u32x4){0, 0, 0, 0});
+    for (int64_t i = n / E::V * E::V + first; i < n; i += step) out[i] = E::put(0.0f);
+}
+
+// How a row of `vecs` vectors is cut: L lanes hold R vectors each, lane l the
+// vectors l, l + L, ...; a wave's first min(R, 8) are a unit, its next ones
+// another.  Rows of more than 1024 * 16 vectors: blocks of so many.
+constexpr int kUnitVecs = 8, kBlockVecs = 1024 * 16;
+
+// A row in the registers of L lanes: read once, its gradient written once.
+template <typename E, int L, int R, bool GRAD>
+__global__ __launch_bounds__(L < 256 ? 256 : L) void
+row_kernel(PolicyArgs a, Scratch w, float c, int64_t first) {
+    constexpr int B = L < 256 ? 256 : L, N = R < kUnitVecs ? R : kUnitVecs;
+    constexpr int UNITS = L / 64 * (R / N);
+    static_assert(UNITS <= 64, "a lane each");
+    const int lane = threadIdx.x % L;
+    const int64_t row = first + (int64_t)blockIdx.x * (B / L) + threadIdx.x / L;
+    if (L < B && row >= a.rows) return;
+    float weight;
+    const int token = take_token(a, row, weight);
+    const MutPtr<E> out = (MutPtr<E>)a.grad + row * a.ldg;
+    const int n = (int)a.vocab, nv = n / E::V;
+    if (token < 0) {
+        if (lane == 0) put_row(a, w, row, false, 0.0f, 0.0f, {});
+        if constexpr (GRAD) zero_row<E>(out, lane, L, n);
+        return;
+    }
+    const Ptr<E> z = (Ptr<E>)a.logits + row * a.ld;
+    u32x4 v[R];
+    load_logits<E, R>(z, lane, L, nv, v);
+    const float tail = nv * E::V + lane < n ? E::get(z[nv * E::V + lane]) : -INFINITY;
+    const float at = E::get(z[token]);
+    Stats st;
+    if constexpr (UNITS == 1) {
+        st = unit_stats<E, N>(v, tail, c);
+    } else {
+        __shared__ Stats units[UNITS];
+#pragma unroll
+        for (int u = 0; u < R / N; ++u) {
+            const Stats p = unit_stats<E, N>(v + u * N, u == 0 ? tail : -INFINITY, c);
+            if (threadIdx.x % 64 == 0) units[u * (L / 64) + threadIdx.x / 64] = p;
+        }
+        __syncthreads();
+        const int i = threadIdx.x % 64;
+        st = join_lanes(i < UNITS ? units[i] : Stats{-INFINITY, 0.0f}, c);
+    }
+    const Grad g = finish_row(a, w, row, weight, at, st, c, lane == 0);
+    if constexpr (!GRAD) return;
+    store_grad<E, R>(out, lane, L, nv, v, g);
+    store_tail<E>(out, lane, nv * E::V, n, tail, g);
+    // the token's own, over what the same lane has just written
+    if (lane == (token < nv * E::V ? token / E::V % L : token - nv * E::V)) out[token] = E::put(g.own);
+}
+
+// Few rows, and rows longer than the registers of a workgroup: a wave for
+// every unit, then one for every unit of the gradient.
+template <typename E, int L, int R>
+__global__ __launch_bounds__(64) void unit_stats_kernel(PolicyArgs a, Scratch w, float c, int units,
+                                                        int64_t first) {
+    constexpr int N = R < kUnitVecs ? R : kUnitVecs, OF_BLOCK = L / 64 * (R / N);
     const int64_t item = first + blockIdx.x;
-    const int64_t row = item / parts, at = item % parts * kLogitPart;
+    const int64_t row = item / units;
+    const int unit = (int)(item % units), block = unit / OF_BLOCK, of = unit % OF_BLOCK;
     float weight;
     const int token = take_token(a, row, weight);
     if (token < 0) return;
     const Ptr<E> z = (Ptr<E>)a.logits + row * a.ld;
-    float x[R][V];
-    float m = -INFINITY;
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-        load_part<E, Use::Again>(z, at + (r * kBlock + (int)threadIdx.x) * V, a.vocab, -INFINITY,
-                                 x[r]);
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-        for (int j = 0; j < V; ++j) m = fmaxf(m, x[r][j]);
-    m = block_join<kBlock>(m, Max());
-    // a part of -inf alone: differences from 0, which count nothing
-    const float from = m == -INFINITY ? 0.0f : m;
-    float s = 0.0f;
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-        for (int j = 0; j < V; ++j) s += power(x[r][j], from, c);
-    s = block_join<kBlock>(s, Sum());
-    if (threadIdx.x != 0) return;
-    w.stats[item] = {m, s};
-    if (token >= at && token < at + kLogitPart) w.at[row] = E::get(z[token]);
+    const int n = (int)a.vocab, nv = n / E::V;
+    const int i0 = block * kBlockVecs + of / (L / 64) * N * L + of % (L / 64) * 64 + threadIdx.x;
+    u32x4 v[N];
+    load_logits<E, N>(z, i0, L, nv, v);
+    const int last = nv * E::V + threadIdx.x;
+    const float tail = unit == 0 && last < n ? E::get(z[last]) : -INFINITY;
+    if (unit == 0 && threadIdx.x == 0) w.at[row] = E::get(z[token]);
+    const Stats st = unit_stats<E, N>(v, tail, c);
+    if (threadIdx.x == 0) w.stats[item] = st;
 }
 
-// A row's statistics from its parts', to every thread of the workgroup.
-__device__ __forceinline__ Stats join_parts(const Stats *p, int64_t parts, float c) {
-    float m = -INFINITY, s = 0.0f;
-    for (int64_t i = threadIdx.x; i < parts; i += kBlock) m = fmaxf(m, p[i].m);
-    m = block_join<kBlock>(m, Max());
-    for (int64_t i = threadIdx.x; i < parts; i += kBlock) s += rescaled(p[i], m, c);
-    return {m, block_join<kBlock>(s, Sum())};
-}
-
-// log p of the token from the row's statistics.
-__device__ __forceinline__ float log_prob(const PolicyArgs &a, float z, Stats st) {
-    return (float)((double)(z - st.m) * a.inv_temperature - (double)logf(st.s));
-}
-
-// The gradient of one part of a row; the first part's workgroup writes what
-// the row adds to the sums.
-template <typename E>
-__global__ __launch_bounds__(kBlock) void part_grad_kernel(PolicyArgs a, Scratch w, int64_t parts,
-                                                           int64_t grads, float c, int64_t first) {
-    constexpr int V = E::V, R = kLogitPart / (kBlock * V);
-    const int64_t item = first + blockIdx.x;   // (row, one of the `grads` parts written)
-    const int64_t row = item / grads, part = item % grads, at = part * kLogitPart;
+template <typename E, int L, int R>
+__global__ __launch_bounds__(64) void unit_grad_kernel(PolicyArgs a, Scratch w, float c, int units,
+                                                       int grads, int64_t first) {
+    constexpr int N = R < kUnitVecs ? R : kUnitVecs, OF_BLOCK = L / 64 * (R / N);
+    const int64_t item = first + blockIdx.x;   // (row, one of the `grads` units written)
+    const int64_t row = item / grads;
+    const int unit = (int)(item % grads), block = unit / OF_BLOCK, of = unit % OF_BLOCK;
     float weight;
     const int token = take_token(a, row, weight);
-    const Ptr<E> z = (Ptr<E>)a.logits + row * a.ld;
     const MutPtr<E> out = (MutPtr<E>)a.grad + row * a.ldg;
-    Terms t{0.0f, 0.0f, 0.0f, 0.0f};
-    Stats st{0.0f, 1.0f};
-    float lp = 0.0f, p = 0.0f;
-    if (token >= 0) {
-        st = join_parts(w.stats + row * parts, parts, c);
-        lp = log_prob(a, w.at[row], st);
-        p = power(w.at[row], st.m, c) / st.s;
-        if (a.sums != nullptr) t = terms_of(a, row, weight, lp);
+    if (token < 0) {
+        if (unit == 0 && threadIdx.x == 0) put_row(a, w, row, false, 0.0f, 0.0f, {});
+        if (a.grad != nullptr) zero_row<E>(out, unit * 64 + threadIdx.x, grads * 64, a.vocab);
+        return;
     }
-    if (part == 0 && threadIdx.x == 0) {
-        a.logps[row] = lp;
-        if (a.sums != nullptr) {
-            w.terms[row] = (double)weight * t.loss;
-            w.terms[a.rows + row] = (double)weight * t.kl;
-            w.terms[2 * a.rows + row] = (double)weight * t.cut;
-            if (token < 0)
-                for (int k = 0; k < 3; ++k) w.terms[k * a.rows + row] = 0.0;
+    Stats p{-INFINITY, 0.0f};
+    const Stats *of_row = w.stats + row * units;
+    if (units <= 64) {
+        if ((int)threadIdx.x < units) p = of_row[threadIdx.x];
+    } else {
+        // a lane's units first: 64 apart, in order, relative to their maximum
+        for (int i = threadIdx.x; i < units; i += 64) p.m = fmaxf(p.m, of_row[i].m);
+        const bool fast = is_fast(p.m, c);
+        for (int i = threadIdx.x; i < units; i += 64) {
+            const Stats q = of_row[i];
+            const float by = fast ? __builtin_amdgcn_exp2f(q.m * c - p.m * c) : Slow(c, p.m)(q.m);
+            p.s += q.s == 0.0f ? 0.0f : q.s * by;
         }
     }
+    const Grad g = finish_row(a, w, row, weight, w.at[row], join_lanes(p, c), c,
+                              unit == 0 && threadIdx.x == 0);
     if (a.grad == nullptr) return;
-    const float by = -t.coef / st.s;
+    const Ptr<E> z = (Ptr<E>)a.logits + row * a.ld;
+    const int n = (int)a.vocab, nv = n / E::V, lane = threadIdx.x;
+    const int i0 = block * kBlockVecs + of / (L / 64) * N * L + of % (L / 64) * 64 + lane;
+    u32x4 v[N];
+    load_logits<E, N>(z, i0, L, nv, v);
+    store_grad<E, N>(out, i0, L, nv, v, g);
+    // the token's own, over what the same lane has just written
+    const int of_token = token / E::V - i0;
+    if (token < nv * E::V && of_token >= 0 && of_token < N * L && of_token % L == 0)
+        out[token] = E::put(g.own);
+    if (unit != 0) return;
+    if (nv * E::V + lane < n) store_tail<E>(out, lane, nv * E::V, n, E::get(z[nv * E::V + lane]), g);
+    if (lane == token - nv * E::V) out[token] = E::put(g.own);
+}
+
+// The loss and the two other sums, in fp64 and an order that the number of
+// rows fixes: of n terms each, `step` a workgroup; to `to` [3][workgroups],
+// or to sums from one workgroup.
+__global__ __launch_bounds__(1024) void sum_terms_kernel(const double *terms, int64_t n,
+                                                         int64_t step, double *to, float *sums) {
+    const int64_t from = blockIdx.x * step, end = from + step < n ? from + step : n;
+    double s[3] = {0.0, 0.0, 0.0};
+    for (int64_t i = from + threadIdx.x; i < end; i += 1024)
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int64_t i = at + (r * kBlock + (int)threadIdx.x) * V;
-        if (i >= a.vocab) continue;
-        float x[V] = {};
-        if (token >= 0) {
-            load_part<E, Use::Once>(z, i, a.vocab, 0.0f, x);
+        for (int k = 0; k < 3; ++k) s[k] += terms[k * n + i];
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                x[j] = power(x[j], st.m, c) * by;
-                if (i + j == token) x[j] = t.coef * (1.0f - p);
-            }
-        }
-        if (i + V <= a.vocab) {
-            store_vec<E, Use::Once>(out + i, E::pack(x));
-            continue;
-        }
-#pragma unroll
-        for (int j = 0; j < V; ++j)
-            if (i + j < a.vocab) out[i + j] = E::put(x[j]);
+    for (int k = 0; k < 3; ++k) {
+        s[k] = block_sum<1024>(s[k]);
+        if (threadIdx.x != 0) continue;
+        if (gridDim.x > 1) to[k * gridDim.x + blockIdx.x] = s[k];
+        else sums[k] = (float)s[k];
     }
 }
 
-// The loss and the two other sums, in fp64 and a fixed order.
-__global__ __launch_bounds__(1024) void sum_terms_kernel(const double *terms, int64_t rows,
-                                                         float *sums) {
-    for (int k = 0; k < 3; ++k) {
-        double s = 0.0;
-        for (int64_t i = threadIdx.x; i < rows; i += 1024) s += terms[k * rows + i];
-        s = block_sum<1024>(s);
-        if (threadIdx.x == 0) sums[k] = (float)s;
-    }
+hipError_t start_sums(const PolicyArgs &a, const Scratch &w, hipStream_t s) {
+    const unsigned groups = (unsigned)sum_groups(a.rows);
+    const int64_t step = (a.rows + groups - 1) / groups;
+    sum_terms_kernel<<<groups, 1024, 0, s>>>(w.terms, a.rows, step, w.partial, a.sums);
+    if (groups > 1)
+        sum_terms_kernel<<<1, 1024, 0, s>>>(w.partial, groups, groups, nullptr, a.sums);
+    return hipGetLastError();
 }
 
 // Calls launch(first, n) until `blocks` workgroups are launched.
@@ -233,24 +366,47 @@ hipError_t over_blocks(int64_t blocks, F &&launch) {
     return hipSuccess;
 }
 
-template <typename E>
-hipError_t start_policy(const PolicyArgs &a, hipStream_t s) {
-    const PolicyPlan plan = policy_plan(a.rows, a.vocab);
-    char *const ws = (char *)a.ws;
-    const Scratch w{(double *)(ws + plan.terms), (Stats *)(ws + plan.stats),
-                    (float *)(ws + plan.at)};
-    const float c = (float)(1.4426950408889634 * a.inv_temperature);
-    hipError_t e = over_blocks(a.rows * plan.parts, [&](int64_t first, unsigned n) {
-        part_stats_kernel<E><<<n, kBlock, 0, s>>>(a, w, plan.parts, c, first);
+// Rows longer than this and fewer than kFewRows go by units.
+constexpr int64_t kFewRows = 128;
+
+template <typename E, int L, int R>
+hipError_t start_rows(const PolicyArgs &a, const Scratch &w, float c, int units, bool by_units,
+                      hipStream_t s) {
+    constexpr int B = L < 256 ? 256 : L;
+    if (!by_units)
+        return over_blocks((a.rows + B / L - 1) / (B / L), [&](int64_t first, unsigned n) {
+            first *= B / L;
+            if (a.grad != nullptr) row_kernel<E, L, R, true><<<n, B, 0, s>>>(a, w, c, first);
+            else row_kernel<E, L, R, false><<<n, B, 0, s>>>(a, w, c, first);
+        });
+    const hipError_t e = over_blocks(a.rows * units, [&](int64_t first, unsigned n) {
+        unit_stats_kernel<E, L, R><<<n, 64, 0, s>>>(a, w, c, units, first);
     });
     if (e != hipSuccess) return e;
-    const int64_t grads = a.grad != nullptr && plan.parts > 0 ? plan.parts : 1;
-    e = over_blocks(a.rows * grads, [&](int64_t first, unsigned n) {
-        part_grad_kernel<E><<<n, kBlock, 0, s>>>(a, w, plan.parts, grads, c, first);
+    const int grads = a.grad != nullptr ? units : 1;
+    return over_blocks(a.rows * grads, [&](int64_t first, unsigned n) {
+        unit_grad_kernel<E, L, R><<<n, 64, 0, s>>>(a, w, c, units, grads, first);
     });
+}
+
+template <typename E>
+hipError_t start_policy(const PolicyArgs &a, hipStream_t s) {
+    const PolicyPlan plan = policy_plan(a.rows, a.vocab, sizeof(typename E::T));
+    char *const ws = (char *)a.ws;
+    const Scratch w{(double *)(ws + plan.terms), (double *)(ws + plan.partial), (Stats *)(ws + plan.stats),
+                    (float *)(ws + plan.at)};
+    const float c = (float)(1.4426950408889634 * a.inv_temperature);
+    const int64_t nv = (a.vocab + E::V - 1) / E::V;
+    const int units = plan.units;
+    hipError_t e;
+    if (nv <= 64) e = start_rows<E, 64, 1>(a, w, c, units, false, s);
+    else if (nv <= 256) e = start_rows<E, 64, 4>(a, w, c, units, false, s);
+    else if (nv <= 1024) e = start_rows<E, 256, 4>(a, w, c, units, false, s);
+    else if (nv <= 4096) e = start_rows<E, 256, 16>(a, w, c, units, a.rows < kFewRows, s);
+    else if (nv <= 8192) e = start_rows<E, 512, 16>(a, w, c, units, a.rows < kFewRows, s);
+    else e = start_rows<E, 1024, 16>(a, w, c, units, a.rows < kFewRows || nv > kBlockVecs, s);
     if (e != hipSuccess || a.sums == nullptr) return e;
-    sum_terms_kernel<<<1, 1024, 0, s>>>(w.terms, a.rows, a.sums);
-    return hipGetLastError();
+    return start_sums(a, w, s);
 }
 
 }  // namespace

@@ -163,7 +163,7 @@ size_t aspis_policy_workspace(int64_t rows, int64_t vocab, aspis_dtype dtype) {
     if (elem_bytes(dtype) == 0 || rows < 0 || vocab < 0 || vocab > aspis::kMaxLogits ||
         (rows > 0 && vocab > kMaxElements / rows))
         return SIZE_MAX;
-    return aspis::policy_plan(rows, vocab).bytes;
+    return aspis::policy_plan(rows, vocab, elem_bytes(dtype)).bytes;
 }
 
 namespace {

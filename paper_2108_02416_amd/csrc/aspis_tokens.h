@@ -91,20 +91,32 @@ struct DropoutArgs {
 };
 hipError_t launch_dropout(const DropoutArgs &a, hipStream_t s);
 
-// Rows of logits are cut into parts of kLogitPart elements, a workgroup each.
 constexpr int64_t kMaxLogits = int64_t(1) << 24;
-constexpr int kLogitPart = 8192;
+// Units of a row (aspis_policy.hip): 64 lanes and at most 8 vectors each.
+inline int policy_units(int64_t vocab, int elem_bytes) {
+    const int64_t vecs = (vocab * elem_bytes + 15) / 16;
+    if (vecs <= 256) return 1;
+    if (vecs <= 1024) return 4;
+    if (vecs <= 4096) return 8;
+    if (vecs <= 8192) return 16;
+    return (int)((vecs + 16383) / 16384) * 32;
+}
+// Workgroups that add up the rows' terms, before one joins theirs.
+inline int sum_groups(int64_t rows) {
+    return rows <= 8192 ? 1 : rows >= 64 * 4096 ? 64 : (int)((rows + 4095) / 4096);
+}
 struct PolicyPlan {
-    int64_t parts;             // of a row
-    size_t stats, at, terms;   // offsets of the workspace's arrays
+    int units;                          // of a row
+    size_t terms, partial, stats, at;   // offsets of the workspace's arrays
     size_t bytes;
 };
-inline PolicyPlan policy_plan(int64_t rows, int64_t vocab) {
+inline PolicyPlan policy_plan(int64_t rows, int64_t vocab, int elem_bytes) {
     PolicyPlan p;
-    p.parts = (vocab + kLogitPart - 1) / kLogitPart;
-    p.terms = 0;                                            // double [3][rows]
-    p.stats = p.terms + (size_t)rows * 3 * sizeof(double);  // float2 [rows][parts]
-    p.at = p.stats + (size_t)(rows * p.parts) * 8;          // float [rows]
+    p.units = policy_units(vocab, elem_bytes);
+    p.terms = 0;                                   // double [3][rows], then [3][sum_groups]
+    p.partial = p.terms + (size_t)rows * 3 * sizeof(double);
+    p.stats = p.partial + (size_t)sum_groups(rows) * 3 * sizeof(double);   // float2 [rows][units]
+    p.at = p.stats + (size_t)(rows * p.units) * 8;          // float [rows]
     p.bytes = (p.at + (size_t)rows * 4 + 15) / 16 * 16;
     return p;
 }

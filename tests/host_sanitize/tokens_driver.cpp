@@ -27,10 +27,9 @@ hipError_t launch_dropout(const DropoutArgs &a, hipStream_t) {
     return hipSuccess;
 }
 hipError_t launch_policy(const PolicyArgs &a, hipStream_t) {
-    const PolicyPlan p = policy_plan(a.rows, a.vocab);
-    if (p.parts * kLogitPart < a.vocab || p.stats % 8 != 0 || p.at % 4 != 0 || p.bytes % 16 != 0)
-        abort();
-    if (p.bytes < p.at + (size_t)a.rows * 4 || p.at != p.stats + (size_t)(a.rows * p.parts) * 8)
+    const PolicyPlan p = policy_plan(a.rows, a.vocab, a.dtype == ASPIS_F32 ? 4 : 2);
+    if (p.units < 1 || p.stats % 8 != 0 || p.at % 4 != 0 || p.bytes % 16 != 0) abort();
+    if (p.bytes < p.at + (size_t)a.rows * 4 || p.at != p.stats + (size_t)(a.rows * p.units) * 8)
         abort();
     ++reached;
     return hipSuccess;
