@@ -39,26 +39,27 @@ struct EmbedArgs {
 };
 hipError_t launch_embed(const EmbedArgs &a, hipStream_t s);
 
-// The gradient: tokens sorted in runs of kSortRun, the runs merged kMergeRuns
-// at a time, then the sorted positions cut into tiles, whose sums of segments
-// that cross a tile's border are joined afterwards.
-constexpr int kSortRun = 2048, kMergeRuns = 16;
-// Positions of a tile.  A function of n alone, since the order of a sum
-// follows it.
-inline int embed_tile(int64_t n) { return n <= 4096 ? 8 : 32; }
+// The gradient: tokens sorted in runs of kSortRun, kMergeRuns of them merged
+// in LDS, longer ones where they are; then the sums of the sorted positions'
+// segments, window by window of positions, long ones in pieces of at most a
+// block of two windows that are joined afterwards.
+constexpr int kSortRun = 1024, kMergeRuns = 32;
+// log2 of a window's positions: a function of n alone, since the order of a
+// sum follows it.
+inline int embed_shift(int64_t n) { return n <= 4096 ? 3 : 5; }
 inline int64_t embed_row(int64_t d) { return (d + 3) / 4 * 4; }   // floats of a partial sum
 struct EmbedGradPlan {
-    int tile;
-    int64_t tiles;
-    size_t pairs;    // bytes of one array of sorted (token, position) pairs
-    size_t bytes;    // two of them, then two partial sums a tile
+    int shift;       // log2 of a window's positions
+    int64_t blocks;
+    size_t words;    // bytes of an array of n words, and 8 that may be read past them
+    size_t bytes;    // four of them (tokens and positions, twice), two partial sums a block
 };
 inline EmbedGradPlan embed_grad_plan(int64_t n, int64_t d) {
     EmbedGradPlan p;
-    p.tile = embed_tile(n);
-    p.tiles = (n + p.tile - 1) / p.tile;
-    p.pairs = (size_t)((n + 1) / 2 * 16);
-    p.bytes = 2 * p.pairs + (size_t)(p.tiles * 2 * embed_row(d)) * sizeof(float);
+    p.shift = embed_shift(n);
+    p.blocks = (n + (2 << p.shift) - 1) / (2 << p.shift);
+    p.words = n > 0 ? (size_t)((n + 3) / 4 * 16 + 32) : 0;
+    p.bytes = 4 * p.words + (size_t)(p.blocks * 2 * embed_row(d)) * sizeof(float);
     return p;
 }
 struct EmbedGradArgs {

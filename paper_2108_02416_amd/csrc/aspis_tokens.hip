@@ -52,320 +52,526 @@ unsigned grid_for(int64_t items, int per_block) {
 // ---------------------------------------------------------------------------
 // embedding lookup
 
-template <typename EI, typename EO>
+// 2^shift lanes take U rows at a time.  Memory bounds it: 16,384 rows of
+// 2,048 f32 out of 32,003, to bf16, in 22.7 us, 4.9 TB/s, with two rows at a
+// time and stores past the cache; one at a time 30.3 us, four 22.8, two with
+// plain stores 27.4.  Few rows, whose results stay in the cache, are latency.
+constexpr int64_t kPairRows = 4096;   // workgroups of single rows from which on pairs are taken
+
+template <typename EI, typename EO, int U>
 __global__ __launch_bounds__(kBlock) void embed_kernel(EmbedArgs a, int shift) {
-    constexpr int N = EI::V > EO::V ? EI::V : EO::V;
+    constexpr int N = EI::V > EO::V ? EI::V : EO::V, W = N / EI::V;
     const int lane = (int)threadIdx.x & ((1 << shift) - 1);
-    const int per_block = kBlock >> shift;
+    const int64_t per_block = (kBlock >> shift) * U;
     const int64_t nv = a.d / N;
-    for (int64_t row = (int64_t)blockIdx.x * per_block + (threadIdx.x >> shift); row < a.n;
-         row += (int64_t)gridDim.x * per_block) {
-        const int token = a.tokens.get(row, a.vocab);
-        const Ptr<EI> from = (Ptr<EI>)a.table + (token < 0 ? 0 : token) * a.ld;
-        const MutPtr<EO> to = (MutPtr<EO>)a.out + row * a.ldo;
-        for (int64_t v = lane; v < nv; v += 1 << shift) {
-            float x[N] = {};
-            if (token >= 0) load_floats<EI, N>(from + v * N, x);
+    for (int64_t row0 = blockIdx.x * per_block + (threadIdx.x >> shift) * U; row0 < a.n;
+         row0 += gridDim.x * per_block) {
+        int token[U];
 #pragma unroll
-            for (int j = 0; j < N; ++j) x[j] *= a.scale;
-            store_floats<EO, N>(to + v * N, x);
+        for (int u = 0; u < U; ++u) token[u] = a.tokens.get(row0 + u < a.n ? row0 + u : a.n - 1, a.vocab);
+        auto from = [&](int u) { return (Ptr<EI>)a.table + (token[u] < 0 ? 0 : token[u]) * a.ld; };
+        auto to = [&](int u) { return (MutPtr<EO>)a.out + (row0 + u) * a.ldo; };
+        for (int64_t v = lane; v < nv; v += 1 << shift) {
+            u32x4 x[U][W];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int w = 0; w < W; ++w) {
+                    x[u][w] = (u32x4){0, 0, 0, 0};
+                    if (token[u] >= 0) x[u][w] = load_vec<EI>(from(u) + v * N + w * EI::V);
+                }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                float y[N];
+#pragma unroll
+                for (int w = 0; w < W; ++w) {
+                    float z[EI::V];
+                    EI::unpack(x[u][w], z);
+#pragma unroll
+                    for (int j = 0; j < EI::V; ++j) y[w * EI::V + j] = z[j] * a.scale;
+                }
+                if (row0 + u < a.n) store_floats<EO, N, U == 1 ? Use::Again : Use::Once>(to(u) + v * N, y);
+            }
         }
         for (int64_t i = nv * N + lane; i < a.d; i += 1 << shift)
-            to[i] = EO::put(token >= 0 ? EI::get(from[i]) * a.scale : 0.0f);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (row0 + u < a.n)
+                    to(u)[i] = EO::put(token[u] >= 0 ? EI::get(from(u)[i]) * a.scale : 0.0f);
     }
 }
 
 // ---------------------------------------------------------------------------
 // its gradient: the tokens sorted
 
-// A token (vocab where it is none) and its position, in one word that orders
-// by both: no two are equal, so every way of sorting gives the same order.
-typedef uint64_t Pair;
-__device__ __forceinline__ Pair pair_of(uint32_t token, uint32_t at) {
-    return (uint64_t)token << 32 | at;
-}
-__device__ __forceinline__ uint32_t token_of(Pair p) { return (uint32_t)(p >> 32); }
+// The tokens in order (vocab where a token is none, so that those come last)
+// and the positions they were at, those of equal tokens in order.
+struct Sorted {
+    uint32_t *token, *at;
+};
 
-template <typename K>
-__device__ __forceinline__ K lane_xor(K v, int mask) {
-    return __shfl_xor(v, mask, 64);
+// The value of the lane whose index differs in the bits of M.
+template <int M>
+__device__ __forceinline__ uint32_t lane_xor(uint32_t v) {
+    const int w = (int)v;
+    if constexpr (M == 1) return __builtin_amdgcn_update_dpp(0, w, 0xB1, 0xF, 0xF, true);
+    else if constexpr (M == 2) return __builtin_amdgcn_update_dpp(0, w, 0x4E, 0xF, 0xF, true);
+    else if constexpr (M == 4)   // the mirrors of 8 and of 4 lanes
+        return __builtin_amdgcn_update_dpp(
+            0, __builtin_amdgcn_update_dpp(0, w, 0x141, 0xF, 0xF, true), 0x1B, 0xF, 0xF, true);
+    else if constexpr (M == 8)   // half a turn of 16 lanes
+        return __builtin_amdgcn_update_dpp(0, w, 0x128, 0xF, 0xF, true);
+    else return __shfl_xor(v, M, 64);
+}
+template <int M>
+__device__ __forceinline__ uint64_t lane_xor(uint64_t v) {
+    return (uint64_t)lane_xor<M>((uint32_t)(v >> 32)) << 32 | lane_xor<M>((uint32_t)v);
 }
 
-// kSortRun tokens sorted by one workgroup: a bitonic sort of eight keys a
-// thread, exchanged in registers, between lanes, and through LDS.
+// A bitonic sort of kSortRun keys, kSortKeys a thread: key r of thread t is
+// number t * kSortKeys + r.  Keys meet in a thread, between lanes, and
+// through LDS between waves.  No two are equal (but those past the end).
 constexpr int kSortKeys = kSortRun / kBlock;
 
-template <typename K>
-__device__ __forceinline__ void order(K &a, K &b, bool up) {
-    const bool swap = up ? b < a : a < b;
-    const K low = swap ? b : a;
-    b = swap ? a : b;
-    a = low;
-}
-
-template <typename K>
-__device__ void sort_run(K (&key)[kSortKeys], K *lds) {
+// Step J of the merge to sequences of K.
+template <int K, int J, typename T>
+__device__ __forceinline__ void sort_step(T (&key)[kSortKeys], T *lds) {
     const int t = threadIdx.x;
-#pragma unroll 1
-    for (int k = 2; k <= kSortRun; k *= 2) {
-#pragma unroll 1
-        for (int j = k / 2; j >= kSortKeys; j /= 2) {
-            const int m = j / kSortKeys;   // the other key is m threads away
-            const bool up = (t * kSortKeys & k) == 0, low = (t & m) == 0;
-            K other[kSortKeys];
-            if (m < 64) {
+    if constexpr (J < kSortKeys) {
 #pragma unroll
-                for (int r = 0; r < kSortKeys; ++r) other[r] = lane_xor(key[r], m);
-            } else {
-                __syncthreads();
-#pragma unroll
-                for (int r = 0; r < kSortKeys; ++r) lds[r * kBlock + t] = key[r];
-                __syncthreads();
-#pragma unroll
-                for (int r = 0; r < kSortKeys; ++r) other[r] = lds[r * kBlock + (t ^ m)];
-            }
-#pragma unroll
-            for (int r = 0; r < kSortKeys; ++r)
-                key[r] = (other[r] < key[r]) == (up == low) ? other[r] : key[r];
+        for (int r = 0; r < kSortKeys; ++r) {
+            if (r & J) continue;
+            const bool up = ((t * kSortKeys + r) & K) == 0;
+            const T x = key[r], y = key[r | J];
+            const bool swap = (y < x) == up;
+            key[r] = swap ? y : x;
+            key[r | J] = swap ? x : y;
         }
-        // distances below kSortKeys: within the thread
+    } else {
+        constexpr int M = J / kSortKeys;   // the other key is that many threads away
+        const bool low = ((t * kSortKeys & K) == 0) == ((t & M) == 0);   // it keeps the lower
+        if constexpr (M >= 64) {
+            __syncthreads();
 #pragma unroll
-        for (int j = kSortKeys / 2; j >= 1; j /= 2) {
-            if (j >= k) continue;
+            for (int r = 0; r < kSortKeys; ++r) lds[r * kBlock + t] = key[r];
+            __syncthreads();
+        }
 #pragma unroll
-            for (int r = 0; r < kSortKeys; ++r)
-                if ((r & j) == 0) order(key[r], key[r | j], ((t * kSortKeys + r) & k) == 0);
+        for (int r = 0; r < kSortKeys; ++r) {
+            T other;
+            if constexpr (M >= 64) other = lds[r * kBlock + (t ^ M)];
+            else other = lane_xor<M>(key[r]);
+            key[r] = (other < key[r]) == low ? other : key[r];
         }
     }
+    if constexpr (J > 1) sort_step<K, J / 2>(key, lds);
+}
+template <int K, typename T>
+__device__ __forceinline__ void sort_run(T (&key)[kSortKeys], T *lds) {
+    if constexpr (K > 2) sort_run<K / 2>(key, lds);
+    sort_step<K, K / 2>(key, lds);
 }
 
-// K: 32 bits where a token and its place in the run fit them, else 64.
-template <typename K>
-__global__ __launch_bounds__(kBlock) void sort_runs_kernel(EmbedGradArgs a, Pair *out) {
-    constexpr int kBits = 11;
+// Runs of kSortRun tokens, a workgroup each.  T: 32 bits where a token and
+// its place in the run fit them, else 64.
+template <typename T>
+__global__ __launch_bounds__(kBlock) void sort_runs_kernel(EmbedGradArgs a, Sorted out) {
+    constexpr int kBits = 10;
     static_assert(kSortRun == 1 << kBits, "");
-    __shared__ K lds[kSortRun];
+    __shared__ T lds[kSortRun];
     const int64_t base = (int64_t)blockIdx.x * kSortRun;
     const int n = (int)(a.n - base < kSortRun ? a.n - base : kSortRun);
-    K key[kSortKeys];
+    T key[kSortKeys];
 #pragma unroll
     for (int r = 0; r < kSortKeys; ++r) {
         const int i = r * kBlock + threadIdx.x;
-        key[r] = ~(K)0;   // above every token's
+        key[r] = ~(T)0;   // above every token's
         if (i < n) {
             const int token = a.tokens.get(base + i, a.vocab);
-            key[r] = (K)(token < 0 ? (uint32_t)a.vocab : (uint32_t)token) << kBits | (K)i;
+            key[r] = (T)(token < 0 ? (uint32_t)a.vocab : (uint32_t)token) << kBits | (T)i;
         }
     }
-    sort_run(key, lds);
+    sort_run<kSortRun>(key, lds);
 #pragma unroll
     for (int r = 0; r < kSortKeys; ++r) {
         const int i = (int)threadIdx.x * kSortKeys + r;
-        if (i < n)
-            out[base + i] = pair_of((uint32_t)(key[r] >> kBits),
-                                    (uint32_t)base + (uint32_t)(key[r] & (kSortRun - 1)));
+        if (i >= n) continue;
+        out.token[base + i] = (uint32_t)(key[r] >> kBits);
+        out.at[base + i] = (uint32_t)base + (uint32_t)(key[r] & (kSortRun - 1));
     }
 }
 
-// Merges kMergeRuns sorted runs of `length` pairs: a pair's place is the
-// number of smaller ones in all of them, found by a binary search in each,
-// all searches a step at a time.
-__global__ __launch_bounds__(kBlock) void merge_runs_kernel(const Pair *in, Pair *out, int64_t n,
+// Merges runs in LDS, kMergeRuns * kSortRun tokens at most: a token's place
+// is the number of tokens before it in every run (the lower ones, and the
+// equal ones of earlier runs), found by binary searches.  SHARE threads share
+// a token's, each doing all of its own a step at a time: the more, the more
+// workgroups there are, which all hold the whole.
+constexpr int kMergeBlock = 1024;
+
+template <int SHARE>
+__global__ __launch_bounds__(kMergeBlock) void merge_runs_kernel(Sorted in, Sorted out, int64_t n) {
+    constexpr int kGroup = kMergeRuns * kSortRun, R = kMergeRuns / SHARE;
+    constexpr int V = kGroup / (4 * kMergeBlock);
+    // runs begin 16 bytes apart in the banks: searches of several of them
+    // begin in the same places (8.6 us of 32,768 tokens without)
+    constexpr int kRun = kSortRun + 4;
+    __shared__ u32x4 vecs[kMergeRuns * kRun / 4];
+    const uint32_t *all = (const uint32_t *)vecs;
+    const int per_block = kMergeBlock / SHARE;
+    const int64_t group = (int64_t)blockIdx.x * per_block / kGroup * kGroup;
+    const int size = (int)(n - group < kGroup ? n - group : kGroup);
+    u32x4 v[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) {   // (the last vector: into the array's padding)
+        const int i = k * kMergeBlock + threadIdx.x;
+        v[k] = *((const u32x4 *)(in.token + group) + (i * 4 < size ? i : 0));
+    }
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+        const int i = k * kMergeBlock + threadIdx.x;
+        vecs[i + i / (kSortRun / 4)] = v[k];
+    }
+    __syncthreads();
+    const int i = (int)((int64_t)blockIdx.x * per_block - group) + (int)threadIdx.x / SHARE;
+    const int own = i / kSortRun, first = threadIdx.x % SHARE;
+    const uint32_t token = i < size ? all[i + own * (kRun - kSortRun)] : 0;
+    uint32_t below[R];
+#pragma unroll
+    for (int k = 0; k < R; ++k) below[k] = 0;
+    for (int step = kSortRun; step > 0; step /= 2) {
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            const int r = first + k * SHARE, at = (int)below[k] + step;
+            const bool inside = (at <= kSortRun) & (r * kSortRun + at <= size);
+            const uint32_t other = all[inside ? r * kRun + at - 1 : 0];
+            if (inside & ((other < token) | ((r < own) & (other == token)))) below[k] = at;
+        }
+    }
+    uint32_t place = 0;
+#pragma unroll
+    for (int k = 0; k < R; ++k)
+        place += first + k * SHARE == own ? (uint32_t)(i % kSortRun) : below[k];
+#pragma unroll
+    for (int m = 1; m < SHARE; m *= 2) place += __shfl_xor(place, m, 64);
+    if (i >= size || first != 0) return;
+    out.token[group + place] = token;
+    out.at[group + place] = in.at[group + i];
+}
+
+// Longer runs where they are, kMergeWide at a time, all searches a step at a
+// time.
+constexpr int kMergeWide = 16;
+
+__global__ __launch_bounds__(kBlock) void merge_long_kernel(Sorted in, Sorted out, int64_t n,
                                                             int64_t length) {
     const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
     if (i >= n) return;
-    const int64_t group = i / (length * kMergeRuns) * (length * kMergeRuns);
+    const int64_t group = i / (length * kMergeWide) * (length * kMergeWide);
     const int64_t left = n - group;
     const int own = (int)((i - group) / length);
-    const int runs = (int)(left < length * kMergeRuns ? (left + length - 1) / length : kMergeRuns);
-    const Pair key = in[i];
-    uint32_t below[kMergeRuns];
+    const int runs = (int)(left < length * kMergeWide ? (left + length - 1) / length : kMergeWide);
+    const uint32_t token = in.token[i];
+    uint32_t below[kMergeWide];
 #pragma unroll
-    for (int r = 0; r < kMergeRuns; ++r) below[r] = 0;
+    for (int r = 0; r < kMergeWide; ++r) below[r] = 0;
     for (int64_t step = length; step > 0; step /= 2) {
 #pragma unroll
-        for (int r = 0; r < kMergeRuns; ++r) {
+        for (int r = 0; r < kMergeWide; ++r) {
             if (r >= runs || r == own) continue;
-            const int64_t at = below[r] + step;   // pairs taken as smaller, if the last one is
-            const int64_t first = group + r * length;
-            if (at <= length && first + at <= n && in[first + at - 1] < key) below[r] += step;
+            const int64_t at = below[r] + step, first = group + r * length;
+            if (at > length || first + at > n) continue;
+            const uint32_t other = in.token[first + at - 1];
+            if (other < token || (r < own && other == token)) below[r] += step;
         }
     }
     int64_t place = i - group - own * length;
 #pragma unroll
-    for (int r = 0; r < kMergeRuns; ++r) place += below[r];
-    out[group + place] = key;
+    for (int r = 0; r < kMergeWide; ++r) place += below[r];
+    out.token[group + place] = token;
+    out.at[group + place] = in.at[i];
 }
 
-// The first of n sorted pairs whose token is not below `token`.
-__device__ __forceinline__ int64_t first_not_below(const Pair *pairs, int64_t n, uint32_t token) {
-    int64_t low = 0, high = n;
-    while (low < high) {
-        const int64_t mid = (low + high) / 2;
-        if (token_of(pairs[mid]) < token) low = mid + 1;
-        else high = mid;
-    }
-    return low;
-}
+// ---------------------------------------------------------------------------
+// its gradient: the sums
 
+// A segment is the sorted positions of one token.  A group of lanes takes the
+// segments that begin in its window of positions, each to its end; a long
+// one is cut at the borders of blocks of two windows, and its pieces, of a
+// block at most, are the windows' that they begin in, to be joined by another
+// launch.  Long: it holds all of a block after the first border in it.  So
+// at a border within a segment it is cut where it also holds the position a
+// block before or after, and few segments are cut at all.
 struct SumArgs {
     EmbedGradArgs a;
-    const Pair *pairs;
-    float *partial;      // [tiles][2][row]: the segment a tile begins in, the one it ends in
-    int64_t tiles, row;
-    int tile, shift;     // positions of a tile; log2 of the lanes that share it
-    int64_t slabs;       // of columns, where 256 lanes do not hold a row
-    int64_t sum_blocks;  // workgroups of tiles; the others fill rows with zeros
+    Sorted sorted;
+    float *partial;      // [blocks][2][row]: the piece from the block's border on, and
+                         // the one before it
+    int64_t row;
+    int shift;           // log2 of a window's positions
+    int64_t windows;
+    int slabs, tail;     // waves that share a row's whole vectors; 1 for the elements after
+    int64_t sum_blocks;  // workgroups of windows; the others fill rows with zeros
     int64_t first;       // the launch's first workgroup
 };
 
-// The sum of a row, scaled, to the result.
+// What nothing writes while a kernel runs, read through the scalar cache
+// where the address is the same in all lanes.
+#define CONSTANT __attribute__((address_space(4)))
+typedef const uint32_t CONSTANT *ConstWords;
+
+// Whether position i holds this token.  (Always a load, so that several of
+// them are on their way at once.)
+__device__ __forceinline__ bool holds(const SumArgs &g, int64_t i, uint32_t token) {
+    const bool inside = (uint64_t)i < (uint64_t)g.a.n;
+    return (((ConstWords)g.sorted.token)[inside ? i : 0] == token) & inside;
+}
+
+// N elements of a row from column col on, scaled, to the result.
 template <typename EO, int N>
 __device__ __forceinline__ void finish_row(const EmbedGradArgs &a, uint32_t token, int64_t col,
-                                           bool whole, float (&x)[N]) {
+                                           const float (&x)[N]) {
     const MutPtr<EO> to = (MutPtr<EO>)a.out + (int64_t)token * a.ldo + col;
-    if (whole) {
+    if constexpr (N == 1) {
+        const float v = x[0] * a.scale;
+        *to = EO::put(a.accumulate ? EO::get(*to) + v : v);
+    } else {
         float y[N] = {};
         if (a.accumulate) load_floats<EO, N>((Ptr<EO>)to, y);
 #pragma unroll
         for (int j = 0; j < N; ++j) y[j] = a.accumulate ? y[j] + x[j] * a.scale : x[j] * a.scale;
         store_floats<EO, N>(to, y);
-        return;
     }
-#pragma unroll
-    for (int j = 0; j < N; ++j)
-        if (col + j < a.d) {
-            const float v = x[j] * a.scale;
-            to[j] = EO::put(a.accumulate ? EO::get(to[j]) + v : v);
-        }
 }
 
-constexpr int kZeroRows = 64;   // rows of a workgroup that fills in zeros
+constexpr int kZeroRows = 16;   // rows of a workgroup that fills in zeros
+
+// The first position whose token is not below `token`; a wave looks at 64
+// places at once.
+__device__ __forceinline__ int64_t first_not_below(const uint32_t *sorted, int64_t n, uint32_t token) {
+    int64_t low = 0, high = n;   // the answer lies in [low, high]
+    while (low < high) {
+        const int64_t step = (high - low + 63) / 64;
+        const int64_t at = low + (int64_t)(threadIdx.x % 64) * step;
+        const int below = __popcll(__ballot(at < high && sorted[at] < token));
+        if (below == 0) return low;
+        const int64_t last = low + (below - 1) * step;   // the last place looked at that is below
+        low = last + 1;
+        high = last + step < high ? last + step : high;
+    }
+    return low;
+}
 
 template <typename EO>
 __device__ __forceinline__ void zero_rows(const SumArgs &g, int64_t block) {
-    __shared__ uint64_t there;
+    __shared__ uint32_t there;
     const EmbedGradArgs &a = g.a;
     const int64_t first = block * kZeroRows;
+    const int rows = (int)(a.vocab - first < kZeroRows ? a.vocab - first : kZeroRows);
     if (threadIdx.x < 64) {
-        const uint32_t token = (uint32_t)first + threadIdx.x;
-        const int64_t at = first_not_below(g.pairs, a.n, token);
-        const uint64_t mask = __ballot(at < a.n && token_of(g.pairs[at]) == token);
+        const uint32_t *sorted = g.sorted.token;
+        int64_t low = first_not_below(sorted, a.n, (uint32_t)first);
+        uint32_t mask = 0;
+        while (low < a.n) {   // from one of the rows' tokens to the next
+            const uint32_t token = sorted[low];
+            if (token >= (uint32_t)(first + rows)) break;
+            const int64_t at = low + threadIdx.x % 64;
+            const uint32_t mine = at < a.n ? sorted[at] : ~0u;
+#pragma unroll
+            for (int r = 0; r < kZeroRows; ++r)
+                mask |= (uint32_t)(__ballot(mine == (uint32_t)first + r) != 0) << r;
+            // all 64 are of these rows: go on, past what the last one fills
+            if (low + 63 >= a.n) break;
+            const uint32_t last = sorted[low + 63];
+            if (last >= (uint32_t)(first + rows)) break;
+            low = last == token ? first_not_below(sorted, a.n, last + 1) : low + 64;
+        }
         if (threadIdx.x == 0) there = mask;
     }
     __syncthreads();
-    const int rows = (int)(a.vocab - first < kZeroRows ? a.vocab - first : kZeroRows);
+    const uint32_t mask = there;
     const float zero[EO::V] = {};
     const int64_t nv = a.d / EO::V;
     for (int r = 0; r < rows; ++r) {
-        if (there >> r & 1) continue;
+        if (mask >> r & 1) continue;
         const MutPtr<EO> to = (MutPtr<EO>)a.out + (first + r) * a.ldo;
-        for (int64_t v = threadIdx.x; v < nv; v += kBlock) store_floats<EO>(to + v * EO::V, zero);
+        for (int64_t v = threadIdx.x; v < nv; v += kBlock)
+            store_floats<EO>(to + v * EO::V, zero);
         for (int64_t i = nv * EO::V + threadIdx.x; i < a.d; i += kBlock) to[i] = EO::put(0.0f);
     }
 }
 
-template <typename EI, typename EO>
-__global__ __launch_bounds__(kBlock) void sum_tiles_kernel(SumArgs g) {
-    constexpr int N = EI::V > EO::V ? EI::V : EO::V, U = 4;
+// N columns of a lane from col on, of the segments and pieces that begin in
+// a window: the same window in all lanes.
+template <typename EI, typename EO, int N>
+__device__ __forceinline__ void sum_window(const SumArgs &g, int64_t window, int64_t col) {
+    constexpr int W = N == 1 ? 1 : N / EI::V, U = 8;
     const EmbedGradArgs &a = g.a;
+    const uint32_t none = (uint32_t)a.vocab;
+    const int64_t span = int64_t(2) << g.shift;   // positions of a block
+    const int64_t p0 = window << g.shift, p1 = p0 + span / 2 < a.n ? p0 + span / 2 : a.n;
+    const ConstWords tokens = (ConstWords)g.sorted.token, places = (ConstWords)g.sorted.at;
+
+    const bool border = (window & 1) == 0;
+    const int64_t next = border ? p0 + span : p0 + span / 2;   // the border from p1 on
+    auto look = [&](int64_t i) { return tokens[(uint64_t)i < (uint64_t)a.n ? i : p0]; };
+    auto inside = [&](int64_t i) { return (uint64_t)i < (uint64_t)a.n; };
+    uint32_t token = tokens[p0], last = tokens[p1 - 1], w0 = look(p0 - 1), w1 = look(p0 - span),
+             w2 = look(p0 + span), w3 = look(p1), w4 = look(next), w5 = look(next - span),
+             w6 = look(next + span);
+    // all of them on their way before the first is waited for
+    asm volatile("" : "+s"(token), "+s"(last), "+s"(w0), "+s"(w1), "+s"(w2), "+s"(w3), "+s"(w4),
+                 "+s"(w5), "+s"(w6));
+    if (token >= none) return;
+    const uint32_t first = token;
+    const bool begun = inside(p0 - 1) & (w0 == first), before = inside(p0 - span) & (w1 == first),
+               after = inside(p0 + span) & (w2 == first), goes_on = inside(p1) & (w3 == last);
+    const bool at_next = inside(next) & (w4 == last), by_next = inside(next - span) & (w5 == last),
+               past_next = inside(next + span) & (w6 == last);
+    // the segment at p0: begun before, and not cut here, it is another window's
+    const bool long_one = border & (after | (begun & before));
+    const bool skip = begun & !long_one;
+    // where the last one ends, at the latest, and whether it is cut there
+    const bool tail_cut = goes_on & at_next & (by_next | past_next);
+    const int64_t end = !goes_on ? p1 : tail_cut ? next : next + span < a.n ? next + span : a.n;
+
+    enum { kSkip, kPiece, kSegment } kind = skip ? kSkip : long_one ? kPiece : kSegment;
+    float acc[N] = {};
+    auto flush = [&](bool cut) {
+        if (kind == kSkip) return;
+        if (kind == kSegment && !cut) {
+            finish_row<EO, N>(a, token, col, acc);
+            return;
+        }
+        const int64_t slot = kind == kPiece ? window : (end >> (g.shift + 1)) * 2 + 1;
+        float GLOBAL *to = (float GLOBAL *)g.partial + slot * g.row + col;
+        if constexpr (N == 1) *to = acc[0];
+        else store_floats<F32, N>(to, acc);
+    };
+    for (int64_t p = p0; p < end; p += U) {
+        typedef uint32_t Eight __attribute__((ext_vector_type(8), aligned(4)));
+        // (past the end of the array: its padding)
+        const Eight tok = *(const Eight CONSTANT *)(tokens + p);
+        const Eight place = *(const Eight CONSTANT *)(places + p);
+        uint32_t now[U];
+        typename EI::T one[U];
+        u32x4 x[U][W];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            now[u] = tok[u];
+            // no more of this window, or not its
+            if ((p + u >= end) | ((p + u >= p1) & (now[u] != last))) now[u] = none;
+            const Ptr<EI> from = (Ptr<EI>)a.grad + (int64_t)place[u] * a.ld + col;
+            if constexpr (N == 1) one[u] = EI::put(0.0f);
+#pragma unroll
+            for (int i = 0; i < W; ++i) x[u][i] = (u32x4){0, 0, 0, 0};
+            if ((now[u] >= none) | (skip & (now[u] == first))) continue;
+            if constexpr (N == 1) {
+                one[u] = *from;
+            } else {
+#pragma unroll
+                for (int i = 0; i < W; ++i) x[u][i] = load_vec<EI, Use::Once>(from + i * EI::V);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (now[u] != token) {
+                flush(false);
+                if (now[u] >= none) return;
+#pragma unroll
+                for (int j = 0; j < N; ++j) acc[j] = 0.0f;
+                token = now[u];
+                kind = kSegment;
+            }
+            if constexpr (N == 1) {
+                acc[0] += EI::get(one[u]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < W; ++i) {
+                    float y[EI::V];
+                    EI::unpack(x[u][i], y);
+#pragma unroll
+                    for (int j = 0; j < EI::V; ++j) acc[i * EI::V + j] += y[j];
+                }
+            }
+        }
+    }
+    flush(tail_cut);
+}
+
+// A wave for every window and 64 vectors of a row.  Reading the gradient's
+// rows bounds it, with what the table's rows take.
+template <typename EI, typename EO>
+__global__ __launch_bounds__(kBlock) void sum_rows_kernel(SumArgs g) {
+    constexpr int N = EI::V > EO::V ? EI::V : EO::V;
     const int64_t block = g.first + blockIdx.x;
     if (block >= g.sum_blocks) {
         zero_rows<EO>(g, block - g.sum_blocks);
         return;
     }
-    const int lane = (int)threadIdx.x & ((1 << g.shift) - 1);
-    const int64_t item = (block * kBlock + threadIdx.x) >> g.shift;
-    const int64_t tile = item / g.slabs;
-    const int64_t col = (item % g.slabs * (1 << g.shift) + lane) * N;
-    if (tile >= g.tiles || col >= a.d) return;
-    const bool whole = col + N <= a.d;
-    const int64_t p0 = tile * g.tile;
-    const int64_t p1 = p0 + g.tile < a.n ? p0 + g.tile : a.n;
-    float acc[N] = {};
-    uint32_t token = token_of(g.pairs[p0]);
-    // whether the segment at hand began before the tile
-    bool open = p0 > 0 && token_of(g.pairs[p0 - 1]) == token;
-    auto flush = [&](bool goes_on) {
-        if (!open && !goes_on) {
-            finish_row<EO, N>(a, token, col, whole, acc);
-            return;
-        }
-        float GLOBAL *to = (float GLOBAL *)g.partial + (tile * 2 + (open ? 0 : 1)) * g.row + col;
-#pragma unroll
-        for (int j = 0; j < N; ++j)
-            if (col + j < a.d) to[j] = acc[j];
-    };
-    for (int64_t p = p0; p < p1; p += U) {
-        Pair pair[U];
-        float x[U][N];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            pair[u] = g.pairs[p + u < p1 ? p + u : p1 - 1];
-            const bool real = token_of(pair[u]) < (uint32_t)a.vocab;
-            const Ptr<EI> from = (Ptr<EI>)a.grad + (int64_t)(uint32_t)pair[u] * a.ld + col;
-#pragma unroll
-            for (int j = 0; j < N; ++j) x[u][j] = 0.0f;
-            if (!real || p + u >= p1) continue;
-            if (whole) {
-                load_floats<EI, N, Use::Once>(from, x[u]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < N; ++j)
-                    if (col + j < a.d) x[u][j] = EI::get(from[j]);
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (p + u >= p1) continue;
-            if (token_of(pair[u]) != token) {
-                flush(false);
-#pragma unroll
-                for (int j = 0; j < N; ++j) acc[j] = 0.0f;
-                token = token_of(pair[u]);
-                open = false;
-            }
-            if (token >= (uint32_t)a.vocab) return;   // none: the last segment
-#pragma unroll
-            for (int j = 0; j < N; ++j) acc[j] += x[u][j];
-        }
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
+    const int64_t item = block * (kBlock / 64) + wave;
+    const int64_t window = item / (g.slabs + g.tail);
+    const int slab = (int)(item % (g.slabs + g.tail));
+    if (window >= g.windows) return;
+    const int64_t whole = g.a.d / N * N;
+    if (slab < g.slabs) {
+        const int64_t col = ((int64_t)slab * 64 + lane) * N;
+        if (col < whole) sum_window<EI, EO, N>(g, window, col);
+    } else if (whole + lane < g.a.d) {
+        sum_window<EI, EO, 1>(g, window, whole + lane);
     }
-    flush(p1 < a.n && token_of(g.pairs[p1]) == token);
 }
 
-// Joins the sums of a segment that several tiles hold, in their order: a
-// workgroup for each tile that such a segment begins in and 256 columns.
+// Joins the pieces of a long segment in their order: a workgroup for the
+// first border in it and 256 columns.
 template <typename EO>
-__global__ __launch_bounds__(kBlock) void join_tiles_kernel(SumArgs g, int64_t slabs) {
-    constexpr int N = EO::V > 4 ? 4 : EO::V, WAVES = kBlock / 64;
+__global__ __launch_bounds__(kBlock) void join_pieces_kernel(SumArgs g, int64_t slabs) {
+    constexpr int N = 4, WAVES = kBlock / 64;
     __shared__ float sums[WAVES][64 * N];
     const EmbedGradArgs &a = g.a;
-    const int64_t block = g.first + blockIdx.x;
-    const int64_t tile = block / slabs;
+    const int64_t item = g.first + blockIdx.x;
+    const int64_t block = item / slabs, span = int64_t(2) << g.shift;
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const int64_t col = (block % slabs * 64 + lane) * N;
-    const int64_t p0 = tile * g.tile, p1 = p0 + g.tile;
-    if (p1 >= a.n) return;   // the last tile: nothing goes on
-    const uint32_t token = token_of(g.pairs[p1 - 1]);
-    if (token >= (uint32_t)a.vocab || token_of(g.pairs[p1]) != token) return;
-    // it began in an earlier tile
-    if (token_of(g.pairs[p0]) == token && p0 > 0 && token_of(g.pairs[p0 - 1]) == token) return;
-    // the tiles after this one that begin with it
-    int64_t low = tile + 1, high = g.tiles;   // low begins with it
-    while (high - low > 1) {
-        const int64_t mid = (low + high) / 2;
-        if (token_of(g.pairs[mid * g.tile]) == token) low = mid;
-        else high = mid;
+    const int64_t col = (item % slabs * 64 + lane) * N;
+    const int64_t p = block * span;
+    const ConstWords tokens = (ConstWords)g.sorted.token;
+    const uint32_t token = tokens[p];
+    if (token >= (uint32_t)a.vocab || !holds(g, p + span, token) || holds(g, p - span, token)) return;
+    const int64_t head = holds(g, p - 1, token);   // a piece before the border
+    // the blocks that begin with it: `high` is past them
+    const int64_t blocks = (a.n + span - 1) / span;
+    int64_t low = block + 1, high = blocks;   // low begins with it
+    const int64_t near = low + lane;
+    const uint64_t are = __ballot(near < blocks && g.sorted.token[near < blocks ? near * span : p] == token);
+    if (~are != 0) {
+        high = low + __ffsll((unsigned long long)~are) - 1;
+    } else {
+        low += 63;
+        while (high - low > 1) {
+            const int64_t mid = (low + high) / 2;
+            if (tokens[mid * span] == token) low = mid;
+            else high = mid;
+        }
     }
-    const int64_t count = high - tile;   // sums: this tile's second, the others' first
+    const int64_t count = high - block + head;
     const int64_t share = (count + WAVES - 1) / WAVES;
     const int64_t from = wave * share, to = from + share < count ? from + share : count;
     float acc[N] = {};
     if (col < a.d) {
-        for (int64_t k = from; k < to; ++k) {
-            const float *p = g.partial + ((tile + k) * 2 + (k == 0 ? 1 : 0)) * g.row + col;
+        constexpr int U = 8;
+        for (int64_t k = from; k < to; k += U) {
+            u32x4 w[U];
 #pragma unroll
-            for (int j = 0; j < N; ++j) acc[j] += p[j];
+            for (int u = 0; u < U; ++u) {
+                const int64_t i = k + u < to ? k + u : to - 1;
+                const int64_t slot = head && i == 0 ? block * 2 + 1 : (block + i - head) * 2;
+                w[u] = *(const u32x4 GLOBAL *)((const float GLOBAL *)g.partial + slot * g.row + col);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (k + u < to)
+#pragma unroll
+                    for (int j = 0; j < N; ++j) acc[j] += __uint_as_float(w[u][j]);
         }
     }
 #pragma unroll
@@ -404,48 +610,99 @@ __device__ __forceinline__ u32x4 philox(uint64_t key, uint64_t counter) {
     return (u32x4){c0, c1, c2, c3};
 }
 
-// Eight positions share a block of random bits; `shift` lanes (log2) take a
-// row's blocks, or, 256 of them, one of its `chunks`.
+// A row's blocks of eight positions, which share random bits: 2^shift lanes
+// take `chunks` groups of them.  The elements of a row's first and last block,
+// where those are cut, are few among many for a long row: there they go to
+// workgroups of their own, a lane each, since a wave that does both kinds
+// takes the time of both (10,007 rows of 2,049 f16: 21.9 against 19 us).
+struct DropPlan {
+    int shift;
+    int64_t chunks;
+    double inverse;        // 1 / chunks
+    bool apart;            // cut blocks on their own
+    int64_t whole_blocks;  // workgroups of the others
+};
+
 template <typename E, bool RES>
-__global__ __launch_bounds__(kBlock) void dropout_kernel(DropoutArgs a, int shift, int64_t chunks) {
+__global__ __launch_bounds__(kBlock) void dropout_kernel(DropoutArgs a, DropPlan plan) {
     const uint64_t key = a.seed_at != nullptr ? *a.seed_at : a.seed;
-    const int lane = (int)threadIdx.x & ((1 << shift) - 1);
-    const int per_block = kBlock >> shift;
-    for (int64_t item = (int64_t)blockIdx.x * per_block + (threadIdx.x >> shift);
-         item < a.rows * chunks; item += (int64_t)gridDim.x * per_block) {
-        const int64_t row = item / chunks;
+    auto kept = [&](uint32_t word, int j) { return (word >> (j % 2 * 16) & 0xFFFFu) >= a.limit; };
+    if (blockIdx.x >= plan.whole_blocks) {
+        // 16 lanes a row: positions of the block it begins in, and of the one
+        // it ends in (rows of a block at least)
+        for (int64_t i = ((int64_t)blockIdx.x - plan.whole_blocks) * kBlock + threadIdx.x;
+             i < a.rows * 16; i += ((int64_t)gridDim.x - plan.whole_blocks) * kBlock) {
+            const int64_t row = i / 16;
+            const uint64_t q0 = a.offset + (uint64_t)row * (uint64_t)a.d;
+            const int head = (int)(q0 & 7), skip = (int)(-q0 & 7);
+            const int64_t at = i % 16 < 8 ? i % 8 - head : skip + (a.d - skip) / 8 * 8 + i % 8;
+            if (at < 0 || at >= (i % 16 < 8 ? skip : a.d)) continue;
+            const uint64_t q = q0 + (uint64_t)at;
+            const u32x4 bits = philox(key, q >> 3);
+            const int j = (int)(q & 7);
+            const uint32_t word = j < 4 ? (j < 2 ? bits.x : bits.y) : (j < 6 ? bits.z : bits.w);
+            float y = kept(word, j) ? E::get(((Ptr<E>)a.x)[row * a.ld + at]) * a.scale : 0.0f;
+            if constexpr (RES) y += E::get(((Ptr<E>)a.residual)[row * a.ldr + at]);
+            ((MutPtr<E>)a.out)[row * a.ldo + at] = E::put(y);
+        }
+        return;
+    }
+    const int lane = (int)threadIdx.x & ((1 << plan.shift) - 1);
+    const int per_block = kBlock >> plan.shift;
+    for (int64_t item = (int64_t)blockIdx.x * per_block + (threadIdx.x >> plan.shift);
+         item < a.rows * plan.chunks; item += plan.whole_blocks * per_block) {
+        int64_t row = 0, block = item;
+        if (a.rows > 1) {   // fewer than 2^31 items: off by one at most
+            row = (int)((double)item * plan.inverse);
+            block = item - row * plan.chunks;
+            if (block < 0) --row, block += plan.chunks;
+            else if (block >= plan.chunks) ++row, block -= plan.chunks;
+        }
+        block = (block << plan.shift) + lane;
         const uint64_t q0 = a.offset + (uint64_t)row * (uint64_t)a.d;
         const int head = (int)(q0 & 7);
-        const int64_t block = item % chunks * kBlock + lane;
         const int64_t i0 = block * 8 - head;   // the row's element at the block's start
-        if (i0 >= a.d) continue;
+        const bool whole = i0 >= 0 && i0 + 8 <= a.d;
+        if (i0 >= a.d || (plan.apart && !whole)) continue;
         // (counters wrap as positions do)
         const u32x4 bits = philox(key, ((q0 >> 3) + (uint64_t)block) & (~uint64_t(0) >> 3));
         const Ptr<E> x = (Ptr<E>)a.x + row * a.ld + i0;
         const Ptr<E> r = (Ptr<E>)a.residual + row * a.ldr + i0;
         const MutPtr<E> out = (MutPtr<E>)a.out + row * a.ldo + i0;
-        auto kept = [&](int j) { return (bits[j / 2] >> (j % 2 * 16) & 0xFFFFu) >= a.limit; };
-        if (i0 >= 0 && i0 + 8 <= a.d) {
+        if (whole) {
             float v[8], add[8];
             load_floats<E, 8, Use::Once>(x, v);
             if constexpr (RES) load_floats<E, 8, Use::Once>(r, add);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                v[j] = kept(j) ? v[j] * a.scale : 0.0f;
+                v[j] = kept(bits[j / 2], j) ? v[j] * a.scale : 0.0f;
                 if constexpr (RES) v[j] += add[j];
             }
             store_floats<E, 8, Use::Once>(out, v);
             continue;
         }
+        // all elements loaded before one is stored
+        typename E::T v[8], add[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            if (i0 + j < 0 || i0 + j >= a.d) continue;
-            float v = kept(j) ? E::get(x[j]) * a.scale : 0.0f;
-            if constexpr (RES) v += E::get(r[j]);
-            out[j] = E::put(v);
+            const bool inside = (i0 + j >= 0) & (i0 + j < a.d);
+            const int64_t at = inside ? j : i0 < 0 ? head : 0;   // else one that is
+            v[j] = x[at];
+            if constexpr (RES) add[j] = r[at];
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            float y = kept(bits[j / 2], j) ? E::get(v[j]) * a.scale : 0.0f;
+            if constexpr (RES) y += E::get(add[j]);
+            if ((i0 + j >= 0) & (i0 + j < a.d)) out[j] = E::put(y);
         }
     }
 }
+
+template <int N>
+struct Int {
+    static constexpr int value = N;
+};
 
 // Calls launch(first, n) until `blocks` workgroups are launched.
 template <typename F>
@@ -479,13 +736,30 @@ hipError_t start_dropout(DropoutArgs a, hipStream_t s) {
         a.rows = 1;
         a.ld = a.ldr = a.ldo = a.d;
     }
+    DropPlan plan;
     const int64_t blocks = (a.d + 14) / 8;   // of a row, wherever it begins
-    const int shift = lane_shift(blocks);
-    const int64_t chunks = (blocks + (1 << shift) - 1) >> shift;
-    const unsigned grid = grid_for(a.rows * chunks, kBlock >> shift);
-    if (a.residual != nullptr) dropout_kernel<E, true><<<grid, kBlock, 0, s>>>(a, shift, chunks);
-    else dropout_kernel<E, false><<<grid, kBlock, 0, s>>>(a, shift, chunks);
-    return hipGetLastError();
+    plan.shift = lane_shift(blocks) < 3 ? lane_shift(blocks) : 3;
+    plan.chunks = (blocks + (1 << plan.shift) - 1) >> plan.shift;
+    plan.inverse = 1.0 / (double)plan.chunks;
+    // rows of a launch, fewer than 2^31 chunks together
+    const int64_t most = int64_t(1) << 30, rows = a.rows;
+    const int64_t step = plan.chunks > most ? 1 : most / plan.chunks;
+    for (int64_t first = 0; first < rows; first += step) {
+        DropoutArgs b = a;
+        b.rows = rows - first < step ? rows - first : step;
+        b.x = (const typename E::T *)a.x + first * a.ld;
+        b.out = (typename E::T *)a.out + first * a.ldo;
+        if (a.residual != nullptr) b.residual = (const typename E::T *)a.residual + first * a.ldr;
+        b.offset += (uint64_t)first * (uint64_t)a.d;
+        plan.apart = a.d >= 64 && (b.offset % 8 != 0 || a.d % 8 != 0);
+        plan.whole_blocks = grid_for(b.rows * plan.chunks, kBlock >> plan.shift);
+        const unsigned grid = (unsigned)plan.whole_blocks + (plan.apart ? grid_for(b.rows * 16, kBlock) : 0);
+        if (a.residual != nullptr) dropout_kernel<E, true><<<grid, kBlock, 0, s>>>(b, plan);
+        else dropout_kernel<E, false><<<grid, kBlock, 0, s>>>(b, plan);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace
@@ -497,7 +771,10 @@ hipError_t launch_embed(const EmbedArgs &a, hipStream_t s) {
         typedef decltype(to) EO;
         constexpr int N = EI::V > EO::V ? EI::V : EO::V;
         const int shift = lane_shift((a.d + N - 1) / N);
-        embed_kernel<EI, EO><<<grid_for(a.n, kBlock >> shift), kBlock, 0, s>>>(a, shift);
+        const int per_block = kBlock >> shift;
+        if (a.n >= kPairRows * per_block)
+            embed_kernel<EI, EO, 2><<<grid_for(a.n, 2 * per_block), kBlock, 0, s>>>(a, shift);
+        else embed_kernel<EI, EO, 1><<<grid_for(a.n, per_block), kBlock, 0, s>>>(a, shift);
         return hipGetLastError();
     });
 }
@@ -505,48 +782,64 @@ hipError_t launch_embed(const EmbedArgs &a, hipStream_t s) {
 hipError_t launch_embed_grad(const EmbedGradArgs &a, hipStream_t s) {
     if (a.vocab == 0 || a.d == 0 || (a.n == 0 && a.accumulate)) return hipSuccess;
     const EmbedGradPlan plan = embed_grad_plan(a.n, a.d);
-    Pair *pairs = (Pair *)a.ws, *other = (Pair *)((char *)a.ws + plan.pairs);
-    hipError_t e = hipSuccess;
+    char *ws = (char *)a.ws;
+    auto array = [&](int i) { return (uint32_t *)(ws + i * plan.words); };
+    Sorted sorted{array(0), array(1)}, other{array(2), array(3)};
+    auto merged = [&]() {
+        const Sorted swap = sorted;
+        sorted = other;
+        other = swap;
+        return hipGetLastError();
+    };
     if (a.n > 0) {
         const unsigned runs = (unsigned)((a.n + kSortRun - 1) / kSortRun);
-        if (a.vocab < (1 << 21) - 1) sort_runs_kernel<uint32_t><<<runs, kBlock, 0, s>>>(a, pairs);
-        else sort_runs_kernel<uint64_t><<<runs, kBlock, 0, s>>>(a, pairs);
-        e = hipGetLastError();
-        for (int64_t length = kSortRun; length < a.n && e == hipSuccess; length *= kMergeRuns) {
-            merge_runs_kernel<<<(unsigned)((a.n + kBlock - 1) / kBlock), kBlock, 0, s>>>(
-                pairs, other, a.n, length);
-            e = hipGetLastError();
-            Pair *const swap = pairs;
-            pairs = other;
-            other = swap;
+        if (a.vocab < (1 << 22) - 1) sort_runs_kernel<uint32_t><<<runs, kBlock, 0, s>>>(a, sorted);
+        else sort_runs_kernel<uint64_t><<<runs, kBlock, 0, s>>>(a, sorted);
+        hipError_t e = hipGetLastError();
+        if (e == hipSuccess && a.n > kSortRun) {
+            auto merge = [&](auto share) {   // about a workgroup per compute unit
+                constexpr int S = decltype(share)::value, kTokens = kMergeBlock / S;
+                const unsigned blocks = (unsigned)((a.n + kTokens - 1) / kTokens);
+                merge_runs_kernel<S><<<blocks, kMergeBlock, 0, s>>>(sorted, other, a.n);
+            };
+            if (a.n <= 256 * kMergeBlock / 8) merge(Int<8>());
+            else if (a.n <= 256 * kMergeBlock / 4) merge(Int<4>());
+            else merge(Int<2>());
+            e = merged();
+        }
+        for (int64_t length = kSortRun * kMergeRuns; length < a.n && e == hipSuccess;
+             length *= kMergeWide) {
+            merge_long_kernel<<<(unsigned)((a.n + kBlock - 1) / kBlock), kBlock, 0, s>>>(
+                sorted, other, a.n, length);
+            e = merged();
         }
         if (e != hipSuccess) return e;
     }
     SumArgs g{};
     g.a = a;
-    g.pairs = pairs;
-    g.partial = (float *)((char *)a.ws + 2 * plan.pairs);
-    g.tiles = plan.tiles;
-    g.tile = plan.tile;
+    g.sorted = sorted;
+    g.partial = (float *)(ws + 4 * plan.words);
+    g.shift = plan.shift;
+    g.windows = (a.n + (1 << plan.shift) - 1) >> plan.shift;
     g.row = embed_row(a.d);
     return with_types(a.dtype, a.out_dtype, [&](auto from, auto to) {
         typedef decltype(from) EI;
         typedef decltype(to) EO;
         constexpr int N = EI::V > EO::V ? EI::V : EO::V;
-        const int64_t vecs = (a.d + N - 1) / N;
-        g.shift = lane_shift(vecs);
-        g.slabs = (vecs + (1 << g.shift) - 1) >> g.shift;
-        g.sum_blocks = (g.tiles * g.slabs + (kBlock >> g.shift) - 1) >> (8 - g.shift);
+        g.slabs = (int)((a.d / N + 63) / 64);
+        g.tail = a.d % N != 0;
+        g.sum_blocks = (g.windows * (g.slabs + g.tail) + kBlock / 64 - 1) / (kBlock / 64);
         const int64_t zero = a.accumulate ? 0 : (a.vocab + kZeroRows - 1) / kZeroRows;
         const hipError_t st = over_blocks(g.sum_blocks + zero, [&](int64_t first, unsigned n) {
             g.first = first;
-            sum_tiles_kernel<EI, EO><<<n, kBlock, 0, s>>>(g);
+            sum_rows_kernel<EI, EO><<<n, kBlock, 0, s>>>(g);
         });
-        if (st != hipSuccess || g.tiles <= 1) return st;
+        // a long segment holds more than a block
+        if (st != hipSuccess || a.n <= (2 << g.shift)) return st;
         const int64_t slabs = (a.d + 255) / 256;
-        return over_blocks(g.tiles * slabs, [&](int64_t first, unsigned n) {
+        return over_blocks(plan.blocks * slabs, [&](int64_t first, unsigned n) {
             g.first = first;
-            join_tiles_kernel<EO><<<n, kBlock, 0, s>>>(g, slabs);
+            join_pieces_kernel<EO><<<n, kBlock, 0, s>>>(g, slabs);
         });
     });
 }
