@@ -9,6 +9,7 @@ the library -- there is no fallback.
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 from dataclasses import dataclass
 
@@ -1006,23 +1007,73 @@ def clipped_adamw(params, grads, mean, square, *, step: int, lr: float, betas=(0
 
 # ------------------------------------------ a worker's step on token data
 
-def _token_buffer(tokens, n: int, device) -> tuple[int, int]:
-    """Address and type code of the n tokens of a call."""
-    torch = _torch()
-    if not isinstance(tokens, torch.Tensor) or tokens.numel() != n:
-        raise AspisError(ERR_INVALID_ARG, f"tokens must be a tensor of {n} tokens")
-    wide = tokens.dtype == torch.int64
-    if not wide and tokens.dtype != torch.int32:
-        raise AspisError(ERR_INVALID_ARG, f"tokens must be int32 or int64, not {tokens.dtype}")
-    return _buffer("tokens", tokens, tokens.dtype, n, device), int(wide)
-
-
-def _matrix(name: str, x, device=None):
-    """rows, d, elements between rows and type code of [rows, d] on a device."""
+def _place(name: str, x):
+    """Address, rows, d, elements between rows, type code and device index of a
+    tensor of rows [..., d]."""
+    place = _tensors().place(x)
+    if place is not None:
+        return place
     rows, d, ld, code = _rows(name, x)
-    if x.dim() != 2 or (device is not None and x.device != device):
-        raise AspisError(ERR_INVALID_ARG, f"{name} must be [rows, d], on the device of the others")
-    return rows, d, ld, code
+    return x.data_ptr(), rows, d, ld, code, x.device.index
+
+
+def _token_place(tokens, n: int, index: int):
+    """Address and type code of the n tokens of a call on device `index`."""
+    place = _tensors().tokens(tokens)
+    if place is None or place[1] != n or place[3] != index:
+        torch = _torch()
+        what = f"{tokens.dtype}, {tuple(tokens.shape)}, {tokens.device}" \
+            if isinstance(tokens, torch.Tensor) else type(tokens).__name__
+        raise AspisError(ERR_INVALID_ARG, f"tokens must be a contiguous int32 or int64 tensor of {n} "
+                                          f"tokens on cuda:{index} (got {what})")
+    return place[0], place[2]
+
+
+def _floats(name: str, t, n: int, index: int) -> int:
+    """The address of a contiguous float32 tensor of n elements at least."""
+    at = _tensors().buffer(t, _float32(), n, index)
+    return at if at is not None else \
+        _buffer(name, t, _float32(), n, _torch().device("cuda", index))
+
+
+def _scratch_at(ws, index: int) -> int:
+    """The address of a workspace (its size is the library's to check)."""
+    at = _tensors().buffer(ws, _uint8(), 0, index)
+    return at if at is not None else \
+        _buffer("ws", ws, _uint8(), 0, _torch().device("cuda", index))
+
+
+_kinds: list = []
+
+
+def _float32():
+    if not _kinds:
+        torch = _torch()
+        _kinds.extend([torch.float32, torch.uint8])
+    return _kinds[0]
+
+
+def _uint8():
+    _float32()
+    return _kinds[1]
+
+
+_cuda: list = []
+
+
+def _enqueue(index: int, call, *args):
+    """Calls a library function with the current stream of a device as its last
+    argument, and checks its status."""
+    if not _cuda:
+        c = _torch()._C
+        _cuda.extend([c._cuda_getDevice, c._cuda_getCurrentRawStream])
+    if _cuda[0]() == index:
+        status = call(*args, _cuda[1](index))
+    else:
+        with _torch().cuda.device(index):
+            status = call(*args, _cuda[1](index))
+    if status != OK:
+        _check(status)
 
 
 def embed(table, tokens, scale: float = 1.0, out=None):
@@ -1032,17 +1083,19 @@ def embed(table, tokens, scale: float = 1.0, out=None):
     one that another rank's part of the table holds (subtract the part's first
     token, add the ranks' results).  Its gradient is embed_grad; autograd does
     not see either."""
-    torch = _torch()
-    vocab, d, ld, code = _matrix("table", table)
-    n = tokens.numel() if isinstance(tokens, torch.Tensor) else 0
-    at, wide = _token_buffer(tokens, n, table.device)
+    at, vocab, d, ld, code, index = _place("table", table)
+    if table.dim() != 2:
+        raise AspisError(ERR_INVALID_ARG, f"table must be [vocab, d], not {tuple(table.shape)}")
     if out is None:
-        out = torch.empty((*tokens.shape, d), dtype=table.dtype, device=table.device)
-    rows, width, ldo, out_code = _rows("out", out)
-    if rows != n or width != d or out.device != table.device:
-        raise AspisError(ERR_INVALID_ARG, f"out must hold {n} rows of {d} on {table.device}")
-    _launch(table.device, lib().aspis_embed, table.data_ptr(), vocab, d, ld, code, at, n, wide,
-            scale, out.data_ptr(), ldo, out_code, _raw_stream(table.device))
+        torch = _torch()
+        shape = tokens.shape if isinstance(tokens, torch.Tensor) else ()
+        out = torch.empty((*shape, d), dtype=table.dtype, device=table.device)
+    to, n, width, ldo, out_code, out_index = _place("out", out)
+    ids, wide = _token_place(tokens, n, index)
+    if width != d or out_index != index:
+        raise AspisError(ERR_INVALID_ARG, f"out must hold rows of {d} on {table.device}")
+    _enqueue(index, lib().aspis_embed, at, vocab, d, ld, code, ids, n, wide, scale, to, ldo,
+             out_code)
     return out
 
 
@@ -1050,7 +1103,7 @@ def embed_workspace(grad, tokens, vocab: int):
     """Workspace of embed_grad for a gradient [..., d] of these tokens (of any
     vocabulary)."""
     torch = _torch()
-    rows, d, _, _ = _rows("grad", grad)
+    _, rows, d, _, _, index = _place("grad", grad)
     n = int(lib().aspis_embed_workspace(rows, d))
     if n == ctypes.c_size_t(-1).value:
         raise AspisError(ERR_OVERFLOW, f"{rows} tokens of {d} are too many")
@@ -1064,23 +1117,20 @@ def embed_grad(grad, tokens, vocab: int, scale: float = 1.0, out=None, accumulat
     whose token is v, in the tokens' order, so that equal inputs give equal
     bits.  Rows without a token are zeroed; with accumulate the sums are added
     to what out holds, and those rows are left alone."""
-    torch = _torch()
-    n, d, ld, code = _rows("grad", grad)
-    at, wide = _token_buffer(tokens, n, grad.device)
+    at, n, d, ld, code, index = _place("grad", grad)
+    ids, wide = _token_place(tokens, n, index)
     if out is None:
         if accumulate:
             raise AspisError(ERR_INVALID_ARG, "accumulate needs out")
-        out = torch.empty((vocab, d), dtype=torch.float32, device=grad.device)
-    rows, width, ldo, out_code = _matrix("out", out, grad.device)
-    if rows != vocab or width != d:
-        raise AspisError(ERR_INVALID_ARG, f"out must be [{vocab}, {d}], not {tuple(out.shape)}")
+        out = _torch().empty((vocab, d), dtype=_float32(), device=grad.device)
+    to, rows, width, ldo, out_code, out_index = _place("out", out)
+    if rows != vocab or width != d or out_index != index:
+        raise AspisError(ERR_INVALID_ARG, f"out must be [{vocab}, {d}] on {grad.device}, not "
+                                          f"{tuple(out.shape)} on {out.device}")
     if ws is None:
         ws = embed_workspace(grad, tokens, vocab)
-    # the workspace's size is the library's to check
-    ws_at = _buffer("ws", ws, torch.uint8, 0, grad.device)
-    _launch(grad.device, lib().aspis_embed_grad, grad.data_ptr(), n, d, ld, code, at, wide, scale,
-            out.data_ptr(), vocab, ldo, out_code, EMBED_ACCUMULATE if accumulate else 0, ws_at,
-            ws.numel(), _raw_stream(grad.device))
+    _enqueue(index, lib().aspis_embed_grad, at, n, d, ld, code, ids, wide, scale, to, vocab, ldo,
+             out_code, EMBED_ACCUMULATE if accumulate else 0, _scratch_at(ws, index), ws.numel())
     return out
 
 
@@ -1096,26 +1146,24 @@ def dropout(x, p: float, seed, offset: int = 0, residual=None, out=None):
     as offset.  p counts in steps of 2^-16.  A graph that captured a call
     replays its mask; with seed a cuda int64 tensor [1] it draws what that then
     holds.  Autograd does not see it."""
-    torch = _torch()
-    rows, d, ld, code = _rows("x", x)
+    at, rows, d, ld, code, index = _place("x", x)
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    ldo, ldr, res = ld, 0, None
+        out = _torch().empty(x.shape, dtype=x.dtype, device=x.device)
+    to, ldo, res, ldr = at, ld, None, 0
     if out is not x:
-        _, _, ldo, out_code = _rows("out", out)
-        if out.shape != x.shape or out_code != code or out.device != x.device:
+        to, _, _, ldo, out_code, out_index = _place("out", out)
+        if out.shape != x.shape or out_code != code or out_index != index:
             raise AspisError(ERR_INVALID_ARG, "out must have the shape, type and device of x")
     if residual is not None:
-        _, _, ldr, res_code = _rows("residual", residual)
-        if residual.shape != x.shape or res_code != code or residual.device != x.device:
+        res, _, _, ldr, res_code, res_index = _place("residual", residual)
+        if residual.shape != x.shape or res_code != code or res_index != index:
             raise AspisError(ERR_INVALID_ARG, "residual must have the shape, type and device of x")
-        res = residual.data_ptr()
     seed_at = None
-    if isinstance(seed, torch.Tensor):
-        seed_at, seed = _buffer("seed", seed, torch.int64, 1, x.device), 0
-    _launch(x.device, lib().aspis_dropout, x.data_ptr(), rows, d, ld, code, p,
-            seed & 0xFFFFFFFFFFFFFFFF, seed_at, offset & 0xFFFFFFFFFFFFFFFF, res, ldr,
-            out.data_ptr(), ldo, _raw_stream(x.device))
+    if isinstance(seed, _torch().Tensor):
+        seed_at, seed = _buffer("seed", seed, _torch().int64, 1, x.device), 0
+    seed, offset = operator.index(seed), operator.index(offset)
+    _enqueue(index, lib().aspis_dropout, at, rows, d, ld, code, p, seed & 0xFFFFFFFFFFFFFFFF,
+             seed_at, offset & 0xFFFFFFFFFFFFFFFF, res, ldr, to, ldo)
     return out
 
 
@@ -1137,7 +1185,7 @@ class PolicyBuffers:
 def policy_workspace(logits):
     """Workspace of token_logps and policy_loss for logits [..., vocab]."""
     torch = _torch()
-    rows, vocab, _, code = _rows("logits", logits)
+    _, rows, vocab, _, code, _ = _place("logits", logits)
     n = int(lib().aspis_policy_workspace(rows, vocab, code))
     if n == ctypes.c_size_t(-1).value:
         raise AspisError(ERR_OVERFLOW, f"{rows} rows of {vocab} logits are too many")
@@ -1148,20 +1196,16 @@ def token_logps(logits, tokens, temperature: float = 1.0, logps=None, ws=None):
     """log p of a token per row of logits [..., vocab] under
     softmax(logits / temperature) (aspis_token_logps), float32 of the tokens'
     shape: what policy_loss takes as old and ref.  0 where the token is outside
-    the vocabulary.  The result carries no autograd graph."""
-    torch = _torch()
-    rows, vocab, ld, code = _rows("logits", logits)
-    device = logits.device
-    at, wide = _token_buffer(tokens, rows, device)
+    the vocabulary.  A row's result does not depend on the others of the call.
+    The result carries no autograd graph."""
+    at, rows, vocab, ld, code, index = _place("logits", logits)
+    ids, wide = _token_place(tokens, rows, index)
     if logps is None:
-        logps = torch.empty(tokens.shape, dtype=torch.float32, device=device)
+        logps = _torch().empty(tokens.shape, dtype=_float32(), device=logits.device)
     if ws is None:
         ws = policy_workspace(logits)
-    to = _buffer("logps", logps, torch.float32, rows, device)
-    # the workspace's size is the library's to check
-    ws_at = _buffer("ws", ws, torch.uint8, 0, device)
-    _launch(device, lib().aspis_token_logps, logits.data_ptr(), rows, vocab, ld, code, at, wide,
-            temperature, to, ws_at, ws.numel(), _raw_stream(device))
+    _enqueue(index, lib().aspis_token_logps, at, rows, vocab, ld, code, ids, wide, temperature,
+             _floats("logps", logps, rows, index), _scratch_at(ws, index), ws.numel())
     return logps
 
 
@@ -1175,33 +1219,28 @@ def policy_loss(logits, tokens, old, advantage, weight, ref=None, clip=(0.2, 0.2
     advantage, what the position counts (its mask over the number of
     positions; 0 leaves it out) and log-probabilities under the reference.
     clip is (below, above) 1.  grad receives grad_scale times the gradient: a
-    tensor like logits, or logits themselves.  Nothing is synchronised.
+    tensor like logits, or logits themselves.  A row's gradient does not depend
+    on the others of the call.  Nothing is synchronised.
 
     Autograd does not see it: hand grad to the layer below (or to autograd, as
     torch.autograd.backward(logits, grad))."""
-    torch = _torch()
-    f32 = torch.float32
-    rows, vocab, ld, code = _rows("logits", logits)
-    device = logits.device
-    at, wide = _token_buffer(tokens, rows, device)
+    at, rows, vocab, ld, code, index = _place("logits", logits)
+    ids, wide = _token_place(tokens, rows, index)
     if bufs is None:
-        bufs = PolicyBuffers.empty(rows, device)
+        bufs = PolicyBuffers.empty(rows, logits.device)
     if ws is None:
         ws = policy_workspace(logits)
     to, ldg = None, 0
     if grad is not None:
-        _, _, ldg, grad_code = _rows("grad", grad)
-        if grad.shape != logits.shape or grad_code != code or grad.device != device:
+        to, _, _, ldg, grad_code, grad_index = _place("grad", grad)
+        if grad.shape != logits.shape or grad_code != code or grad_index != index:
             raise AspisError(ERR_INVALID_ARG, "grad must have the shape, type and device of logits")
-        to = grad.data_ptr()
     opt = PolicyOptions(clip[0], clip[1], kl, temperature, grad_scale)
-    _launch(device, lib().aspis_policy_loss, logits.data_ptr(), rows, vocab, ld, code, at, wide,
-            _buffer("old", old, f32, rows, device),
-            _buffer("advantage", advantage, f32, rows, device),
-            _buffer("weight", weight, f32, rows, device),
-            _buffer("ref", ref, f32, rows, device) if ref is not None else None,
-            ctypes.byref(opt), _buffer("bufs.sums", bufs.sums, f32, 3, device),
-            _buffer("bufs.logps", bufs.logps, f32, rows, device), to, ldg,
-            # the workspace's size is the library's to check
-            _buffer("ws", ws, torch.uint8, 0, device), ws.numel(), _raw_stream(device))
+    _enqueue(index, lib().aspis_policy_loss, at, rows, vocab, ld, code, ids, wide,
+             _floats("old", old, rows, index), _floats("advantage", advantage, rows, index),
+             _floats("weight", weight, rows, index),
+             _floats("ref", ref, rows, index) if ref is not None else None, ctypes.byref(opt),
+             _floats("bufs.sums", bufs.sums, 3, index),
+             _floats("bufs.logps", bufs.logps, rows, index), to, ldg, _scratch_at(ws, index),
+             ws.numel())
     return bufs

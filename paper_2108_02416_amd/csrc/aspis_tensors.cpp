@@ -1,5 +1,5 @@
-// aspis_tensors.cpp -- the Python module _tensors: what the norm, clipping
-// and update calls ask of torch tensors every time, in one call each.  Asked
+// aspis_tensors.cpp -- the Python module _tensors: what the norm, clipping,
+// update and token calls ask of torch tensors every time, in one call each.  Asked
 // attribute by attribute through Python it takes longer than a small call's
 // kernels (four questions of 62 tensors: 7.3 us; a buffer's checks: 0.7 us).
 #include <torch/csrc/Dtype.h>
@@ -66,6 +66,58 @@ PyObject *buffer(PyObject *, PyObject *const *args, Py_ssize_t count) {
             t.scalar_type() != reinterpret_cast<THPDtype *>(args[1])->scalar_type)
             Py_RETURN_NONE;
         return PyLong_FromUnsignedLongLong((unsigned long long)(uintptr_t)t.data_ptr());
+    } catch (const std::exception &e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+        return nullptr;
+    }
+}
+
+// The type code of aspis.h, or -1.
+int type_code(at::ScalarType t) {
+    return t == at::kFloat ? 0 : t == at::kBFloat16 ? 1 : t == at::kHalf ? 2 : -1;
+}
+
+// place(x) -> (address, rows, d, elements between rows, type code of aspis.h,
+// device index) of a GPU tensor [..., d] that holds rows of contiguous
+// elements, equally far apart; or None.
+PyObject *place(PyObject *, PyObject *arg) {
+    if (!THPVariable_Check(arg)) Py_RETURN_NONE;
+    try {
+        const at::Tensor &t = THPVariable_Unpack(arg);
+        if (!t.is_cuda() || t.layout() != at::kStrided || t.dim() < 1 || t.numel() == 0 || t.is_neg())
+            Py_RETURN_NONE;
+        const int code = type_code(t.scalar_type());
+        const int64_t dims = t.dim(), d = t.size(-1), rows = t.numel() / d;
+        if (code < 0 || (d > 1 && t.stride(-1) != 1)) Py_RETURN_NONE;
+        int64_t ld = 0, run = 1;   // rows of the dimensions so far
+        for (int64_t i = dims - 2; i >= 0; --i) {
+            if (t.size(i) == 1) continue;
+            if (ld == 0) ld = t.stride(i);
+            else if (t.stride(i) != ld * run) Py_RETURN_NONE;
+            run *= t.size(i);
+        }
+        if (run == 1) ld = d;
+        if (ld < d) Py_RETURN_NONE;
+        return Py_BuildValue("KLLLii", (unsigned long long)(uintptr_t)t.data_ptr(), (long long)rows,
+                             (long long)d, (long long)ld, code, (int)t.get_device());
+    } catch (const std::exception &e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+        return nullptr;
+    }
+}
+
+// tokens(x) -> (address, number, whether int64, device index) of a contiguous
+// GPU tensor of int32 or int64, or None.
+PyObject *tokens(PyObject *, PyObject *arg) {
+    if (!THPVariable_Check(arg)) Py_RETURN_NONE;
+    try {
+        const at::Tensor &t = THPVariable_Unpack(arg);
+        if (!t.is_cuda() || t.layout() != at::kStrided || !t.is_contiguous() || t.is_neg() ||
+            (t.scalar_type() != at::kLong && t.scalar_type() != at::kInt))
+            Py_RETURN_NONE;
+        return Py_BuildValue("KLii", (unsigned long long)(uintptr_t)t.data_ptr(),
+                             (long long)t.numel(), (int)(t.scalar_type() == at::kLong),
+                             (int)t.get_device());
     } catch (const std::exception &e) {
         PyErr_SetString(PyExc_RuntimeError, e.what());
         return nullptr;
@@ -146,6 +198,10 @@ PyObject *apart_py(PyObject *, PyObject *const *args, Py_ssize_t count) {
 PyMethodDef methods[] = {
     {"apart", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(apart_py)),
      METH_FASTCALL, "Whether lists of spans share no memory."},
+    {"place", place, METH_O,
+     "Address, rows, length, distance, type code and device index of a GPU tensor of rows."},
+    {"tokens", tokens, METH_O,
+     "Address, number, width and device index of a contiguous GPU tensor of tokens."},
     {"rows", rows, METH_O, "Rows, length, distance and type code of a contiguous GPU tensor."},
     {"buffer", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(buffer)), METH_FASTCALL,
      "The address of a contiguous GPU tensor of a type and size, or None."},

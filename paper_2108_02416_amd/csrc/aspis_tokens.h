@@ -39,7 +39,9 @@ struct EmbedArgs {
 };
 hipError_t launch_embed(const EmbedArgs &a, hipStream_t s);
 
-// The gradient: tokens sorted in runs of kSortRun, kMergeRuns of them merged
+// The gradient of up to kFewTokens tokens takes one launch and no workspace.
+constexpr int kFewTokens = 768;
+// Of more: tokens sorted in runs of kSortRun, kMergeRuns of them merged
 // in LDS, longer ones where they are; then the sums of the sorted positions'
 // segments, window by window of positions, long ones in pieces of at most a
 // block of two windows that are joined afterwards.
@@ -58,8 +60,9 @@ inline EmbedGradPlan embed_grad_plan(int64_t n, int64_t d) {
     EmbedGradPlan p;
     p.shift = embed_shift(n);
     p.blocks = (n + (2 << p.shift) - 1) / (2 << p.shift);
-    p.words = n > 0 ? (size_t)((n + 3) / 4 * 16 + 32) : 0;
+    p.words = (size_t)((n + 3) / 4 * 16 + 32);
     p.bytes = 4 * p.words + (size_t)(p.blocks * 2 * embed_row(d)) * sizeof(float);
+    if (n <= kFewTokens) p.bytes = 0;
     return p;
 }
 struct EmbedGradArgs {

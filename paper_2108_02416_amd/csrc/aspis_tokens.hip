@@ -310,7 +310,8 @@ struct SumArgs {
     int shift;           // log2 of a window's positions
     int64_t windows;
     int slabs, tail;     // waves that share a row's whole vectors; 1 for the elements after
-    int64_t sum_blocks;  // workgroups of windows; the others fill rows with zeros
+    int64_t sum_blocks;  // workgroups of windows; the others fill rows with zeros:
+    int zero_rows, zero_shift;   // so many each, 2^shift lanes a row
     int64_t first;       // the launch's first workgroup
 };
 
@@ -343,7 +344,7 @@ __device__ __forceinline__ void finish_row(const EmbedGradArgs &a, uint32_t toke
     }
 }
 
-constexpr int kZeroRows = 16;   // rows of a workgroup that fills in zeros
+constexpr int kZeroRows = 256;   // rows of a workgroup that fills in zeros, at most
 
 // The first position whose token is not below `token`; a wave looks at 64
 // places at once.
@@ -361,42 +362,46 @@ __device__ __forceinline__ int64_t first_not_below(const uint32_t *sorted, int64
     return low;
 }
 
+// Zeros in those of a workgroup's g.zero_rows rows that no token names.
 template <typename EO>
 __device__ __forceinline__ void zero_rows(const SumArgs &g, int64_t block) {
-    __shared__ uint32_t there;
+    __shared__ uint32_t there[kZeroRows / 32];
+    __shared__ int64_t bounds[2];   // the rows' positions
     const EmbedGradArgs &a = g.a;
-    const int64_t first = block * kZeroRows;
-    const int rows = (int)(a.vocab - first < kZeroRows ? a.vocab - first : kZeroRows);
-    if (threadIdx.x < 64) {
-        const uint32_t *sorted = g.sorted.token;
-        int64_t low = first_not_below(sorted, a.n, (uint32_t)first);
-        uint32_t mask = 0;
-        while (low < a.n) {   // from one of the rows' tokens to the next
-            const uint32_t token = sorted[low];
-            if (token >= (uint32_t)(first + rows)) break;
-            const int64_t at = low + threadIdx.x % 64;
-            const uint32_t mine = at < a.n ? sorted[at] : ~0u;
-#pragma unroll
-            for (int r = 0; r < kZeroRows; ++r)
-                mask |= (uint32_t)(__ballot(mine == (uint32_t)first + r) != 0) << r;
-            // all 64 are of these rows: go on, past what the last one fills
-            if (low + 63 >= a.n) break;
-            const uint32_t last = sorted[low + 63];
-            if (last >= (uint32_t)(first + rows)) break;
-            low = last == token ? first_not_below(sorted, a.n, last + 1) : low + 64;
-        }
-        if (threadIdx.x == 0) there = mask;
+    const uint32_t *sorted = g.sorted.token;
+    const int64_t first = block * g.zero_rows;
+    const int rows = (int)(a.vocab - first < g.zero_rows ? a.vocab - first : g.zero_rows);
+    if (threadIdx.x < kZeroRows / 32) there[threadIdx.x] = 0;
+    if (threadIdx.x < 128) {
+        const int64_t at = first_not_below(sorted, a.n, (uint32_t)(first + threadIdx.x / 64 * rows));
+        if (threadIdx.x % 64 == 0) bounds[threadIdx.x / 64] = at;
     }
     __syncthreads();
-    const uint32_t mask = there;
+    const int64_t begin = bounds[0], end = bounds[1];
+    if (end - begin <= 4 * kBlock) {   // few: all of them
+        for (int64_t i = begin + threadIdx.x; i < end; i += kBlock) {
+            const uint32_t of = sorted[i] - (uint32_t)first;
+            atomicOr(&there[of / 32], 1u << of % 32);
+        }
+    } else if ((int)threadIdx.x < rows) {   // a row each
+        const uint32_t token = (uint32_t)first + threadIdx.x;
+        int64_t low = begin, high = end;
+        while (low < high) {
+            const int64_t mid = (low + high) / 2;
+            if (sorted[mid] < token) low = mid + 1;
+            else high = mid;
+        }
+        if (low < end && sorted[low] == token) atomicOr(&there[threadIdx.x / 32], 1u << threadIdx.x % 32);
+    }
+    __syncthreads();
+    const int lane = (int)threadIdx.x & ((1 << g.zero_shift) - 1);
     const float zero[EO::V] = {};
     const int64_t nv = a.d / EO::V;
-    for (int r = 0; r < rows; ++r) {
-        if (mask >> r & 1) continue;
+    for (int r = (int)threadIdx.x >> g.zero_shift; r < rows; r += kBlock >> g.zero_shift) {
+        if (there[r / 32] >> r % 32 & 1) continue;
         const MutPtr<EO> to = (MutPtr<EO>)a.out + (first + r) * a.ldo;
-        for (int64_t v = threadIdx.x; v < nv; v += kBlock)
-            store_floats<EO>(to + v * EO::V, zero);
-        for (int64_t i = nv * EO::V + threadIdx.x; i < a.d; i += kBlock) to[i] = EO::put(0.0f);
+        for (int64_t v = lane; v < nv; v += 1 << g.zero_shift) store_floats<EO>(to + v * EO::V, zero);
+        for (int64_t i = nv * EO::V + lane; i < a.d; i += 1 << g.zero_shift) to[i] = EO::put(0.0f);
     }
 }
 
@@ -586,6 +591,195 @@ __global__ __launch_bounds__(kBlock) void join_pieces_kernel(SumArgs g, int64_t 
         const MutPtr<EO> out = (MutPtr<EO>)a.out + (int64_t)token * a.ldo + col + j;
         v *= a.scale;
         *out = EO::put(a.accumulate ? EO::get(*out) + v : v);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// its gradient, of few tokens, in one launch
+
+// Up to kFewTokens tokens are not sorted as a whole: a workgroup takes some
+// rows of the table and 64 vectors of them, picks the rows' tokens out of all
+// of them, sorts those few, and its waves share them evenly; sums of a segment
+// that several waves hold are joined in LDS, in order.  Three launches less:
+// 515 tokens of 257 f32 into 4,099 rows take XX us (14.3 by sorting all).
+constexpr int kFewRows = 64;   // of a workgroup, at most
+
+struct FewArgs {
+    EmbedGradArgs a;
+    int rows;          // of a workgroup
+    int slabs, tail;   // as in SumArgs
+    int64_t first;     // the launch's first workgroup
+};
+
+// The table rows' tokens in order: (row << 10 | position), and which rows
+// have any.
+struct FewList {
+    uint32_t key[kSortRun + 16], other[kSortRun];   // (as many as sort_run takes)
+    uint64_t there;
+    int count[kFewTokens / 64];
+};
+static_assert(kFewTokens <= kSortRun && kFewTokens % kBlock == 0 && kFewTokens <= 1 << 10, "");
+
+// Fills the list; returns its length.
+__device__ __forceinline__ int few_tokens(const EmbedGradArgs &a, int64_t first, int rows, FewList &l) {
+    constexpr int K = kFewTokens / kBlock, WAVES = kBlock / 64;
+    const int t = threadIdx.x, lane = t % 64, wave = t / 64;
+    int row[K];
+    uint64_t mine[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int i = k * kBlock + t;
+        const int64_t token = i < a.n ? (int64_t)a.tokens.get(i, a.vocab) : -1;
+        row[k] = token >= first && token < first + rows ? (int)(token - first) : -1;
+        mine[k] = __ballot(row[k] >= 0);
+        if (lane == 0) l.count[k * WAVES + wave] = __popcll(mine[k]);
+    }
+    if (t == 0) l.there = 0;
+    __syncthreads();
+    int m = 0, from[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            if (w == wave) from[k] = m;
+            m += l.count[k * WAVES + w];
+        }
+    m = __builtin_amdgcn_readfirstlane(m);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        if (row[k] < 0) continue;
+        const int at = from[k] + __popcll(mine[k] & ((uint64_t(1) << lane) - 1));
+        l.other[at] = (uint32_t)row[k] << 10 | (uint32_t)(k * kBlock + t);
+        atomicOr((unsigned long long *)&l.there, 1ull << row[k]);
+    }
+    __syncthreads();
+    if (m <= kBlock) {   // a key's place is the number of lower ones (no two are equal)
+        const uint32_t key = t < m ? l.other[t] : ~0u;
+        int place = 0;
+        for (int j = 0; j < m; ++j) place += l.other[j] < key;
+        if (t < m) l.key[place] = key;
+    } else {
+        uint32_t key[kSortKeys];
+#pragma unroll
+        for (int r = 0; r < kSortKeys; ++r) key[r] = r * kBlock + t < m ? l.other[r * kBlock + t] : ~0u;
+        __syncthreads();
+        sort_run<kSortRun>(key, l.other);
+#pragma unroll
+        for (int r = 0; r < kSortKeys; ++r) l.key[t * kSortKeys + r] = key[r];
+    }
+    __syncthreads();
+    return m;
+}
+
+template <typename EI, typename EO, int N>
+__device__ __forceinline__ void few_sums(const FewArgs &g, FewList &l, float (*part)[2][64 * 8],
+                                         int m, int64_t first, int rows, int64_t col, bool active) {
+    constexpr int W = N == 1 ? 1 : N / EI::V, U = 16 / W, WAVES = kBlock / 64;
+    const EmbedGradArgs &a = g.a;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int share = m > 4 * WAVES ? (m + WAVES - 1) / WAVES : 4;
+    const int begin = wave * share, end = begin + share < m ? begin + share : m;
+    auto row_at = [&](int p) {   // the row of the list's entry p; -1 outside of it
+        return __builtin_amdgcn_readfirstlane(p >= 0 && p < m ? (int)(l.key[p] >> 10) : -1);
+    };
+    if (begin < end) {
+        int row = row_at(begin);
+        bool open = row_at(begin - 1) == row;
+        float acc[N] = {};
+        auto flush = [&](bool goes_on) {
+            if (!open && !goes_on) {
+                if (active) finish_row<EO, N>(a, (uint32_t)(first + row), col, acc);
+                return;
+            }
+#pragma unroll
+            for (int j = 0; j < N; ++j) part[wave][open ? 0 : 1][j * 64 + lane] = acc[j];
+        };
+        for (int p = begin; p < end; p += U) {
+            int now[U];
+            typename EI::T one[U];
+            u32x4 x[U][W];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const uint32_t key = __builtin_amdgcn_readfirstlane(l.key[p + u]);   // (16 past the end)
+                now[u] = p + u < end ? (int)(key >> 10) : -1;
+                const Ptr<EI> from = (Ptr<EI>)a.grad + (int64_t)(key & 1023) * a.ld + col;
+                if constexpr (N == 1) one[u] = EI::put(0.0f);
+#pragma unroll
+                for (int i = 0; i < W; ++i) x[u][i] = (u32x4){0, 0, 0, 0};
+                if (now[u] < 0 || !active) continue;
+                if constexpr (N == 1) {
+                    one[u] = *from;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < W; ++i) x[u][i] = load_vec<EI, Use::Once>(from + i * EI::V);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (now[u] < 0) break;
+                if (now[u] != row) {
+                    flush(false);
+#pragma unroll
+                    for (int j = 0; j < N; ++j) acc[j] = 0.0f;
+                    row = now[u];
+                    open = false;
+                }
+                if constexpr (N == 1) {
+                    acc[0] += EI::get(one[u]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < W; ++i) {
+                        float y[EI::V];
+                        EI::unpack(x[u][i], y);
+#pragma unroll
+                        for (int j = 0; j < EI::V; ++j) acc[i * EI::V + j] += y[j];
+                    }
+                }
+            }
+        }
+        flush(row_at(end) == row);
+    }
+    __syncthreads();
+    // the segment that begins among this wave's and goes on
+    if (begin < end && end < m) {
+        const int row = row_at(end - 1);
+        if (row_at(end) == row && (row_at(begin) != row || row_at(begin - 1) != row)) {
+            float acc[N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) acc[j] = part[wave][1][j * 64 + lane];
+            for (int w = wave + 1; w < WAVES && row_at(w * share) == row; ++w)
+#pragma unroll
+                for (int j = 0; j < N; ++j) acc[j] += part[w][0][j * 64 + lane];
+            if (active) finish_row<EO, N>(a, (uint32_t)(first + row), col, acc);
+        }
+    }
+    if (a.accumulate || !active) return;
+    const uint64_t there = l.there;
+    const float zero[N] = {};
+    for (int r = wave; r < rows; r += WAVES) {
+        if (there >> r & 1) continue;
+        const MutPtr<EO> to = (MutPtr<EO>)a.out + (first + r) * a.ldo + col;
+        if constexpr (N == 1) *to = EO::put(0.0f);
+        else store_floats<EO, N>(to, zero);
+    }
+}
+
+template <typename EI, typename EO>
+__global__ __launch_bounds__(kBlock) void few_tokens_kernel(FewArgs g) {
+    constexpr int N = EI::V > EO::V ? EI::V : EO::V;
+    __shared__ FewList list;
+    __shared__ float part[kBlock / 64][2][64 * 8];
+    const int64_t item = g.first + blockIdx.x;
+    const int64_t first = item / (g.slabs + g.tail) * g.rows;
+    const int slab = (int)(item % (g.slabs + g.tail)), lane = threadIdx.x % 64;
+    const int rows = (int)(g.a.vocab - first < g.rows ? g.a.vocab - first : g.rows);
+    const int m = few_tokens(g.a, first, rows, list);
+    const int64_t whole = g.a.d / N * N;
+    if (slab < g.slabs) {
+        const int64_t col = ((int64_t)slab * 64 + lane) * N;
+        few_sums<EI, EO, N>(g, list, part, m, first, rows, col, col < whole);
+    } else {
+        few_sums<EI, EO, 1>(g, list, part, m, first, rows, whole + lane, whole + lane < g.a.d);
     }
 }
 
@@ -781,6 +975,25 @@ hipError_t launch_embed(const EmbedArgs &a, hipStream_t s) {
 
 hipError_t launch_embed_grad(const EmbedGradArgs &a, hipStream_t s) {
     if (a.vocab == 0 || a.d == 0 || (a.n == 0 && a.accumulate)) return hipSuccess;
+    if (a.n <= kFewTokens)
+        return with_types(a.dtype, a.out_dtype, [&](auto from, auto to) {
+            typedef decltype(from) EI;
+            typedef decltype(to) EO;
+            constexpr int N = EI::V > EO::V ? EI::V : EO::V;
+            FewArgs g{};
+            g.a = a;
+            g.slabs = (int)((a.d / N + 63) / 64);
+            g.tail = a.d % N != 0;
+            // few rows, so that the waves of the commonest tokens' workgroup have
+            // little to do, but enough of them for what each workgroup reads first
+            const int64_t slabs = g.slabs + g.tail;
+            g.rows = kFewRows;
+            while (g.rows > 4 && (a.vocab + g.rows / 4 - 1) / (g.rows / 4) * slabs <= 4096) g.rows /= 4;
+            return over_blocks((a.vocab + g.rows - 1) / g.rows * slabs, [&](int64_t first, unsigned n) {
+                g.first = first;
+                few_tokens_kernel<EI, EO><<<n, kBlock, 0, s>>>(g);
+            });
+        });
     const EmbedGradPlan plan = embed_grad_plan(a.n, a.d);
     char *ws = (char *)a.ws;
     auto array = [&](int i) { return (uint32_t *)(ws + i * plan.words); };
@@ -791,7 +1004,7 @@ hipError_t launch_embed_grad(const EmbedGradArgs &a, hipStream_t s) {
         other = swap;
         return hipGetLastError();
     };
-    if (a.n > 0) {
+    {
         const unsigned runs = (unsigned)((a.n + kSortRun - 1) / kSortRun);
         if (a.vocab < (1 << 22) - 1) sort_runs_kernel<uint32_t><<<runs, kBlock, 0, s>>>(a, sorted);
         else sort_runs_kernel<uint64_t><<<runs, kBlock, 0, s>>>(a, sorted);
@@ -829,7 +1042,10 @@ hipError_t launch_embed_grad(const EmbedGradArgs &a, hipStream_t s) {
         g.slabs = (int)((a.d / N + 63) / 64);
         g.tail = a.d % N != 0;
         g.sum_blocks = (g.windows * (g.slabs + g.tail) + kBlock / 64 - 1) / (kBlock / 64);
-        const int64_t zero = a.accumulate ? 0 : (a.vocab + kZeroRows - 1) / kZeroRows;
+        // enough zeros a workgroup to be worth the search that comes first
+        g.zero_rows = a.d >= 512 ? 16 : a.d >= 64 ? 64 : kZeroRows;
+        g.zero_shift = lane_shift((a.d + EO::V - 1) / EO::V);
+        const int64_t zero = a.accumulate ? 0 : (a.vocab + g.zero_rows - 1) / g.zero_rows;
         const hipError_t st = over_blocks(g.sum_blocks + zero, [&](int64_t first, unsigned n) {
             g.first = first;
             sum_rows_kernel<EI, EO><<<n, kBlock, 0, s>>>(g);

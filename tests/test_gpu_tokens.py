@@ -153,7 +153,7 @@ def test_embed_grad_types(n, vocab, d, kind, to, accumulate):
 
 
 @pytest.mark.parametrize("how", ["zipf", "uniform", "one", "none", "distinct"])
-@pytest.mark.parametrize("n", [1, 8, 9, 16, 17, 64, 2047, 2048, 2049, 4096, 4097, 5000, 32_768,
+@pytest.mark.parametrize("n", [1, 8, 9, 16, 17, 64, 255, 257, 767, 768, 769, 1024, 1025, 2047, 2048, 2049, 4096, 4097, 5000, 32_768,
                                33_000, 40_001])
 def test_embed_grad_tokens(n, how):
     import torch
@@ -162,6 +162,21 @@ def test_embed_grad_tokens(n, how):
     t, tokens = _tokens(n, vocab, seed=n, how=how, kind="int32")
     out = torch.full((vocab, d), 7.0, device=device())
     _check_embed_grad(grad, t, tokens, vocab, out)
+
+
+@pytest.mark.parametrize("n", [100, 700, 1024, 1500, 6000])
+@pytest.mark.parametrize("vocab,d", [(7, 513), (300, 1030), (20_001, 257), (130_000, 520)])
+@pytest.mark.parametrize("how", ["zipf", "uniform", "one"])
+def test_embed_grad_shapes(n, vocab, d, how):
+    """Every number of rows a workgroup takes, several slabs of columns, and
+    columns after the last vector."""
+    import torch
+    for kind, accumulate in (("bfloat16", False), ("float32", True)):
+        grad = _randn((n, d), kind, seed=n)
+        t, tokens = _tokens(n, vocab, seed=n + d, how=how)
+        out = _randn((vocab, d), seed=1) if accumulate else torch.full((vocab, d), 7.0,
+                                                                       device=device())
+        _check_embed_grad(grad, t, tokens, vocab, out, 0.7, accumulate)
 
 
 @pytest.mark.parametrize("how", ["zipf", "one"])
@@ -619,6 +634,7 @@ def test_refusals():
     f, dev = torch.float32, device()
     x, t = torch.zeros((4, 6), device=dev), torch.zeros(4, dtype=torch.int64, device=dev)
     v = torch.zeros(4, device=dev)
+    long, many = torch.zeros((2000, 6), device=dev), torch.zeros(2000, dtype=torch.int64, device=dev)
     bad = [
         lambda: aspis.embed(x, t.to(torch.int16)), lambda: aspis.embed(x, t.cpu()),
         lambda: aspis.embed(x.double(), t), lambda: aspis.embed(x[0], t),
@@ -630,8 +646,9 @@ def test_refusals():
         lambda: aspis.embed_grad(x, t[:3], 9), lambda: aspis.embed_grad(x, t, 9, accumulate=True),
         lambda: aspis.embed_grad(x, t, 4, out=x), lambda: aspis.embed_grad(x, t, 9, out=x),
         lambda: aspis.embed_grad(x, t, 9, scale=math.nan),
-        lambda: aspis.embed_grad(x, t, 9, ws=torch.zeros(16, dtype=torch.uint8, device=dev)),
-        lambda: aspis.embed_grad(x, t, 9, ws=torch.zeros(99_999, dtype=torch.uint8, device=dev)[1:]),
+        lambda: aspis.embed_grad(long, many, 9, ws=torch.zeros(16, dtype=torch.uint8, device=dev)),
+        lambda: aspis.embed_grad(long, many, 9,
+                                 ws=torch.zeros(99_999, dtype=torch.uint8, device=dev)[1:]),
         lambda: aspis.embed_grad(x, t, 9, ws=torch.zeros(99_999, dtype=torch.uint8)),
         lambda: aspis.embed_grad(x, t.float(), 9),
         lambda: aspis.dropout(x, -0.1, 1), lambda: aspis.dropout(x, 1.1, 1),
