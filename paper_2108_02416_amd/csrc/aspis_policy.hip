@@ -57,34 +57,54 @@ __device__ __forceinline__ Stats join_lanes(Stats p, float c) {
     return {m, lanes_join<64>(p.s == 0.0f ? 0.0f : p.s * by, Sum())};
 }
 
-// Of N vectors a lane, and one element.
+// Of N vectors a lane, and one element.  Any power near the largest will do
+// as the scale, since a sum of powers up to 2^kRoom above it loses nothing in
+// f32: the largest of one element in V, which takes a third of the time of
+// the largest of all, and that one only where the sum says so.
+constexpr float kRoom = 0x1p100f;
+
 template <typename E, int N>
 __device__ __forceinline__ Stats unit_stats(const u32x4 *v, float tail, float c) {
+    auto sum = [&](float m) {
+        float s = 0.0f;
+        auto add = [&](auto power) {
+#pragma unroll
+            for (int r = 0; r < N; ++r) {
+                u32x4 again = v[r];
+                asm volatile("" : "+v"(again));   // unpacked anew: kept, it takes twice the registers
+                float x[E::V];
+                E::unpack(again, x);
+#pragma unroll
+                for (int j = 0; j < E::V; ++j) s += power(x[j]);
+            }
+            s += power(tail);
+        };
+        if (__builtin_amdgcn_readfirstlane(is_fast(m, c))) add(Fast{c, m * c});
+        else add(Slow(c, m));
+        return lanes_join<64>(s, Sum());
+    };
     float m = tail;
 #pragma unroll
     for (int r = 0; r < N; ++r) {
         float x[E::V];
         E::unpack(v[r], x);
-#pragma unroll
-        for (int j = 0; j < E::V; ++j) m = fmaxf(m, x[j]);
+        m = fmaxf(m, x[0]);
     }
     m = lanes_join<64>(m, Max());
-    float s = 0.0f;
-    auto add = [&](auto power) {
+    float s = sum(m);
+    if (__builtin_amdgcn_readfirstlane(m == -INFINITY || !(s <= kRoom))) {
+        m = tail;
 #pragma unroll
         for (int r = 0; r < N; ++r) {
-            u32x4 again = v[r];
-            asm volatile("" : "+v"(again));   // unpacked anew: kept, it takes twice the registers
             float x[E::V];
-            E::unpack(again, x);
+            E::unpack(v[r], x);
 #pragma unroll
-            for (int j = 0; j < E::V; ++j) s += power(x[j]);
+            for (int j = 0; j < E::V; ++j) m = fmaxf(m, x[j]);
         }
-        s += power(tail);
-    };
-    if (__builtin_amdgcn_readfirstlane(is_fast(m, c))) add(Fast{c, m * c});
-    else add(Slow(c, m));
-    return {m, lanes_join<64>(s, Sum())};
+        m = lanes_join<64>(m, Max());
+        s = sum(m);
+    }
+    return {m, s};
 }
 
 // e^x - 1 - x: by its series near 0, where the difference would cancel.
@@ -120,10 +140,11 @@ __device__ __forceinline__ Terms terms_of(const PolicyArgs &a, int64_t row, floa
     return t;
 }
 
-// The position's token, or -1 where it is left out; its weight.
+// The position's token, or -1 where it is left out; its weight.  (A row is a
+// wave's at least: the same in all lanes.)
 __device__ __forceinline__ int take_token(const PolicyArgs &a, int64_t row, float &weight) {
     weight = a.sums != nullptr ? a.weight[row] : 1.0f;
-    return weight == 0.0f ? -1 : a.tokens.get(row, a.vocab);
+    return __builtin_amdgcn_readfirstlane(weight == 0.0f ? -1 : a.tokens.get(row, a.vocab));
 }
 
 struct Scratch {
@@ -143,52 +164,60 @@ __device__ __forceinline__ void put_row(const PolicyArgs &a, const Scratch &w, i
     w.terms[2 * a.rows + row] = used ? (double)weight * t.cut : 0.0;
 }
 
+// Element i of a row, fewer than 2^30 bytes on: the row's address stays in
+// scalar registers.
+template <typename P>
+__device__ __forceinline__ P element(P row, int i) {
+    typedef const char GLOBAL *Bytes;
+    return (P)((Bytes)row + (uint32_t)i * (uint32_t)sizeof(*row));
+}
+
 // The whole vectors lane, lane + step, ... of a row of nv; -inf past them.
 // 16-bit rows that begin in the middle of a word are loaded from one element
 // earlier, in the same word, and shifted (align) once they are there: 8,192
-// rows of 128,003 bf16, half of them such, in 810 us, unshifted 902.  (Stores
-// shifted as well: 793 us, but 60,000 rows of 1,001 in 73 us instead of 67.)
+// rows of 128,003 bf16, half of them such, took 810 us so and 902 without.
+// (Stores shifted alike took longer, 4,096 rows 471 instead of 438 us; so did
+// whole 16-byte blocks read and written, by shifts of 0 to 7 elements.)
 template <typename E, int N>
 struct Logits {
+    static_assert(N <= 16, "a lane each");
     u32x4 v[N];
-    uint32_t last[N];   // the element that the next lane does not hold
+    uint32_t past;   // lane r's: the element after the last lane's vector r, but one
+    uint32_t end;    // the last element of the row's last vector
     __device__ __forceinline__ static bool odd(Ptr<E> row) {
-        return E::V == 8 && ((uint64_t)row & 2) != 0;
-    }
-    __device__ __forceinline__ static bool edge(int i, int nv) {
-        return threadIdx.x % 64 == 63 || i == nv - 1;
+        return E::V == 8 && __builtin_amdgcn_readfirstlane((int)((uint64_t)row & 2)) != 0;
     }
     __device__ __forceinline__ void load(Ptr<E> row, int lane, int step, int nv) {
         const bool shift = odd(row);
         const Ptr<E> from = shift ? row - 1 : row;
 #pragma unroll
         for (int r = 0; r < N; ++r) {
-            const int i = lane + r * step;
             v[r] = (u32x4){E::kLowest, E::kLowest, E::kLowest, E::kLowest};
-            if (i < nv) v[r] = load_vec<E, Use::Once>(from + i * E::V);
+            if (lane < nv - r * step)
+                v[r] = load_vec<E, Use::Once>(element(from + r * step * E::V, lane * E::V));
         }
         if (E::V != 8 || !shift) return;
-#pragma unroll
-        for (int r = 0; r < N; ++r) {
-            const int i = lane + r * step;
-            last[r] = 0;
-            if (i < nv && edge(i, nv)) last[r] = *(const uint16_t GLOBAL *)(row + i * E::V + 7);
-        }
+        const int l = threadIdx.x % 64, i = lane - l + 63 + l * step;
+        past = end = E::kLowest;
+        if (l < N && i < nv) past = *(const uint16_t GLOBAL *)(row + i * E::V + 7);
+        if (nv > 0) end = *(const uint16_t GLOBAL *)(row + nv * E::V - 1);
     }
     // Vectors FROM to FROM + M - 1 into their places.
     template <int FROM, int M>
     __device__ __forceinline__ void align(Ptr<E> row, int lane, int step, int nv) {
         if (E::V != 8 || !odd(row)) return;
+        const int first = __builtin_amdgcn_readfirstlane(lane);
 #pragma unroll
         for (int r = FROM; r < FROM + M; ++r) {
-            const int i = lane + r * step;
             const u32x4 a = v[r];
             uint32_t next = __builtin_amdgcn_update_dpp(0, (int)a.x, 0x130, 0xF, 0xF, true);
-            if (edge(i, nv)) next = last[r];
-            if (i < nv)
-                v[r] = (u32x4){__builtin_amdgcn_alignbit(a.y, a.x, 16),
-                               __builtin_amdgcn_alignbit(a.z, a.y, 16),
-                               __builtin_amdgcn_alignbit(a.w, a.z, 16), next << 16 | a.w >> 16};
+            const uint32_t last = __builtin_amdgcn_readlane(past, r);
+            next = threadIdx.x % 64 == 63 ? last : next;
+            const int i = first + r * step;
+            if (i < nv && nv <= i + 64 && lane + r * step == nv - 1) next = end;
+            v[r] = (u32x4){__builtin_amdgcn_alignbit(a.y, a.x, 16),
+                           __builtin_amdgcn_alignbit(a.z, a.y, 16),
+                           __builtin_amdgcn_alignbit(a.w, a.z, 16), next << 16 | a.w >> 16};
         }
     }
 };
@@ -198,27 +227,34 @@ struct Grad {
     float m, c, by, own;   // -(the factor) / S; the token's own element
 };
 
-// The gradient of those vectors, and of the element `tail` in its place.
+// The gradient of a vector's logits.
+template <typename E>
+__device__ __forceinline__ u32x4 make_grad(u32x4 v, const Grad &g) {
+    asm volatile("" : "+v"(v));
+    float x[E::V];
+    E::unpack(v, x);
+    if (__builtin_amdgcn_readfirstlane(is_fast(g.m, g.c))) {
+        const Fast power{g.c, g.m * g.c};
+#pragma unroll
+        for (int j = 0; j < E::V; ++j) x[j] = power(x[j]) * g.by;
+    } else {
+        const Slow power(g.c, g.m);
+#pragma unroll
+        for (int j = 0; j < E::V; ++j) x[j] = power(x[j]) * g.by;
+    }
+    return E::pack(x);
+}
+// The gradient of the vectors in their place.
 template <typename E, int N>
 __device__ __forceinline__ void store_grad(MutPtr<E> out, int lane, int step, int nv, const u32x4 *v,
                                            const Grad &g) {
-    auto write = [&](auto power) {
 #pragma unroll
-        for (int r = 0; r < N; ++r) {
-            u32x4 again = v[r];
-            asm volatile("" : "+v"(again));
-            float x[E::V];
-            E::unpack(again, x);
-#pragma unroll
-            for (int j = 0; j < E::V; ++j) x[j] = power(x[j]) * g.by;
-            if (lane + r * step < nv)
-                store_vec<E, Use::Once>(out + (lane + r * step) * E::V, E::pack(x));
-        }
-    };
-    if (__builtin_amdgcn_readfirstlane(is_fast(g.m, g.c))) write(Fast{g.c, g.m * g.c});
-    else write(Slow(g.c, g.m));
+    for (int r = 0; r < N; ++r) {
+        const u32x4 w = make_grad<E>(v[r], g);
+        if (lane < nv - r * step) store_vec<E, Use::Once>(element(out + r * step * E::V, lane * E::V), w);
+    }
 }
-// ... and of an element after them, in the first lanes.
+// ... and of an element after them, `tail`, in the first lanes.
 template <typename E>
 __device__ __forceinline__ void store_tail(MutPtr<E> out, int lane, int first, int n, float tail,
                                            const Grad &g) {
@@ -250,20 +286,27 @@ __device__ __forceinline__ void zero_row(MutPtr<E> out, int64_t first, int64_t s
     for (int64_t i = n / E::V * E::V + first; i < n; i += step) out[i] = E::put(0.0f);
 }
 
-// How a row of `vecs` vectors is cut: L lanes hold R vectors each, lane l the
-// vectors l, l + L, ...; a wave's first min(R, 8) are a unit, its next ones
-// another.  Rows of more than 1024 * 16 vectors: blocks of so many.
-constexpr int kUnitVecs = 8, kBlockVecs = 1024 * 16;
+// How a row of `vecs` vectors is cut (policy_cut): L lanes hold R vectors each,
+// lane l the vectors l, l + L, ...; a wave's are a unit, or, of more than 8,
+// its first half is one and its second half another.  Rows of more than
+// kBlockVecs vectors: blocks of so many, cut alike.
+constexpr int unit_vecs(int r) { return r <= 8 ? r : r / 2; }
 
 // A row in the registers of L lanes: read once, its gradient written once.
+// Memory bounds it, and what a workgroup of 1,024 lanes computes while its
+// compute unit has no other to load: 8,192 rows of 128,000 bf16 in 767 us, 5.5
+// TB/s; of 128,003, a quarter of them left out, in 797, 4.6 TB/s, since a
+// wave's stores then begin and end within lines.  A loop over rows that sends
+// for the next one's logits while it stores took as long (768, 791).
 template <typename E, int L, int R, bool GRAD>
 __global__ __launch_bounds__(L < 256 ? 256 : L) void
 row_kernel(PolicyArgs a, Scratch w, float c, int64_t first) {
-    constexpr int B = L < 256 ? 256 : L, N = R < kUnitVecs ? R : kUnitVecs;
+    constexpr int B = L < 256 ? 256 : L, N = unit_vecs(R);
     constexpr int UNITS = L / 64 * (R / N);
     static_assert(UNITS <= 64 && R / N <= 2, "a lane each");
     const int lane = threadIdx.x % L;
-    const int64_t row = first + (int64_t)blockIdx.x * (B / L) + threadIdx.x / L;
+    const int64_t row = first + (int64_t)blockIdx.x * (B / L) +
+                        __builtin_amdgcn_readfirstlane(threadIdx.x / L);
     if (L < B && row >= a.rows) return;
     float weight;
     const int token = take_token(a, row, weight);
@@ -310,7 +353,7 @@ row_kernel(PolicyArgs a, Scratch w, float c, int64_t first) {
 template <typename E, int L, int R>
 __global__ __launch_bounds__(64) void unit_stats_kernel(PolicyArgs a, Scratch w, float c, int units,
                                                         int64_t first) {
-    constexpr int N = R < kUnitVecs ? R : kUnitVecs, OF_BLOCK = L / 64 * (R / N);
+    constexpr int N = unit_vecs(R), OF_BLOCK = L / 64 * (R / N);
     const int64_t item = first + blockIdx.x;
     const int64_t row = item / units;
     const int unit = (int)(item % units), block = unit / OF_BLOCK, of = unit % OF_BLOCK;
@@ -333,7 +376,7 @@ __global__ __launch_bounds__(64) void unit_stats_kernel(PolicyArgs a, Scratch w,
 template <typename E, int L, int R>
 __global__ __launch_bounds__(64) void unit_grad_kernel(PolicyArgs a, Scratch w, float c, int units,
                                                        int grads, int64_t first) {
-    constexpr int N = R < kUnitVecs ? R : kUnitVecs, OF_BLOCK = L / 64 * (R / N);
+    constexpr int N = unit_vecs(R), OF_BLOCK = L / 64 * (R / N);
     const int64_t item = first + blockIdx.x;   // (row, one of the `grads` units written)
     const int64_t row = item / grads;
     const int unit = (int)(item % grads), block = unit / OF_BLOCK, of = unit % OF_BLOCK;
@@ -417,7 +460,10 @@ hipError_t over_blocks(int64_t blocks, F &&launch) {
     return hipSuccess;
 }
 
-// Rows longer than this and fewer than kFewRows go by units.
+// Fewer rows than this of 1,024 lanes go by units, as rows longer than a
+// workgroup holds do: by units and by rows, 16 rows of 128,003 bf16 14.7 and
+// 22.9 us, 64 19.0 and 23.7 (log-probabilities 9.0 and 11.7); 16 of 60,003, of
+// 512 lanes, 14.4 and 16.4, but their log-probabilities 8.6 and 7.4.
 constexpr int64_t kFewRows = 128;
 
 template <typename E, int L, int R>
@@ -448,14 +494,28 @@ hipError_t start_policy(const PolicyArgs &a, hipStream_t s) {
                     (float *)(ws + plan.at)};
     const float c = (float)(1.4426950408889634 * a.inv_temperature);
     const int64_t nv = (a.vocab + E::V - 1) / E::V;
-    const int units = plan.units;
-    hipError_t e;
-    if (nv <= 64) e = start_rows<E, 64, 1>(a, w, c, units, false, s);
-    else if (nv <= 256) e = start_rows<E, 64, 4>(a, w, c, units, false, s);
-    else if (nv <= 1024) e = start_rows<E, 256, 4>(a, w, c, units, false, s);
-    else if (nv <= 4096) e = start_rows<E, 256, 16>(a, w, c, units, a.rows < kFewRows, s);
-    else if (nv <= 8192) e = start_rows<E, 512, 16>(a, w, c, units, a.rows < kFewRows, s);
-    else e = start_rows<E, 1024, 16>(a, w, c, units, a.rows < kFewRows || nv > kBlockVecs, s);
+    const PolicyCut cut = policy_cut(nv);
+    const bool few = cut.lanes == 1024 && a.rows < kFewRows;
+    hipError_t e = hipErrorInvalidValue;
+    auto rows = [&](auto lanes, auto vecs) {
+        constexpr int L = decltype(lanes)::value, R = decltype(vecs)::value;
+        if (cut.lanes == L && cut.vecs == R)
+            e = start_rows<E, L, R>(a, w, c, plan.units, few || nv > kBlockVecs, s);
+    };
+    rows(Int<64>(), Int<1>());
+    rows(Int<64>(), Int<2>());
+    rows(Int<64>(), Int<4>());
+    rows(Int<64>(), Int<8>());
+    rows(Int<256>(), Int<4>());
+    rows(Int<256>(), Int<6>());
+    rows(Int<256>(), Int<8>());
+    rows(Int<256>(), Int<10>());
+    rows(Int<256>(), Int<16>());
+    rows(Int<512>(), Int<10>());
+    rows(Int<512>(), Int<16>());
+    rows(Int<1024>(), Int<10>());
+    rows(Int<1024>(), Int<12>());
+    rows(Int<1024>(), Int<16>());
     if (e != hipSuccess || a.sums == nullptr) return e;
     return start_sums(a, w, s);
 }

@@ -96,14 +96,18 @@ struct DropoutArgs {
 hipError_t launch_dropout(const DropoutArgs &a, hipStream_t s);
 
 constexpr int64_t kMaxLogits = int64_t(1) << 24;
-// Units of a row (aspis_policy.hip): 64 lanes and at most 8 vectors each.
-inline int policy_units(int64_t vocab, int elem_bytes) {
-    const int64_t vecs = (vocab * elem_bytes + 15) / 16;
-    if (vecs <= 256) return 1;
-    if (vecs <= 1024) return 4;
-    if (vecs <= 4096) return 8;
-    if (vecs <= 8192) return 16;
-    return (int)((vecs + 16383) / 16384) * 32;
+// How a row of so many 16-byte vectors is held by `lanes` lanes of `vecs` each,
+// and into how many units that cuts it: by its length alone.
+constexpr int kBlockVecs = 1024 * 16;
+struct PolicyCut {
+    int lanes, vecs, units;
+};
+inline PolicyCut policy_cut(int64_t nv) {
+    const int cuts[][2] = {{64, 1},  {64, 2},   {64, 4},   {64, 8},   {256, 4},   {256, 6},   {256, 8},
+                           {256, 10}, {256, 16}, {512, 10}, {512, 16}, {1024, 10}, {1024, 12}};
+    for (const auto &c : cuts)
+        if (nv <= c[0] * c[1]) return {c[0], c[1], c[0] / 64 * (c[1] > 8 ? 2 : 1)};
+    return {1024, 16, (int)((nv + kBlockVecs - 1) / kBlockVecs) * 32};
 }
 // Workgroups that add up the rows' terms, before one joins theirs.
 inline int sum_groups(int64_t rows) {
@@ -116,7 +120,7 @@ struct PolicyPlan {
 };
 inline PolicyPlan policy_plan(int64_t rows, int64_t vocab, int elem_bytes) {
     PolicyPlan p;
-    p.units = policy_units(vocab, elem_bytes);
+    p.units = policy_cut((vocab * elem_bytes + 15) / 16).units;
     p.terms = 0;                                   // double [3][rows], then [3][sum_groups]
     p.partial = p.terms + (size_t)rows * 3 * sizeof(double);
     p.stats = p.partial + (size_t)sum_groups(rows) * 3 * sizeof(double);   // float2 [rows][units]

@@ -392,6 +392,37 @@ def test_policy_loss(rows, vocab, kind, kl):
         assert (_bits(logits) == first).all()
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("vocab", [40, 300, 4099, 9000, 40_000])
+def test_rows_wherever_they_begin(vocab, kind):
+    """Logits and gradient at every place in a 16-byte block, many rows and
+    few: the same bits, and nothing written beside the rows."""
+    import torch
+    rows = 200
+    z, t, old, adv, w, refs = policy_inputs(rows, vocab, seed=2, kind=kind)
+    t[::7] = np.arange(len(t[::7])) % min(vocab, 9)            # in the first vectors
+    t[1::7] = vocab - 1 - np.arange(len(t[1::7])) % min(vocab, 9)   # and in the last
+    tokens, old, adv, w, refs = _cuda(t, old, adv, w, refs)
+    plain = None
+    places = range(8 if kind != "float32" else 4)
+    for at in places:
+        logits, _ = _padded(z.to(device()), 16, at)
+        for to in ((at + 3) % len(places), at):
+            grad, buf = _padded(torch.zeros_like(logits), 8, to)
+            bufs = aspis.policy_loss(logits, tokens, old, adv, w, ref=refs, kl=0.1, grad=grad)
+            got = _bits(grad), _bits(bufs.logps)
+            if plain is None:
+                plain = got
+            assert (got[0] == plain[0]).all() and (got[1] == plain[1]).all(), (at, to)
+            grad.fill_(7.0)
+            assert (f64(buf) == 7.0).all()
+            few = aspis.policy_loss(logits[:9], tokens[:9], old[:9], adv[:9], w[:9], ref=refs[:9],
+                                    kl=0.1, grad=grad[:9])
+            assert (_bits(grad[:9]) == plain[0][:9]).all() and (_bits(few.logps) == plain[1][:9]).all()
+            grad.fill_(7.0)
+            assert (f64(buf) == 7.0).all()
+
+
 @pytest.mark.parametrize("rows,vocab", [(700, 33), (600, 2500), (520, 9000), (300, 40_003)])
 @pytest.mark.parametrize("kind", ["float32", "bfloat16"])
 def test_policy_loss_of_many_rows(rows, vocab, kind):
