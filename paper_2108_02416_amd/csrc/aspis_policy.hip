@@ -61,7 +61,7 @@ __device__ __forceinline__ Stats join_lanes(Stats p, float c) {
 // as the scale, since a sum of powers up to 2^kRoom above it loses nothing in
 // f32: the largest of one element in V, which takes a third of the time of
 // the largest of all, and that one only where the sum says so.
-constexpr float kRoom = 0x1p100f;
+constexpr float kRoom = 0x1p60f;
 
 template <typename E, int N>
 __device__ __forceinline__ Stats unit_stats(const u32x4 *v, float tail, float c) {
@@ -270,7 +270,11 @@ __device__ __forceinline__ Grad finish_row(const PolicyArgs &a, const Scratch &w
     const double x = is_fast(st.m, c) ? ((double)z * c - (double)(st.m * c)) * 0.6931471805599453
                                       : (double)(z - st.m) * a.inv_temperature;
     const float p = (is_fast(st.m, c) ? Fast{c, st.m * c}(z) : Slow(c, st.m)(z)) / st.s;
-    float lp = (float)(x - (double)logf(st.s));
+    // ln S from its exponent and mantissa: S may lie far above 1, where an f32
+    // logarithm of all of it would lose what x cancels
+    const double ln_s = (double)logf(__builtin_amdgcn_frexp_mantf(st.s)) +
+                        0.6931471805599453 * __builtin_amdgcn_frexp_expf(st.s);
+    float lp = (float)(x - ln_s);
     // where the others' share is below f32's, and where a rounding went past 1
     if (p >= 1.0f || lp > 0.0f) lp = 0.0f;
     Terms t{0.0f, 0.0f, 0.0f, 0.0f};

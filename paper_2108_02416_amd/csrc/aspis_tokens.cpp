@@ -236,6 +236,14 @@ aspis_status aspis_policy_loss(const void *logits, int64_t rows, int64_t vocab, 
         !std::isfinite((float)(opt->grad_scale / opt->temperature)))
         return fail(ASPIS_ERR_INVALID_ARG, "%s: clip_low=%g clip_high=%g kl=%g grad_scale=%g", who,
                     opt->clip_low, opt->clip_high, opt->kl, opt->grad_scale);
+    // a position's inputs are read by several waves, after one may have written
+    const uintptr_t bytes = (uintptr_t)rows * 4;
+    for (const float *in : {old, advantage, weight, ref})
+        for (const float *to : {(const float *)logps, (const float *)sums}) {
+            const uintptr_t a = (uintptr_t)in, b = (uintptr_t)to, n = to == sums ? 12 : bytes;
+            if (rows > 0 && in != nullptr && a < b + n && b < a + bytes)
+                return fail(ASPIS_ERR_INVALID_ARG, "%s: logps or sums overlap an input", who);
+        }
     if (rows > 0 && ref == nullptr && opt->kl != 0.0)
         return fail(ASPIS_ERR_INVALID_ARG, "%s: kl=%g without ref", who, opt->kl);
     const aspis::PolicyArgs a{logits, rows, vocab, ld, dtype, {tokens, index == ASPIS_I64},

@@ -189,7 +189,7 @@ def test_embed_grad_of_three_rounds_of_merging(how):
     _check_embed_grad(grad, t, tokens, vocab, torch.empty((vocab, d), device=device()), 0.5)
 
 
-@pytest.mark.parametrize("vocab", [(1 << 21) - 2, (1 << 21) - 1, (1 << 21) + 5, 1 << 24])
+@pytest.mark.parametrize("vocab", [(1 << 21) - 1, (1 << 22) - 2, (1 << 22) - 1, (1 << 22) + 5, 1 << 24])
 def test_embed_grad_of_many_rows(vocab):
     """Either side of where a token and its place in a run fit 32 bits."""
     import torch
@@ -393,7 +393,7 @@ def test_policy_loss(rows, vocab, kind, kl):
 
 
 @pytest.mark.parametrize("kind", KINDS)
-@pytest.mark.parametrize("vocab", [40, 300, 4099, 9000, 40_000])
+@pytest.mark.parametrize("vocab", [40, 300, 4099, 9000, 40_000, 90_001])
 def test_rows_wherever_they_begin(vocab, kind):
     """Logits and gradient at every place in a 16-byte block, many rows and
     few: the same bits, and nothing written beside the rows."""
@@ -489,6 +489,30 @@ def test_positions_left_out_are_not_read():
     w.zero_()   # nothing left at all
     bufs = aspis.policy_loss(logits, tokens, old, adv, w, ref=refs, kl=0.1, grad=grad)
     assert (bufs.sums == 0).all() and (grad == 0).all() and (bufs.logps == 0).all()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("vocab", [600, 9000, 70_000])
+@pytest.mark.parametrize("rise", [20.0, 60.0, 150.0])
+def test_a_logit_far_above_the_others(vocab, rise, kind):
+    """Wherever it is in a vector: the scale a unit takes is that of other
+    elements, or, where a sum says so, of all."""
+    import torch
+    rows = 24
+    z, t, old, adv, w, refs = policy_inputs(rows, vocab, seed=5, kind=kind, masked=0.0)
+    at = (np.arange(rows) * 37 + np.arange(rows) * (vocab // rows)) % vocab
+    z[np.arange(rows), at] = rise
+    t[::2] = at[::2]
+    lp = Policy(f64(z), t).logps
+    old = (lp - 0.05).astype(np.float32)
+    refs = np.maximum(lp + 0.1, -1e4).astype(np.float32)
+    plain = Policy(f64(z), t, old, adv, w, refs, kl=0.05)
+    logits, tokens, old, adv, w, refs = _cuda(z, t, old, adv, w, refs)
+    grad = torch.empty_like(logits)
+    bufs = aspis.policy_loss(logits, tokens, old, adv, w, ref=refs, kl=0.05, grad=grad)
+    plain.check_logps(bufs.logps)
+    plain.check_sums(bufs.sums)
+    plain.check_grad(grad, kind)
 
 
 def test_rows_with_nan_or_infinity_say_so():

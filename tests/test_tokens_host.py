@@ -46,7 +46,7 @@ def _logps(z=P, rows=4, vocab=6, ld=6, kind=0, tokens=P, index=1, temperature=1.
 
 
 def _policy(z=P, rows=4, vocab=6, ld=6, kind=0, tokens=P, index=1, old=P, adv=P, weight=P, ref=P,
-            sums=P, logps=P, grad=Q, ldg=6, ws=P, size=WS, low=0.2, high=0.2, kl=0.0,
+            sums=P + 4096, logps=P + 8192, grad=Q, ldg=6, ws=P, size=WS, low=0.2, high=0.2, kl=0.0,
             temperature=1.0, scale=1.0):
     opt = aspis.PolicyOptions(low, high, kl, temperature, scale)
     return aspis.lib().aspis_policy_loss(z, rows, vocab, ld, kind, tokens, index, old, adv, weight,
@@ -92,7 +92,8 @@ NAN, INF = math.nan, math.inf
         {"logps": None}, {"grad": Q + 2}, {"ldg": 5}, {"grad": P + 4}, {"grad": P, "ldg": 8},
         {"low": -0.1}, {"low": 1.1}, {"low": NAN}, {"high": -1.0}, {"high": INF}, {"high": NAN},
         {"kl": -1.0}, {"kl": NAN}, {"kl": 1e39}, {"temperature": 0.0}, {"scale": INF},
-        {"scale": NAN}, {"scale": 1e30, "temperature": 1e-20}, {"ws": P + 2})],
+        {"scale": NAN}, {"scale": 1e30, "temperature": 1e-20}, {"ws": P + 2}, {"logps": P},
+        {"logps": P + 12}, {"logps": P - 12}, {"sums": P + 8}, {"sums": P - 8})],
     *[(SMALL, _policy, a) for a in ({"ws": None}, {"size": 10})],
 ])
 def test_refusals(status, call, args):
