@@ -172,10 +172,50 @@ __device__ __forceinline__ void sort_run(T (&key)[kSortKeys], T *lds) {
     sort_step<K, K / 2>(key, lds);
 }
 
+// Zeros in rows of the table's gradient but those whose bit in `skip` is set,
+// 2^shift lanes a row.
+template <typename EO>
+__device__ __forceinline__ void fill_rows(const EmbedGradArgs &a, int64_t first, int rows, int shift,
+                                          const uint32_t *skip) {
+    const int lane = (int)threadIdx.x & ((1 << shift) - 1);
+    const float zero[EO::V] = {};
+    const int64_t nv = a.d / EO::V;
+    for (int r = (int)threadIdx.x >> shift; r < rows; r += kBlock >> shift) {
+        if (skip != nullptr && (skip[r / 32] >> r % 32 & 1)) continue;
+        const MutPtr<EO> to = (MutPtr<EO>)a.out + (first + r) * a.ldo;
+        for (int64_t v = lane; v < nv; v += 1 << shift) store_floats<EO>(to + v * EO::V, zero);
+        for (int64_t i = nv * EO::V + lane; i < a.d; i += 1 << shift) to[i] = EO::put(0.0f);
+    }
+}
+
+constexpr int kZeroRows = 256;   // rows of a workgroup that fills in zeros, at most
+// Bytes of them: 32,768 tokens into 32,003 rows of 2,048 f32, 110 us without,
+// 107.5 with 64 MB, 104 with 96 or 160, 108 with 300.  Not where the tokens
+// are more than twice the rows, most of which would be written twice: 100,000
+// into 8,003 rows of 1,024, 96 us without, 99.7 with 96 MB.
+constexpr int64_t kEarlyBytes = 96 << 20;
+
+// Rows that are filled with zeros while the tokens are sorted, which leaves
+// memory idle: the last ones, from row `from` on, those with tokens too, which
+// are written again afterwards.
+struct EarlyRows {
+    int64_t from;
+    int rows, shift;   // of a workgroup; log2 of the lanes a row
+    int64_t runs;      // workgroups that sort, before those that fill
+};
+
 // Runs of kSortRun tokens, a workgroup each.  T: 32 bits where a token and
 // its place in the run fit them, else 64.
 template <typename T>
-__global__ __launch_bounds__(kBlock) void sort_runs_kernel(EmbedGradArgs a, Sorted out) {
+__global__ __launch_bounds__(kBlock) void sort_runs_kernel(EmbedGradArgs a, Sorted out, EarlyRows early) {
+    if (blockIdx.x >= early.runs) {
+        const int64_t first = early.from + ((int64_t)blockIdx.x - early.runs) * early.rows;
+        const int rows = (int)(a.vocab - first < early.rows ? a.vocab - first : early.rows);
+        with_type(a.out_dtype, [&](auto e) {
+            fill_rows<decltype(e)>(a, first, rows, early.shift, nullptr);
+        });
+        return;
+    }
     constexpr int kBits = 10;
     static_assert(kSortRun == 1 << kBits, "");
     __shared__ T lds[kSortRun];
@@ -258,30 +298,65 @@ __global__ __launch_bounds__(kMergeBlock) void merge_runs_kernel(Sorted in, Sort
     out.at[group + place] = in.at[group + i];
 }
 
-// Longer runs where they are, kMergeWide at a time, all searches a step at a
-// time.
+// The first position whose token is not below `token`; a wave looks at 64
+// places at once.
+__device__ __forceinline__ int64_t first_not_below(const uint32_t *sorted, int64_t n, uint32_t token) {
+    int64_t low = 0, high = n;   // the answer lies in [low, high]
+    while (low < high) {
+        const int64_t step = (high - low + 63) / 64;
+        const int64_t at = low + (int64_t)(threadIdx.x % 64) * step;
+        const int below = __popcll(__ballot(at < high && sorted[at] < token));
+        if (below == 0) return low;
+        const int64_t last = low + (below - 1) * step;   // the last place looked at that is below
+        low = last + 1;
+        high = last + step < high ? last + step : high;
+    }
+    return low;
+}
+
+// Longer runs where they are, kMergeWide at a time.  A workgroup's tokens are
+// neighbours in a run: its waves find where the lowest and the highest of
+// them would come in the other runs, and its threads search between, in all
+// runs a step at a time.
 constexpr int kMergeWide = 16;
 
 __global__ __launch_bounds__(kBlock) void merge_long_kernel(Sorted in, Sorted out, int64_t n,
                                                             int64_t length) {
-    const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
-    if (i >= n) return;
-    const int64_t group = i / (length * kMergeWide) * (length * kMergeWide);
+    __shared__ int64_t bounds[kMergeWide][2];
+    const int64_t i0 = (int64_t)blockIdx.x * kBlock, i = i0 + threadIdx.x;   // (all of one run)
+    const int64_t group = i0 / (length * kMergeWide) * (length * kMergeWide);
     const int64_t left = n - group;
-    const int own = (int)((i - group) / length);
+    const int own = (int)((i0 - group) / length);
     const int runs = (int)(left < length * kMergeWide ? (left + length - 1) / length : kMergeWide);
+    auto size = [&](int r) { return left - r * length < length ? left - r * length : length; };
+    const uint32_t lowest = in.token[i0], highest = in.token[i0 + kBlock <= n ? i0 + kBlock - 1 : n - 1];
+    for (int p = threadIdx.x / 64; p < 2 * runs; p += kBlock / 64) {
+        const int r = p / 2;
+        const int64_t at = r == own ? 0 : first_not_below(in.token + group + r * length, size(r),
+                                                          p % 2 ? highest + 1 : lowest);
+        if (threadIdx.x % 64 == 0) bounds[r][p % 2] = at;
+    }
+    __syncthreads();
+    int64_t widest = 0;
+    for (int r = 0; r < runs; ++r) {
+        const int64_t w = bounds[r][1] - bounds[r][0];
+        if (w > widest) widest = w;
+    }
+    if (i >= n) return;
     const uint32_t token = in.token[i];
-    uint32_t below[kMergeWide];
+    int64_t below[kMergeWide];
 #pragma unroll
-    for (int r = 0; r < kMergeWide; ++r) below[r] = 0;
-    for (int64_t step = length; step > 0; step /= 2) {
+    for (int r = 0; r < kMergeWide; ++r) below[r] = r < runs ? bounds[r][0] : 0;
+    int64_t step = 1;
+    while (step <= widest) step *= 2;
+    for (step /= 2; step > 0; step /= 2) {
 #pragma unroll
         for (int r = 0; r < kMergeWide; ++r) {
             if (r >= runs || r == own) continue;
-            const int64_t at = below[r] + step, first = group + r * length;
-            if (at > length || first + at > n) continue;
-            const uint32_t other = in.token[first + at - 1];
-            if (other < token || (r < own && other == token)) below[r] += step;
+            const int64_t at = below[r] + step;
+            if (at > bounds[r][1]) continue;
+            const uint32_t other = in.token[group + r * length + at - 1];
+            if (other < token || (r < own && other == token)) below[r] = at;
         }
     }
     int64_t place = i - group - own * length;
@@ -311,7 +386,8 @@ struct SumArgs {
     int64_t windows;
     int slabs, tail;     // waves that share a row's whole vectors; 1 for the elements after
     int64_t sum_blocks;  // workgroups of windows; the others fill rows with zeros:
-    int zero_rows, zero_shift;   // so many each, 2^shift lanes a row
+    int zero_rows, zero_shift;   // so many each, 2^shift lanes a row, up to row
+    int64_t zero_end;            // zero_end
     int64_t first;       // the launch's first workgroup
 };
 
@@ -344,23 +420,6 @@ __device__ __forceinline__ void finish_row(const EmbedGradArgs &a, uint32_t toke
     }
 }
 
-constexpr int kZeroRows = 256;   // rows of a workgroup that fills in zeros, at most
-
-// The first position whose token is not below `token`; a wave looks at 64
-// places at once.
-__device__ __forceinline__ int64_t first_not_below(const uint32_t *sorted, int64_t n, uint32_t token) {
-    int64_t low = 0, high = n;   // the answer lies in [low, high]
-    while (low < high) {
-        const int64_t step = (high - low + 63) / 64;
-        const int64_t at = low + (int64_t)(threadIdx.x % 64) * step;
-        const int below = __popcll(__ballot(at < high && sorted[at] < token));
-        if (below == 0) return low;
-        const int64_t last = low + (below - 1) * step;   // the last place looked at that is below
-        low = last + 1;
-        high = last + step < high ? last + step : high;
-    }
-    return low;
-}
 
 // Zeros in those of a workgroup's g.zero_rows rows that no token names.
 template <typename EO>
@@ -370,7 +429,7 @@ __device__ __forceinline__ void zero_rows(const SumArgs &g, int64_t block) {
     const EmbedGradArgs &a = g.a;
     const uint32_t *sorted = g.sorted.token;
     const int64_t first = block * g.zero_rows;
-    const int rows = (int)(a.vocab - first < g.zero_rows ? a.vocab - first : g.zero_rows);
+    const int rows = (int)(g.zero_end - first < g.zero_rows ? g.zero_end - first : g.zero_rows);
     if (threadIdx.x < kZeroRows / 32) there[threadIdx.x] = 0;
     if (threadIdx.x < 128) {
         const int64_t at = first_not_below(sorted, a.n, (uint32_t)(first + threadIdx.x / 64 * rows));
@@ -394,15 +453,7 @@ __device__ __forceinline__ void zero_rows(const SumArgs &g, int64_t block) {
         if (low < end && sorted[low] == token) atomicOr(&there[threadIdx.x / 32], 1u << threadIdx.x % 32);
     }
     __syncthreads();
-    const int lane = (int)threadIdx.x & ((1 << g.zero_shift) - 1);
-    const float zero[EO::V] = {};
-    const int64_t nv = a.d / EO::V;
-    for (int r = (int)threadIdx.x >> g.zero_shift; r < rows; r += kBlock >> g.zero_shift) {
-        if (there[r / 32] >> r % 32 & 1) continue;
-        const MutPtr<EO> to = (MutPtr<EO>)a.out + (first + r) * a.ldo;
-        for (int64_t v = lane; v < nv; v += 1 << g.zero_shift) store_floats<EO>(to + v * EO::V, zero);
-        for (int64_t i = nv * EO::V + lane; i < a.d; i += 1 << g.zero_shift) to[i] = EO::put(0.0f);
-    }
+    fill_rows<EO>(a, first, rows, g.zero_shift, there);
 }
 
 // N columns of a lane from col on, of the segments and pieces that begin in
@@ -995,6 +1046,14 @@ hipError_t launch_embed_grad(const EmbedGradArgs &a, hipStream_t s) {
             });
         });
     const EmbedGradPlan plan = embed_grad_plan(a.n, a.d);
+    const int64_t row_bytes = a.d * (a.out_dtype == ASPIS_F32 ? 4 : 2);
+    // enough rows a workgroup to be worth the search that comes first
+    EarlyRows early{a.vocab, a.d >= 512 ? 16 : a.d >= 64 ? 64 : kZeroRows,
+                    lane_shift(row_bytes / 16 + 1), 0};
+    if (!a.accumulate && a.n <= 2 * a.vocab) {
+        const int64_t most = kEarlyBytes / row_bytes;
+        early.from = a.vocab > most ? a.vocab - most : 0;
+    }
     char *ws = (char *)a.ws;
     auto array = [&](int i) { return (uint32_t *)(ws + i * plan.words); };
     Sorted sorted{array(0), array(1)}, other{array(2), array(3)};
@@ -1005,9 +1064,10 @@ hipError_t launch_embed_grad(const EmbedGradArgs &a, hipStream_t s) {
         return hipGetLastError();
     };
     {
-        const unsigned runs = (unsigned)((a.n + kSortRun - 1) / kSortRun);
-        if (a.vocab < (1 << 22) - 1) sort_runs_kernel<uint32_t><<<runs, kBlock, 0, s>>>(a, sorted);
-        else sort_runs_kernel<uint64_t><<<runs, kBlock, 0, s>>>(a, sorted);
+        early.runs = (a.n + kSortRun - 1) / kSortRun;
+        const unsigned blocks = (unsigned)(early.runs + (a.vocab - early.from + early.rows - 1) / early.rows);
+        if (a.vocab < (1 << 22) - 1) sort_runs_kernel<uint32_t><<<blocks, kBlock, 0, s>>>(a, sorted, early);
+        else sort_runs_kernel<uint64_t><<<blocks, kBlock, 0, s>>>(a, sorted, early);
         hipError_t e = hipGetLastError();
         if (e == hipSuccess && a.n > kSortRun) {
             auto merge = [&](auto share) {   // about a workgroup per compute unit
@@ -1042,10 +1102,10 @@ hipError_t launch_embed_grad(const EmbedGradArgs &a, hipStream_t s) {
         g.slabs = (int)((a.d / N + 63) / 64);
         g.tail = a.d % N != 0;
         g.sum_blocks = (g.windows * (g.slabs + g.tail) + kBlock / 64 - 1) / (kBlock / 64);
-        // enough zeros a workgroup to be worth the search that comes first
-        g.zero_rows = a.d >= 512 ? 16 : a.d >= 64 ? 64 : kZeroRows;
-        g.zero_shift = lane_shift((a.d + EO::V - 1) / EO::V);
-        const int64_t zero = a.accumulate ? 0 : (a.vocab + g.zero_rows - 1) / g.zero_rows;
+        g.zero_rows = early.rows;
+        g.zero_shift = early.shift;
+        g.zero_end = a.accumulate ? 0 : early.from;
+        const int64_t zero = (g.zero_end + g.zero_rows - 1) / g.zero_rows;
         const hipError_t st = over_blocks(g.sum_blocks + zero, [&](int64_t first, unsigned n) {
             g.first = first;
             sum_rows_kernel<EI, EO><<<n, kBlock, 0, s>>>(g);
