@@ -39,16 +39,26 @@ struct EmbedArgs {
 };
 hipError_t launch_embed(const EmbedArgs &a, hipStream_t s);
 
-// The gradient of up to kFewTokens tokens takes one launch and no workspace.
+// Whether a gradient takes one launch, each workgroup searching all tokens for
+// its rows': not where many tokens meet in a row, whose workgroup the others
+// would wait for.  In one launch and by sorting, rows of 512, us: 200 tokens
+// into 2 rows 14.1 and 14.3, into 16 rows 9.2 and 16.0; 700 into 2 rows 34.1 and
+// 14.8, into 64 rows 16.8 and 16.0, into 128 rows 15.4 and 16.6; 1,024 of 2,048
+// into 10,000 rows 33.8 and 30.5.
 constexpr int kFewTokens = 768;
-// Of more: tokens sorted in runs of kSortRun, kMergeRuns of them merged
+inline bool embed_few(int64_t n, int64_t vocab) {
+    return n <= kFewTokens && (n <= 256 || n <= 8 * vocab);
+}
+// Otherwise tokens are sorted in runs of kSortRun, kMergeRuns of them merged
 // in LDS, longer ones where they are; then the sums of the sorted positions'
 // segments, window by window of positions, long ones in pieces of at most a
 // block of two windows that are joined afterwards.
 constexpr int kSortRun = 1024, kMergeRuns = 32;
 // log2 of a window's positions: a function of n alone, since the order of a
-// sum follows it.
-inline int embed_shift(int64_t n) { return n <= 4096 ? 3 : 5; }
+// sum follows it.  Small ones give few tokens more waves, large ones cut fewer
+// segments.  8 and 32 positions, rows of 2,048 bf16, us: 4,096 tokens 55 and 69,
+// 16,384 69 and 77 (into 4 rows 47 and 40), 24,000 82 and 81, 32,768 96 and 88.
+inline int embed_shift(int64_t n) { return n <= 16384 ? 3 : 5; }
 inline int64_t embed_row(int64_t d) { return (d + 3) / 4 * 4; }   // floats of a partial sum
 struct EmbedGradPlan {
     int shift;       // log2 of a window's positions
@@ -62,7 +72,6 @@ inline EmbedGradPlan embed_grad_plan(int64_t n, int64_t d) {
     p.blocks = (n + (2 << p.shift) - 1) / (2 << p.shift);
     p.words = (size_t)((n + 3) / 4 * 16 + 32);
     p.bytes = 4 * p.words + (size_t)(p.blocks * 2 * embed_row(d)) * sizeof(float);
-    if (n <= kFewTokens) p.bytes = 0;
     return p;
 }
 struct EmbedGradArgs {

@@ -131,6 +131,7 @@ __device__ __forceinline__ uint64_t lane_xor(uint64_t v) {
 // A bitonic sort of kSortRun keys, kSortKeys a thread: key r of thread t is
 // number t * kSortKeys + r.  Keys meet in a thread, between lanes, and
 // through LDS between waves.  No two are equal (but those past the end).
+// Its steps, one after the other, bound it: 5.3 us for one run.
 constexpr int kSortKeys = kSortRun / kBlock;
 
 // Step J of the merge to sequences of K.
@@ -457,7 +458,8 @@ __device__ __forceinline__ void zero_rows(const SumArgs &g, int64_t block) {
 }
 
 // N columns of a lane from col on, of the segments and pieces that begin in
-// a window: the same window in all lanes.
+// a window: the same window in all lanes, so that what is decided by tokens
+// is decided in scalar registers.
 template <typename EI, typename EO, int N>
 __device__ __forceinline__ void sum_window(const SumArgs &g, int64_t window, int64_t col) {
     constexpr int W = N == 1 ? 1 : N / EI::V, U = 8;
@@ -554,8 +556,9 @@ __device__ __forceinline__ void sum_window(const SumArgs &g, int64_t window, int
     flush(tail_cut);
 }
 
-// A wave for every window and 64 vectors of a row.  Reading the gradient's
-// rows bounds it, with what the table's rows take.
+// A wave for every window and 64 vectors of a row, eight rows on their way at
+// a time.  Memory bounds it: of 32,768 rows of 2,048 bf16, with the rows of
+// zeros that sorting left over, 300 MB in 58 us, 5.2 TB/s.
 template <typename EI, typename EO>
 __global__ __launch_bounds__(kBlock) void sum_rows_kernel(SumArgs g) {
     constexpr int N = EI::V > EO::V ? EI::V : EO::V;
@@ -648,11 +651,12 @@ __global__ __launch_bounds__(kBlock) void join_pieces_kernel(SumArgs g, int64_t 
 // ---------------------------------------------------------------------------
 // its gradient, of few tokens, in one launch
 
-// Up to kFewTokens tokens are not sorted as a whole: a workgroup takes some
-// rows of the table and 64 vectors of them, picks the rows' tokens out of all
-// of them, sorts those few, and its waves share them evenly; sums of a segment
-// that several waves hold are joined in LDS, in order.  Three launches less:
-// 515 tokens of 257 f32 into 4,099 rows take XX us (14.3 by sorting all).
+// Up to kFewTokens tokens, not too many a row, are not sorted as a whole: a
+// workgroup takes some rows of the table and 64 vectors of them, picks the
+// rows' tokens out of all of them, sorts those few, and its waves share them
+// evenly; sums of a segment that several waves hold are joined in LDS, in
+// order.  Latency bounds it, in one launch instead of three: 515 tokens of 257
+// f32 into 4,099 rows in 9.1 us, 15.0 by sorting all.
 constexpr int kFewRows = 64;   // of a workgroup, at most
 
 struct FewArgs {
@@ -1026,7 +1030,7 @@ hipError_t launch_embed(const EmbedArgs &a, hipStream_t s) {
 
 hipError_t launch_embed_grad(const EmbedGradArgs &a, hipStream_t s) {
     if (a.vocab == 0 || a.d == 0 || (a.n == 0 && a.accumulate)) return hipSuccess;
-    if (a.n <= kFewTokens)
+    if (embed_few(a.n, a.vocab))
         return with_types(a.dtype, a.out_dtype, [&](auto from, auto to) {
             typedef decltype(from) EI;
             typedef decltype(to) EO;
@@ -1035,11 +1039,15 @@ hipError_t launch_embed_grad(const EmbedGradArgs &a, hipStream_t s) {
             g.a = a;
             g.slabs = (int)((a.d / N + 63) / 64);
             g.tail = a.d % N != 0;
-            // few rows, so that the waves of the commonest tokens' workgroup have
-            // little to do, but enough of them for what each workgroup reads first
-            const int64_t slabs = g.slabs + g.tail;
+            // few rows, so that the commonest tokens' workgroup has little to do, but
+            // not so few that reading the tokens takes most of the time: 700 into
+            // 10,000 rows of 1,024, 19 us with 4 rows, 23 with 16; 100 into 131,072 of
+            // 7, 7.2 with 64, 13 with 16
+            const int64_t slabs = g.slabs + g.tail, width = a.d < 256 ? a.d : 256;
             g.rows = kFewRows;
-            while (g.rows > 4 && (a.vocab + g.rows / 4 - 1) / (g.rows / 4) * slabs <= 4096) g.rows /= 4;
+            while (g.rows > 4 && (a.vocab + g.rows / 4 - 1) / (g.rows / 4) * slabs <= 8192 &&
+                   g.rows / 4 * width >= 256)
+                g.rows /= 4;
             return over_blocks((a.vocab + g.rows - 1) / g.rows * slabs, [&](int64_t first, unsigned n) {
                 g.first = first;
                 few_tokens_kernel<EI, EO><<<n, kBlock, 0, s>>>(g);

@@ -17,7 +17,7 @@ hipError_t launch_embed(const EmbedArgs &a, hipStream_t) {
 hipError_t launch_embed_grad(const EmbedGradArgs &a, hipStream_t) {
     const EmbedGradPlan p = embed_grad_plan(a.n, a.d);
     if ((p.blocks << (p.shift + 1)) < a.n || p.words < (size_t)a.n * 4 + 32 || p.words % 16 != 0) abort();
-    if (a.n > kFewTokens && p.bytes != 4 * p.words + (size_t)p.blocks * 2 * embed_row(a.d) * 4) abort();
+    if (p.bytes != 4 * p.words + (size_t)p.blocks * 2 * embed_row(a.d) * 4) abort();
     ++reached;
     return hipSuccess;
 }

@@ -179,6 +179,18 @@ def test_embed_grad_shapes(n, vocab, d, how):
         _check_embed_grad(grad, t, tokens, vocab, out, 0.7, accumulate)
 
 
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("n,vocab", [(256, 1), (257, 1), (256, 32), (257, 32), (257, 33), (768, 95),
+                                     (768, 96), (16_384, 4), (16_384, 900), (16_385, 4), (16_385, 900)])
+def test_embed_grad_where_another_way_begins(n, vocab, accumulate):
+    import torch
+    d = 130
+    grad = _randn((n, d), "bfloat16", seed=n)
+    t, tokens = _tokens(n, vocab, seed=n + vocab, how="uniform")
+    out = _randn((vocab, d), seed=1) if accumulate else torch.full((vocab, d), 7.0, device=device())
+    _check_embed_grad(grad, t, tokens, vocab, out, 0.7, accumulate)
+
+
 @pytest.mark.parametrize("how", ["zipf", "one"])
 def test_embed_grad_of_three_rounds_of_merging(how):
     """More than 16 * 16 runs of 2,048 tokens."""
