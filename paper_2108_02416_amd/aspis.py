@@ -1029,11 +1029,15 @@ def _token_place(tokens, n: int, index: int):
     return place[0], place[2]
 
 
-def _floats(name: str, t, n: int, index: int) -> int:
-    """The address of a contiguous float32 tensor of n elements at least."""
+def _floats(name: str, t, n: int, index: int, exact: bool = True) -> int:
+    """The address of a contiguous float32 tensor of n elements (or at least so
+    many)."""
     at = _tensors().buffer(t, _float32(), n, index)
-    return at if at is not None else \
-        _buffer(name, t, _float32(), n, _torch().device("cuda", index))
+    if at is None:
+        at = _buffer(name, t, _float32(), n, _torch().device("cuda", index))
+    if exact and t.numel() != n:
+        raise AspisError(ERR_INVALID_ARG, f"{name} must hold {n} numbers (got {tuple(t.shape)})")
+    return at
 
 
 def _scratch_at(ws, index: int) -> int:
@@ -1240,7 +1244,7 @@ def policy_loss(logits, tokens, old, advantage, weight, ref=None, clip=(0.2, 0.2
              _floats("old", old, rows, index), _floats("advantage", advantage, rows, index),
              _floats("weight", weight, rows, index),
              _floats("ref", ref, rows, index) if ref is not None else None, ctypes.byref(opt),
-             _floats("bufs.sums", bufs.sums, 3, index),
-             _floats("bufs.logps", bufs.logps, rows, index), to, ldg, _scratch_at(ws, index),
+             _floats("bufs.sums", bufs.sums, 3, index, False),
+             _floats("bufs.logps", bufs.logps, rows, index, False), to, ldg, _scratch_at(ws, index),
              ws.numel())
     return bufs

@@ -700,7 +700,7 @@ def test_refusals():
     import torch
     f, dev = torch.float32, device()
     x, t = torch.zeros((4, 6), device=dev), torch.zeros(4, dtype=torch.int64, device=dev)
-    v = torch.zeros(4, device=dev)
+    v, long_v = torch.zeros(4, device=dev), torch.zeros(5, device=dev)
     long, many = torch.zeros((2000, 6), device=dev), torch.zeros(2000, dtype=torch.int64, device=dev)
     bad = [
         lambda: aspis.embed(x, t.to(torch.int16)), lambda: aspis.embed(x, t.cpu()),
@@ -734,6 +734,8 @@ def test_refusals():
         lambda: aspis.token_logps(x, t, logps=v[:3]), lambda: aspis.token_logps(x, t[:3]),
         lambda: aspis.token_logps(x, t, ws=torch.zeros(8, dtype=torch.uint8, device=dev)),
         lambda: aspis.policy_loss(x, t, v, v, v.double()), lambda: aspis.policy_loss(x, t, v[:3], v, v),
+        lambda: aspis.policy_loss(x, t, long_v, v, v), lambda: aspis.policy_loss(x, t, v, long_v, v),
+        lambda: aspis.policy_loss(x, t, v, v, long_v), lambda: aspis.policy_loss(x, t, v, v, v, ref=long_v),
         lambda: aspis.policy_loss(x, t, v, v, v, kl=0.1), lambda: aspis.policy_loss(x, t, v, v, v, ref=v.cpu()),
         lambda: aspis.policy_loss(x, t, v, v, v, clip=(1.5, 0.2)),
         lambda: aspis.policy_loss(x, t, v, v, v, clip=(0.2, -0.1)),
