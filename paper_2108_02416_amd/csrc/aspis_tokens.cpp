@@ -5,6 +5,7 @@
 
 #include <cmath>
 #include <cstdint>
+#include <initializer_list>
 
 #include "../../include/aspis.h"
 #include "aspis_errors.h"
@@ -44,12 +45,42 @@ aspis_status check_rows(const char *who, const Rows &x) {
     return ASPIS_OK;
 }
 
-// Whether two sets of rows share memory, apart from being the same ones.
-bool overlap(const Rows &a, const Rows &b, bool may_be_same) {
-    if (a.empty() || b.empty()) return false;
-    if (may_be_same && a.at == b.at && a.dtype == b.dtype && (a.ld == b.ld || a.rows == 1))
-        return false;
-    return a.begin() < b.end() && b.begin() < a.end();
+// n values of `size` bytes, as a row.  (More than memory holds: of no rows, so
+// that nothing is written.)
+Rows array(const char *name, const void *at, int64_t n, int64_t size) {
+    const int64_t d = at != nullptr && n <= kMaxElements / 8 ? (n * size + 3) / 4 : 0;
+    return {name, at, 1, d, d, ASPIS_F32};
+}
+
+// Whether two sets of rows share memory.  Columns of the same rows do not.
+bool overlap(const Rows &a, const Rows &b) {
+    if (a.empty() || b.empty() || a.begin() >= b.end() || b.begin() >= a.end()) return false;
+    const uintptr_t size_a = elem_bytes(a.dtype), size_b = elem_bytes(b.dtype);
+    const uintptr_t pitch = a.ld * size_a;
+    if (pitch != b.ld * size_b) return true;
+    const bool swap = b.begin() < a.begin();
+    const uintptr_t apart = (swap ? a.begin() - b.begin() : b.begin() - a.begin()) % pitch;
+    return apart < (swap ? b.d * size_b : a.d * size_a) ||
+           apart + (swap ? a.d * size_a : b.d * size_b) > pitch;
+}
+
+// Whether they are the same rows.
+bool same(const Rows &a, const Rows &b) {
+    return a.at == b.at && a.dtype == b.dtype && (a.ld == b.ld || a.rows == 1);
+}
+
+// What a call writes shares no memory, nor any with what it reads.
+aspis_status check_apart(const char *who, std::initializer_list<Rows> written,
+                         std::initializer_list<Rows> read) {
+    for (const Rows *w = written.begin(); w != written.end(); ++w) {
+        for (const Rows *v = w + 1; v != written.end(); ++v)
+            if (overlap(*w, *v))
+                return fail(ASPIS_ERR_INVALID_ARG, "%s: %s and %s overlap", who, w->name, v->name);
+        for (const Rows &r : read)
+            if (overlap(*w, r))
+                return fail(ASPIS_ERR_INVALID_ARG, "%s: %s overlaps %s", who, w->name, r.name);
+    }
+    return ASPIS_OK;
 }
 
 // n tokens, or n values of `size` bytes.
@@ -97,8 +128,7 @@ aspis_status aspis_embed(const void *table, int64_t vocab, int64_t d, int64_t ld
     CHECK(check_tokens(who, tokens, n, index));
     if (!std::isfinite((float)scale))
         return fail(ASPIS_ERR_INVALID_ARG, "%s: scale=%g", who, scale);
-    if (overlap(from, to, false))
-        return fail(ASPIS_ERR_INVALID_ARG, "%s: out overlaps the table", who);
+    CHECK(check_apart(who, {to}, {from, array("tokens", tokens, n, index == ASPIS_I64 ? 8 : 4)}));
     const aspis::EmbedArgs a{table, vocab, d, ld, dtype, {tokens, index == ASPIS_I64}, n,
                              (float)scale, out, ldo, out_dtype};
     return launched(aspis::launch_embed(a, static_cast<hipStream_t>(stream)), who);
@@ -129,8 +159,8 @@ aspis_status aspis_embed_grad(const void *grad, int64_t n, int64_t d, int64_t ld
     if (flags & ~ASPIS_EMBED_ACCUMULATE)
         return fail(ASPIS_ERR_INVALID_ARG, "%s: unknown flags 0x%x", who, flags);
     CHECK(check_workspace(who, workspace, ws_bytes, need));
-    if (overlap(from, to, false))
-        return fail(ASPIS_ERR_INVALID_ARG, "%s: out overlaps grad", who);
+    CHECK(check_apart(who, {to, array("workspace", workspace, need, 1)},
+                      {from, array("tokens", tokens, n, index == ASPIS_I64 ? 8 : 4)}));
     const aspis::EmbedGradArgs a{grad, n, d, ld, dtype, {tokens, index == ASPIS_I64},
                                  (float)scale, out, vocab, ldo, out_dtype,
                                  (flags & ASPIS_EMBED_ACCUMULATE) != 0, workspace};
@@ -150,8 +180,10 @@ aspis_status aspis_dropout(const void *x, int64_t rows, int64_t d, int64_t ld,
     if (!(p >= 0.0 && p <= 1.0)) return fail(ASPIS_ERR_INVALID_ARG, "%s: p=%g", who, p);
     if ((uintptr_t)seed_at % 8 != 0)
         return fail(ASPIS_ERR_INVALID_ARG, "%s: seed_at is misaligned", who);
-    if (overlap(from, to, true) || (residual != nullptr && overlap(res, to, true)))
+    if ((!same(from, to) && overlap(from, to)) ||
+        (residual != nullptr && !same(res, to) && overlap(res, to)))
         return fail(ASPIS_ERR_INVALID_ARG, "%s: out overlaps an input without being it", who);
+    CHECK(check_apart(who, {to}, {array("seed_at", seed_at, 1, 8)}));
     const double limit = std::nearbyint(p * 65536.0);
     const aspis::DropoutArgs a{x, rows, d, ld, dtype, (uint32_t)limit,
                                limit < 65536.0 ? (float)(65536.0 / (65536.0 - limit)) : 0.0f, seed,
@@ -168,12 +200,12 @@ size_t aspis_policy_workspace(int64_t rows, int64_t vocab, aspis_dtype dtype) {
 
 namespace {
 
-// What the two calls on logits check alike.
+// What the two calls on logits check alike.  need: bytes of workspace.
 aspis_status check_logits(const char *who, const Rows &z, const void *tokens, int index,
                           double temperature, const float *logps, const void *ws,
-                          size_t ws_bytes) {
+                          size_t ws_bytes, size_t &need) {
     CHECK(check_rows(who, z));
-    const size_t need = aspis_policy_workspace(z.rows, z.d, (aspis_dtype)z.dtype);
+    need = aspis_policy_workspace(z.rows, z.d, (aspis_dtype)z.dtype);
     if (need == SIZE_MAX || z.rows > aspis::kMaxTokens)
         return fail(ASPIS_ERR_OVERFLOW, "%s: rows=%lld vocab=%lld", who, (long long)z.rows,
                     (long long)z.d);
@@ -193,7 +225,10 @@ aspis_status aspis_token_logps(const void *logits, int64_t rows, int64_t vocab, 
                                size_t ws_bytes, void *stream) {
     const char *who = "aspis_token_logps";
     const Rows z{"logits", logits, rows, vocab, ld, dtype};
-    CHECK(check_logits(who, z, tokens, index, temperature, logps, workspace, ws_bytes));
+    size_t need;
+    CHECK(check_logits(who, z, tokens, index, temperature, logps, workspace, ws_bytes, need));
+    CHECK(check_apart(who, {array("logps", logps, rows, 4), array("workspace", workspace, need, 1)},
+                      {z, array("tokens", tokens, rows, index == ASPIS_I64 ? 8 : 4)}));
     aspis::PolicyArgs a{};
     a.logits = logits;
     a.rows = rows;
@@ -217,7 +252,8 @@ aspis_status aspis_policy_loss(const void *logits, int64_t rows, int64_t vocab, 
     if (opt == nullptr) return fail(ASPIS_ERR_INVALID_ARG, "%s: NULL options", who);
     const Rows z{"logits", logits, rows, vocab, ld, dtype};
     const Rows g{"grad", grad, rows, vocab, ldg, dtype};
-    CHECK(check_logits(who, z, tokens, index, opt->temperature, logps, workspace, ws_bytes));
+    size_t need;
+    CHECK(check_logits(who, z, tokens, index, opt->temperature, logps, workspace, ws_bytes, need));
     CHECK(check_array(who, "old", old, rows, 4));
     CHECK(check_array(who, "advantage", advantage, rows, 4));
     CHECK(check_array(who, "weight", weight, rows, 4));
@@ -226,7 +262,7 @@ aspis_status aspis_policy_loss(const void *logits, int64_t rows, int64_t vocab, 
         return fail(ASPIS_ERR_INVALID_ARG, "%s: ref is misaligned", who);
     if (grad != nullptr) {
         CHECK(check_rows(who, g));
-        if (overlap(z, g, true))
+        if (!same(z, g) && overlap(z, g))
             return fail(ASPIS_ERR_INVALID_ARG, "%s: grad overlaps the logits without being them",
                         who);
     }
@@ -237,13 +273,16 @@ aspis_status aspis_policy_loss(const void *logits, int64_t rows, int64_t vocab, 
         return fail(ASPIS_ERR_INVALID_ARG, "%s: clip_low=%g clip_high=%g kl=%g grad_scale=%g", who,
                     opt->clip_low, opt->clip_high, opt->kl, opt->grad_scale);
     // a position's inputs are read by several waves, after one may have written
-    const uintptr_t bytes = (uintptr_t)rows * 4;
-    for (const float *in : {old, advantage, weight, ref})
-        for (const float *to : {(const float *)logps, (const float *)sums}) {
-            const uintptr_t a = (uintptr_t)in, b = (uintptr_t)to, n = to == sums ? 12 : bytes;
-            if (rows > 0 && in != nullptr && a < b + n && b < a + bytes)
-                return fail(ASPIS_ERR_INVALID_ARG, "%s: logps or sums overlap an input", who);
-        }
+    const Rows to = grad != nullptr ? g : Rows{"grad", nullptr, 0, 0, 0, dtype};
+    CHECK(check_apart(who,
+                      {to, array("logps", logps, rows, 4), array("sums", sums, 3, 4),
+                       array("workspace", workspace, need, 1)},
+                      {array("tokens", tokens, rows, index == ASPIS_I64 ? 8 : 4),
+                       array("old", old, rows, 4), array("advantage", advantage, rows, 4),
+                       array("weight", weight, rows, 4), array("ref", ref, rows, 4)}));
+    CHECK(check_apart(who,
+                      {array("logps", logps, rows, 4), array("sums", sums, 3, 4),
+                       array("workspace", workspace, need, 1)}, {z}));
     if (rows > 0 && ref == nullptr && opt->kl != 0.0)
         return fail(ASPIS_ERR_INVALID_ARG, "%s: kl=%g without ref", who, opt->kl);
     const aspis::PolicyArgs a{logits, rows, vocab, ld, dtype, {tokens, index == ASPIS_I64},

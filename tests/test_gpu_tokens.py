@@ -701,6 +701,7 @@ def test_refusals():
     f, dev = torch.float32, device()
     x, t = torch.zeros((4, 6), device=dev), torch.zeros(4, dtype=torch.int64, device=dev)
     v, long_v = torch.zeros(4, device=dev), torch.zeros(5, device=dev)
+    wide = torch.zeros(24, device=dev)
     long, many = torch.zeros((2000, 6), device=dev), torch.zeros(2000, dtype=torch.int64, device=dev)
     bad = [
         lambda: aspis.embed(x, t.to(torch.int16)), lambda: aspis.embed(x, t.cpu()),
@@ -736,6 +737,9 @@ def test_refusals():
         lambda: aspis.policy_loss(x, t, v, v, v.double()), lambda: aspis.policy_loss(x, t, v[:3], v, v),
         lambda: aspis.policy_loss(x, t, long_v, v, v), lambda: aspis.policy_loss(x, t, v, long_v, v),
         lambda: aspis.policy_loss(x, t, v, v, long_v), lambda: aspis.policy_loss(x, t, v, v, v, ref=long_v),
+        lambda: aspis.embed(x, wide.view(torch.int64)[:4], out=wide.view(4, 6)),
+        lambda: aspis.dropout(x[:1], 0.1, x.view(torch.int64)[0, :1], out=x[:1]),
+        lambda: aspis.token_logps(x, t, logps=x[0, :4]),
         lambda: aspis.policy_loss(x, t, v, v, v, kl=0.1), lambda: aspis.policy_loss(x, t, v, v, v, ref=v.cpu()),
         lambda: aspis.policy_loss(x, t, v, v, v, clip=(1.5, 0.2)),
         lambda: aspis.policy_loss(x, t, v, v, v, clip=(0.2, -0.1)),
@@ -752,6 +756,35 @@ def test_refusals():
             raise AssertionError(i)
     assert (x == 0).all() and (v == 0).all()
     assert aspis.token_logps(x, t).dtype == f
+
+
+@pytest.mark.parametrize("d", [6, 64, 257])
+@pytest.mark.parametrize("kind", KINDS)
+def test_columns_of_one_tensor(kind, d):
+    """Results beside inputs in the same rows, which share no memory."""
+    import torch
+    rows = 40
+    x = _randn((rows, d), kind, seed=d)
+    _, t = _tokens(rows, d, seed=d)
+    v = _randn((rows,), seed=3)
+
+    def beside():
+        both = torch.full((rows, 2 * d + 3), 7.0, dtype=x.dtype, device=x.device)
+        both[:, :d] = x
+        return both, both[:, :d], both[:, d + 3:]
+
+    def policy(a, out):
+        aspis.policy_loss(a, t, v, v, v, ref=v, kl=0.1, grad=out)
+        return out
+
+    for call in (lambda a, out: aspis.dropout(a, 0.3, 5, residual=a, out=out),
+                 lambda a, out: aspis.embed(a, t % rows, out=out),
+                 lambda a, out: aspis.embed_grad(a, t % rows, rows, out=out), policy):
+        both, a, out = beside()
+        call(a, out)
+        want = call(x, torch.empty_like(x))
+        assert (_bits(out.contiguous()) == _bits(want)).all()
+        assert (_bits(a.contiguous()) == _bits(x)).all() and (both[:, d:d + 3] == 7.0).all()
 
 
 @pytest.mark.parametrize("rows,d", [(0, 5), (3, 0), (0, 0)])

@@ -16,7 +16,8 @@ from _tokens import Policy, embed_sums, kept, philox, policy_inputs, softmax_los
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 ROCM = "/opt/rocm"
-P, Q = 1 << 40, 1 << 41   # addresses that nothing reads: every call below is refused
+# addresses that nothing reads: every call below is refused
+P, Q, W = 1 << 40, 1 << 41, 1 << 42
 BAD, SMALL, OVER = aspis.ERR_INVALID_ARG, aspis.ERR_BUFFER_SMALL, aspis.ERR_OVERFLOW
 WS = 1 << 24
 
@@ -28,7 +29,7 @@ def _embed(table=P, vocab=9, d=6, ld=6, kind=0, tokens=P, n=4, index=1, scale=1.
 
 
 def _embed_grad(grad=P, n=4, d=6, ld=6, kind=0, tokens=P, index=1, scale=1.0, out=Q, vocab=9,
-                ldo=6, to=0, flags=0, ws=P, size=WS):
+                ldo=6, to=0, flags=0, ws=W, size=WS):
     return aspis.lib().aspis_embed_grad(grad, n, d, ld, kind, tokens, index, scale, out, vocab, ldo,
                                         to, flags, ws, size, None)
 
@@ -39,14 +40,14 @@ def _dropout(x=P, rows=4, d=6, ld=6, kind=0, p=0.1, seed=1, at=None, offset=0, r
                                      None)
 
 
-def _logps(z=P, rows=4, vocab=6, ld=6, kind=0, tokens=P, index=1, temperature=1.0, logps=P, ws=P,
+def _logps(z=P, rows=4, vocab=6, ld=6, kind=0, tokens=P, index=1, temperature=1.0, logps=Q, ws=W,
            size=WS):
     return aspis.lib().aspis_token_logps(z, rows, vocab, ld, kind, tokens, index, temperature, logps,
                                          ws, size, None)
 
 
 def _policy(z=P, rows=4, vocab=6, ld=6, kind=0, tokens=P, index=1, old=P, adv=P, weight=P, ref=P,
-            sums=P + 4096, logps=P + 8192, grad=Q, ldg=6, ws=P, size=WS, low=0.2, high=0.2, kl=0.0,
+            sums=P + 4096, logps=P + 8192, grad=Q, ldg=6, ws=W, size=WS, low=0.2, high=0.2, kl=0.0,
             temperature=1.0, scale=1.0):
     opt = aspis.PolicyOptions(low, high, kl, temperature, scale)
     return aspis.lib().aspis_policy_loss(z, rows, vocab, ld, kind, tokens, index, old, adv, weight,
@@ -67,7 +68,7 @@ NAN, INF = math.nan, math.inf
     *[(BAD, _embed_grad, a) for a in (
         {"grad": None}, {"grad": P + 2}, {"tokens": None}, {"tokens": P + 2, "index": 0},
         {"out": None}, {"out": Q + 2}, {"vocab": -1}, {"d": -1}, {"n": -1}, {"ld": 5}, {"ldo": 5},
-        {"kind": 3}, {"to": 5}, {"index": -1}, {"scale": NAN}, {"flags": 2}, {"ws": P + 8, "n": 2000},
+        {"kind": 3}, {"to": 5}, {"index": -1}, {"scale": NAN}, {"flags": 2}, {"ws": W + 8, "n": 2000},
         {"out": P + 48})],
     *[(SMALL, _embed_grad, a) for a in ({"ws": None}, {"size": 100}, {"n": 1 << 20, "size": 1 << 20})],
     *[(OVER, _embed_grad, a) for a in ({"vocab": 1 << 31}, {"n": (1 << 30) + 1},
@@ -81,7 +82,7 @@ NAN, INF = math.nan, math.inf
         {"z": None}, {"z": P + 1}, {"rows": -1}, {"vocab": -1}, {"ld": 5}, {"kind": 4},
         {"tokens": None}, {"tokens": P + 4}, {"index": 7}, {"temperature": 0.0},
         {"temperature": -1.0}, {"temperature": NAN}, {"temperature": INF}, {"temperature": 1e-31},
-        {"logps": None}, {"logps": P + 2}, {"ws": P + 4})],
+        {"logps": None}, {"logps": Q + 2}, {"ws": W + 4})],
     *[(SMALL, _logps, a) for a in ({"ws": None}, {"size": 0})],
     *[(OVER, _logps, a) for a in ({"vocab": (1 << 24) + 1, "ld": 1 << 25},
                                   {"rows": (1 << 30) + 1})],
@@ -91,13 +92,36 @@ NAN, INF = math.nan, math.inf
         {"logps": None}, {"grad": Q + 2}, {"ldg": 5}, {"grad": P + 4}, {"grad": P, "ldg": 8},
         {"low": -0.1}, {"low": 1.1}, {"low": NAN}, {"high": -1.0}, {"high": INF}, {"high": NAN},
         {"kl": -1.0}, {"kl": NAN}, {"kl": 1e39}, {"temperature": 0.0}, {"scale": INF},
-        {"scale": NAN}, {"scale": 1e30, "temperature": 1e-20}, {"ws": P + 2}, {"logps": P},
+        {"scale": NAN}, {"scale": 1e30, "temperature": 1e-20}, {"ws": W + 2}, {"logps": P},
         {"logps": P + 12}, {"logps": P - 12}, {"sums": P + 8}, {"sums": P - 8})],
     *[(SMALL, _policy, a) for a in ({"ws": None}, {"size": 10})],
 ])
 def test_refusals(status, call, args):
     assert call(**args) == status, args
     assert aspis.lib().aspis_last_error()
+
+
+# what is written shares no memory with anything else
+@pytest.mark.parametrize("call,args", [
+    *[(_embed, a) for a in ({"tokens": Q}, {"tokens": Q + 88}, {"tokens": Q - 24},
+                            {"out": P + 24, "tokens": Q}, {"table": Q + 20, "ld": 6})],
+    *[(_embed_grad, a) for a in ({"tokens": Q}, {"ws": P}, {"ws": Q}, {"ws": Q + 208},
+                                 {"tokens": W}, {"tokens": W + 16})],
+    *[(_dropout, a) for a in ({"at": Q}, {"at": Q + 88}, {"out": P + 24, "ldo": 7},
+                              {"x": P, "ld": 12, "out": P + 20, "ldo": 12},
+                              {"x": P, "ld": 12, "out": P + 28, "ldo": 12},
+                              {"x": P, "ld": 12, "out": P + 24, "ldo": 13})],
+    *[(_logps, a) for a in ({"logps": P}, {"logps": P + 92}, {"tokens": Q, "index": 0},
+                            {"tokens": W}, {"ws": P}, {"ws": Q}, {"rows": 1, "vocab": 1, "logps": P})],
+    *[(_policy, a) for a in (
+        {"tokens": Q}, {"tokens": P + 8192}, {"tokens": P + 4096}, {"sums": P + 8196},
+        {"sums": Q}, {"logps": Q + 92}, {"logps": P + 92}, {"ws": P}, {"ws": Q},
+        {"ws": P + 4096}, {"old": W}, {"ref": W + 16}, {"adv": Q},
+        {"weight": Q + 4}, {"ref": Q}, {"ldg": 12, "ld": 12, "grad": P + 20})],
+])
+def test_outputs_over_inputs(call, args):
+    assert call(**args) == BAD, args
+    assert b"overlap" in aspis.lib().aspis_last_error()
 
 
 def test_null_options():
