@@ -26,7 +26,8 @@
  * returns a message for the calling thread's last failure.
  *
  * Asynchrony: aspis_detect, aspis_aggregate, the norm, clipping and update
- * calls and the token operators only enqueue work on the stream.  aspis_clique is host code.
+ * calls and the token operators only enqueue work on the stream.
+ * aspis_clique is host code.
  * aspis_detect_aggregate synchronises the stream (it needs the agreement
  * graph on the host) and returns with its work complete.
  *
@@ -562,8 +563,10 @@ aspis_status aspis_clipped_adamw(const aspis_chunk *params, const aspis_chunk *g
  * start to the next, elements aligned to their type.  All entry points only
  * enqueue work; scratch comes through the caller's workspace, which needs no
  * particular contents.  Calls that overlap must not share workspaces or
- * outputs.  Results must not overlap inputs except where a call says so.
- * Every result is rounded to its type once, from f32. */
+ * outputs.  What a call writes, its workspace included, must not overlap
+ * anything else it takes, except where it says so; columns beside each other
+ * in the same rows do not overlap.  Every result is rounded to its type once,
+ * from f32. */
 typedef enum { ASPIS_I32 = 0, ASPIS_I64 = 1 } aspis_index;
 
 /* Embedding lookup: out_i = scale * table_(t_i) for the n tokens t_i, rounded
@@ -618,7 +621,8 @@ size_t aspis_policy_workspace(int64_t rows, int64_t vocab, aspis_dtype dtype);
  * t_i under softmax(logits_i / temperature); 0 for a token outside
  * [0, vocab), whose logits are not read.  vocab is at most 2^24, rows 2^30,
  * the temperature between 1e-30 and 1e30.  A row with a NaN or +inf, or of
- * -inf alone, gives NaN. */
+ * -inf alone, gives NaN.  A row's result, and its gradient below, depend on
+ * that row alone, not on the others of the call. */
 aspis_status aspis_token_logps(const void *logits, int64_t rows, int64_t vocab,
                                int64_t ld, aspis_dtype dtype, const void *tokens,
                                aspis_index index, double temperature, float *logps,

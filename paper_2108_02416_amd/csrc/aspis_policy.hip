@@ -58,7 +58,7 @@ __device__ __forceinline__ Stats join_lanes(Stats p, float c) {
 }
 
 // Of N vectors a lane, and one element.  Any power near the largest will do
-// as the scale, since a sum of powers up to 2^kRoom above it loses nothing in
+// as the scale, since a sum of up to kRoom relative to it loses nothing in
 // f32: the largest of one element in V, which takes a third of the time of
 // the largest of all, and that one only where the sum says so.
 constexpr float kRoom = 0x1p60f;
