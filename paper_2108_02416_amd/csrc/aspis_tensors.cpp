@@ -77,6 +77,43 @@ int type_code(at::ScalarType t) {
     return t == at::kFloat ? 0 : t == at::kBFloat16 ? 1 : t == at::kHalf ? 2 : -1;
 }
 
+// How a tensor [..., d] holds rows of contiguous elements, equally far apart.
+struct RowLayout {
+    int64_t rows, d, ld;   // ld: elements from one row's start to the next's
+};
+
+// False where it does not: also where rows share memory, as those of a
+// dimension that was expanded.
+bool row_layout(const at::Tensor &t, RowLayout &to) {
+    if (t.dim() < 1 || t.numel() == 0) return false;
+    const int64_t d = t.size(-1);
+    if (d > 1 && t.stride(-1) != 1) return false;
+    int64_t ld = d, run = 1;   // run: rows of the dimensions so far
+    for (int64_t i = t.dim() - 2; i >= 0; --i) {
+        if (t.size(i) == 1) continue;
+        if (run == 1) ld = t.stride(i);   // the first that holds more than one
+        if (ld < d || t.stride(i) != ld * run) return false;
+        run *= t.size(i);
+    }
+    to = {run, d, ld};
+    return true;
+}
+
+// layout(x) -> (rows, d, elements between rows) of a tensor on any device, as
+// place() has it, or None.
+PyObject *layout(PyObject *, PyObject *arg) {
+    if (!THPVariable_Check(arg)) Py_RETURN_NONE;
+    try {
+        const at::Tensor &t = THPVariable_Unpack(arg);
+        RowLayout r;
+        if (t.layout() != at::kStrided || !row_layout(t, r)) Py_RETURN_NONE;
+        return Py_BuildValue("LLL", (long long)r.rows, (long long)r.d, (long long)r.ld);
+    } catch (const std::exception &e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+        return nullptr;
+    }
+}
+
 // place(x) -> (address, rows, d, elements between rows, type code of aspis.h,
 // device index) of a GPU tensor [..., d] that holds rows of contiguous
 // elements, equally far apart; or None.
@@ -84,22 +121,12 @@ PyObject *place(PyObject *, PyObject *arg) {
     if (!THPVariable_Check(arg)) Py_RETURN_NONE;
     try {
         const at::Tensor &t = THPVariable_Unpack(arg);
-        if (!t.is_cuda() || t.layout() != at::kStrided || t.dim() < 1 || t.numel() == 0 || t.is_neg())
-            Py_RETURN_NONE;
+        if (!t.is_cuda() || t.layout() != at::kStrided || t.is_neg()) Py_RETURN_NONE;
         const int code = type_code(t.scalar_type());
-        const int64_t dims = t.dim(), d = t.size(-1), rows = t.numel() / d;
-        if (code < 0 || (d > 1 && t.stride(-1) != 1)) Py_RETURN_NONE;
-        int64_t ld = 0, run = 1;   // rows of the dimensions so far
-        for (int64_t i = dims - 2; i >= 0; --i) {
-            if (t.size(i) == 1) continue;
-            if (ld == 0) ld = t.stride(i);
-            else if (t.stride(i) != ld * run) Py_RETURN_NONE;
-            run *= t.size(i);
-        }
-        if (run == 1) ld = d;
-        if (ld < d) Py_RETURN_NONE;
-        return Py_BuildValue("KLLLii", (unsigned long long)(uintptr_t)t.data_ptr(), (long long)rows,
-                             (long long)d, (long long)ld, code, (int)t.get_device());
+        RowLayout r;
+        if (code < 0 || !row_layout(t, r)) Py_RETURN_NONE;
+        return Py_BuildValue("KLLLii", (unsigned long long)(uintptr_t)t.data_ptr(), (long long)r.rows,
+                             (long long)r.d, (long long)r.ld, code, (int)t.get_device());
     } catch (const std::exception &e) {
         PyErr_SetString(PyExc_RuntimeError, e.what());
         return nullptr;
@@ -198,6 +225,7 @@ PyObject *apart_py(PyObject *, PyObject *const *args, Py_ssize_t count) {
 PyMethodDef methods[] = {
     {"apart", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(apart_py)),
      METH_FASTCALL, "Whether lists of spans share no memory."},
+    {"layout", layout, METH_O, "Rows, length and distance of a tensor of rows, or None."},
     {"place", place, METH_O,
      "Address, rows, length, distance, type code and device index of a GPU tensor of rows."},
     {"tokens", tokens, METH_O,
