@@ -101,6 +101,16 @@ using Ptr = const typename E::T GLOBAL *;
 template <typename E>
 using MutPtr = typename E::T GLOBAL *;
 
+// A product rounded to E.  To f16 the compiler would make one instruction of
+// both where a single element is stored, which adds +0 and so makes +0 of -0,
+// unlike those of pack: the same element would have other bits by where it
+// stands.  It is not to see that x is a product.
+template <typename E>
+__device__ __forceinline__ typename E::T put_product(float x) {
+    if constexpr (E::V == 8) asm("" : "+v"(x));
+    return E::put(x);
+}
+
 // Once: the data is not needed again soon (non-temporal).
 enum class Use { Again, Once };
 

@@ -260,7 +260,7 @@ __device__ __forceinline__ void store_tail(MutPtr<E> out, int lane, int first, i
                                            const Grad &g) {
     if (first + lane >= n) return;
     const float p = is_fast(g.m, g.c) ? Fast{g.c, g.m * g.c}(tail) : Slow(g.c, g.m)(tail);
-    out[first + lane] = E::put(p * g.by);
+    out[first + lane] = put_product<E>(p * g.by);
 }
 
 // The end of a row's statistics: its log-probability, terms and gradient.
@@ -349,7 +349,7 @@ row_kernel(PolicyArgs a, Scratch w, float c, int64_t first) {
     store_grad<E, R>(out, lane, L, nv, x.v, g);
     store_tail<E>(out, lane, nv * E::V, n, tail, g);
     // the token's own, over what the same lane has just written
-    if (lane == (token < nv * E::V ? token / E::V % L : token - nv * E::V)) out[token] = E::put(g.own);
+    if (lane == (token < nv * E::V ? token / E::V % L : token - nv * E::V)) out[token] = put_product<E>(g.own);
 }
 
 // Few rows, and rows longer than the registers of a workgroup: a wave for
@@ -419,10 +419,10 @@ __global__ __launch_bounds__(64) void unit_grad_kernel(PolicyArgs a, Scratch w, 
     // the token's own, over what the same lane has just written
     const int of_token = token / E::V - i0;
     if (token < nv * E::V && of_token >= 0 && of_token < N * L && of_token % L == 0)
-        out[token] = E::put(g.own);
+        out[token] = put_product<E>(g.own);
     if (unit != 0) return;
     if (nv * E::V + lane < n) store_tail<E>(out, lane, nv * E::V, n, E::get(z[nv * E::V + lane]), g);
-    if (lane == token - nv * E::V) out[token] = E::put(g.own);
+    if (lane == token - nv * E::V) out[token] = put_product<E>(g.own);
 }
 
 // The loss and the two other sums, in fp64 and an order that the number of

@@ -99,7 +99,7 @@ __global__ __launch_bounds__(kBlock) void embed_kernel(EmbedArgs a, int shift) {
 #pragma unroll
             for (int u = 0; u < U; ++u)
                 if (row0 + u < a.n)
-                    to(u)[i] = EO::put(token[u] >= 0 ? EI::get(from(u)[i]) * a.scale : 0.0f);
+                    to(u)[i] = put_product<EO>(token[u] >= 0 ? EI::get(from(u)[i]) * a.scale : 0.0f);
     }
 }
 
@@ -415,7 +415,7 @@ __device__ __forceinline__ void finish_row(const EmbedGradArgs &a, uint32_t toke
     const MutPtr<EO> to = (MutPtr<EO>)a.out + (int64_t)token * a.ldo + col;
     if constexpr (N == 1) {
         const float v = x[0] * a.scale;
-        *to = EO::put(a.accumulate ? EO::get(*to) + v : v);
+        *to = put_product<EO>(a.accumulate ? EO::get(*to) + v : v);
     } else {
         float y[N] = {};
         if (a.accumulate) load_floats<EO, N>((Ptr<EO>)to, y);
@@ -649,7 +649,7 @@ __global__ __launch_bounds__(kBlock) void join_pieces_kernel(SumArgs g, int64_t 
         if (col + j >= a.d) continue;
         const MutPtr<EO> out = (MutPtr<EO>)a.out + (int64_t)token * a.ldo + col + j;
         v *= a.scale;
-        *out = EO::put(a.accumulate ? EO::get(*out) + v : v);
+        *out = put_product<EO>(a.accumulate ? EO::get(*out) + v : v);
     }
 }
 
@@ -900,7 +900,7 @@ __global__ __launch_bounds__(kBlock) void dropout_kernel(DropoutArgs a, DropPlan
             const uint32_t word = j < 4 ? (j < 2 ? bits.x : bits.y) : (j < 6 ? bits.z : bits.w);
             float y = kept(word, j) ? E::get(((Ptr<E>)a.x)[row * a.ld + at]) * a.scale : 0.0f;
             if constexpr (RES) y += E::get(((Ptr<E>)a.residual)[row * a.ldr + at]);
-            ((MutPtr<E>)a.out)[row * a.ldo + at] = E::put(y);
+            ((MutPtr<E>)a.out)[row * a.ldo + at] = put_product<E>(y);
         }
         return;
     }
@@ -951,7 +951,7 @@ __global__ __launch_bounds__(kBlock) void dropout_kernel(DropoutArgs a, DropPlan
         for (int j = 0; j < 8; ++j) {
             float y = kept(bits[j / 2], j) ? E::get(v[j]) * a.scale : 0.0f;
             if constexpr (RES) y += E::get(add[j]);
-            if ((i0 + j >= 0) & (i0 + j < a.d)) out[j] = E::put(y);
+            if ((i0 + j >= 0) & (i0 + j < a.d)) out[j] = put_product<E>(y);
         }
     }
 }

@@ -1,0 +1,101 @@
+"""Zeros of either sign have one sign wherever they stand: in whole vectors
+and in the elements after them, in whole blocks of positions and in cut ones,
+and by every kernel that may take a row.  Bits are compared."""
+import numpy as np
+import pytest
+
+from paper_2108_02416_amd import aspis
+
+from _helpers import device
+from _tokens import kept
+
+pytestmark = pytest.mark.gpu
+
+KINDS = ["float32", "bfloat16", "float16"]
+
+
+def _type(kind):
+    import torch
+    return getattr(torch, kind)
+
+
+def _zeros(shape, kind):
+    import torch
+    return torch.full(shape, -0.0, dtype=_type(kind), device=device())
+
+
+def _negative(x):
+    """Where x, of zeros alone, holds -0."""
+    import torch
+    assert (x == 0).all()
+    return torch.signbit(x).cpu().numpy()
+
+
+@pytest.mark.parametrize("scale", [1.0, 3.0])
+@pytest.mark.parametrize("kind,to", [(k, t) for k in KINDS for t in KINDS])
+@pytest.mark.parametrize("n,d", [(5, 1), (9, 7), (33, 257), (3, 2501), (1_050_000, 7), (300_000, 33)])
+def test_rows_of_negative_zeros_are_looked_up(n, d, kind, to, scale):
+    import torch
+    tokens = torch.arange(n, device=device()) % 4
+    out = torch.empty((n, d), dtype=_type(to), device=device())
+    assert _negative(aspis.embed(_zeros((4, d), kind), tokens, scale=scale, out=out)).all()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("rows,d,pad", [(1, 1003, 0), (9, 5, 3), (40, 33, 1), (7, 2049, 63)])
+@pytest.mark.parametrize("offset", [0, 3])
+def test_negative_zeros_are_kept_by_dropout(rows, d, pad, kind, offset):
+    x = _zeros((rows, d + pad), kind)[:, :d]
+    keep = kept(rows * d, 0.4, 7, offset).reshape(rows, d)
+    assert (_negative(aspis.dropout(x, 0.4, 7, offset=offset)) == keep).all()
+    # with a residual of -0: -0 where both are, +0 where x is dropped
+    res = _zeros((rows, d), kind)
+    assert (_negative(aspis.dropout(x, 0.4, 7, offset=offset, residual=res)) == keep).all()
+
+
+@pytest.mark.parametrize("kind,to", [(k, t) for k in KINDS for t in KINDS])
+@pytest.mark.parametrize("n", [20, 700, 3000, 20_000])
+@pytest.mark.parametrize("d", [1, 37, 300])
+def test_sums_of_zero_by_a_negative_factor(n, d, kind, to):
+    """Tokens' rows are -0 in all columns, rows without a token +0."""
+    import torch
+    vocab = 200
+    tokens = torch.arange(n, device=device()) % 150
+    tokens[n // 2:] = 3                               # a long one
+    out = torch.empty((vocab, d), dtype=_type(to), device=device())
+    got = _negative(aspis.embed_grad(_zeros((n, d), kind), tokens, vocab, scale=-2.0, out=out))
+    there = np.zeros(vocab, dtype=bool)
+    there[tokens.cpu().numpy()] = True
+    assert (got == there[:, None]).all()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("vocab", [5, 15, 307, 5003, 90_001])
+def test_gradients_of_a_certain_token(vocab, kind):
+    """One token's probability is 1 and the others' 0: the factors' signs, in
+    every element and by the kernels for few rows and for many."""
+    import torch
+    rows = 12
+    at = np.array([0, 1, vocab - 1, vocab - 2, vocab // 2, vocab // 3] * 2)
+    z = torch.zeros((rows, vocab))
+    z[np.arange(rows), at] = 300.0
+    adv = np.repeat([1.0, -1.0], rows // 2).astype(np.float32)
+    for own in (True, False):   # the token is the certain one, or another
+        t = at if own else (at + 1) % vocab
+        lp = 0.0 if own else -300.0
+        cuda = [torch.from_numpy(a).to(device()) for a in
+                (t, np.full(rows, lp, np.float32), adv, np.ones(rows, np.float32))]
+        for repeat in (1, 20):
+            many = [x.repeat_interleave(repeat, 0) for x in (z.to(_type(kind)).to(device()), *cuda)]
+            grad = torch.empty_like(many[0])
+            aspis.policy_loss(*many, grad=grad)
+            # -advantage (1[v = t] - p_v): both factors' signs
+            sign = np.broadcast_to(np.repeat(adv, repeat)[:, None] < 0, grad.shape).copy()
+            r, t_all, at_all = np.arange(rows * repeat), np.repeat(t, repeat), np.repeat(at, repeat)
+            sign[r, t_all] = ~sign[r, t_all]
+            got = torch.signbit(grad).cpu().numpy()
+            zero = (grad == 0).cpu().numpy()
+            want_zero = np.ones(grad.shape, dtype=bool)
+            if not own:
+                want_zero[r, t_all] = want_zero[r, at_all] = False
+            assert (zero == want_zero).all() and (got == sign)[zero].all()
