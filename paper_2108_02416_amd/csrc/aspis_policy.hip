@@ -13,7 +13,6 @@
 // the call has: files batched together or one by one give the same gradient.
 #include "aspis_tokens.h"
 
-#include <cfloat>
 #include <cmath>
 
 #include "aspis_elements.h"
@@ -25,9 +24,12 @@ namespace {
 constexpr int64_t kMaxGrid = int64_t(1) << 22;   // workgroups of one launch
 
 // 2^((z - m) c) as 2^(z c - k), k = m c rounded: one operation and one
-// rounding less, and the rounding of k is the same for every power of a row.
-// Where k leaves f32 (logits at the type's lowest value, a mask) the
-// difference comes first: its operands cannot be infinities of both signs.
+// rounding less.  k's rounding is a factor that all powers of a unit share, so
+// it cancels where they are divided by their sum; but it is half a step of k,
+// which has to be small beside 127: at |k| = 2^20 it is 2^-5, and from 2^31 on the
+// largest power itself may be infinite or 0.  Beyond (logits masked by a
+// constant, a low temperature) the difference comes first: its operands cannot be
+// infinities of both signs.
 struct Fast {
     float c, k;
     __device__ float operator()(float z) const { return __builtin_amdgcn_exp2f(fmaf(z, c, -k)); }
@@ -37,7 +39,16 @@ struct Slow {
     __device__ Slow(float c, float top) : c(c), m(top == -INFINITY ? 0.0f : top) {}
     __device__ float operator()(float z) const { return __builtin_amdgcn_exp2f((z - m) * c); }
 };
-__device__ __forceinline__ bool is_fast(float m, float c) { return fabsf(m * c) <= FLT_MAX; }
+__device__ __forceinline__ bool is_fast(float m, float c) { return fabsf(m * c) <= 0x1p20f; }
+
+// The factor of a sum of powers relative to `from` that makes it relative to
+// `to`, which is not below; each is Fast's k or Slow's m, by its size.
+__device__ __forceinline__ float rescale(float from, float to, float c) {
+    const float k = from * c;
+    const bool fast = is_fast(from, c);
+    if (is_fast(to, c)) return __builtin_amdgcn_exp2f(fast ? k - to * c : fmaf(from, c, -(to * c)));
+    return fast ? __builtin_amdgcn_exp2f(fmaf(-to, c, k)) : Slow(c, to)(from);
+}
 
 template <int N>
 struct Int {
@@ -53,8 +64,7 @@ struct Stats {
 // The same of every lane's, joined in lane order.
 __device__ __forceinline__ Stats join_lanes(Stats p, float c) {
     const float m = lanes_join<64>(p.m, Max());
-    const float by = is_fast(m, c) ? __builtin_amdgcn_exp2f(p.m * c - m * c) : Slow(c, m)(p.m);
-    return {m, lanes_join<64>(p.s == 0.0f ? 0.0f : p.s * by, Sum())};
+    return {m, lanes_join<64>(p.s == 0.0f ? 0.0f : p.s * rescale(p.m, m, c), Sum())};
 }
 
 // Of N vectors a lane, and one element.  Any power near the largest will do
@@ -266,9 +276,9 @@ __device__ __forceinline__ void store_tail(MutPtr<E> out, int lane, int first, i
 // The end of a row's statistics: its log-probability, terms and gradient.
 __device__ __forceinline__ Grad finish_row(const PolicyArgs &a, const Scratch &w, int64_t row,
                                            float weight, float z, Stats st, float c, bool writes) {
-    // (log2 of the power of the token, in f64: one rounding, in lp)
+    // (log2 of the power of the token, in f64: one rounding, in lp; f32 may not hold the difference)
     const double x = is_fast(st.m, c) ? ((double)z * c - (double)(st.m * c)) * 0.6931471805599453
-                                      : (double)(z - st.m) * a.inv_temperature;
+                                      : ((double)z - (double)st.m) * a.inv_temperature;
     const float p = (is_fast(st.m, c) ? Fast{c, st.m * c}(z) : Slow(c, st.m)(z)) / st.s;
     // ln S from its exponent and mantissa: S may lie far above 1, where an f32
     // logarithm of all of it would lose what x cancels
@@ -399,11 +409,9 @@ __global__ __launch_bounds__(64) void unit_grad_kernel(PolicyArgs a, Scratch w, 
     } else {
         // a lane's units first: 64 apart, in order, relative to their maximum
         for (int i = threadIdx.x; i < units; i += 64) p.m = fmaxf(p.m, of_row[i].m);
-        const bool fast = is_fast(p.m, c);
         for (int i = threadIdx.x; i < units; i += 64) {
             const Stats q = of_row[i];
-            const float by = fast ? __builtin_amdgcn_exp2f(q.m * c - p.m * c) : Slow(c, p.m)(q.m);
-            p.s += q.s == 0.0f ? 0.0f : q.s * by;
+            p.s += q.s == 0.0f ? 0.0f : q.s * rescale(q.m, p.m, c);
         }
     }
     const Grad g = finish_row(a, w, row, weight, w.at[row], join_lanes(p, c), c,
