@@ -73,6 +73,8 @@ __global__ __launch_bounds__(kBlock) void embed_kernel(EmbedArgs a, int shift) {
         for (int u = 0; u < U; ++u) token[u] = a.tokens.get(row0 + u < a.n ? row0 + u : a.n - 1, a.vocab);
         auto from = [&](int u) { return (Ptr<EI>)a.table + (token[u] < 0 ? 0 : token[u]) * a.ld; };
         auto to = [&](int u) { return (MutPtr<EO>)a.out + (row0 + u) * a.ldo; };
+        // (0 times a negative scale is -0)
+        auto scale = [&](int u) { return token[u] < 0 ? 0.0f : a.scale; };
         for (int64_t v = lane; v < nv; v += 1 << shift) {
             u32x4 x[U][W];
 #pragma unroll
@@ -90,7 +92,7 @@ __global__ __launch_bounds__(kBlock) void embed_kernel(EmbedArgs a, int shift) {
                     float z[EI::V];
                     EI::unpack(x[u][w], z);
 #pragma unroll
-                    for (int j = 0; j < EI::V; ++j) y[w * EI::V + j] = z[j] * a.scale;
+                    for (int j = 0; j < EI::V; ++j) y[w * EI::V + j] = z[j] * scale(u);
                 }
                 if (row0 + u < a.n) store_floats<EO, N, U == 1 ? Use::Again : Use::Once>(to(u) + v * N, y);
             }

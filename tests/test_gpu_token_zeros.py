@@ -41,6 +41,19 @@ def test_rows_of_negative_zeros_are_looked_up(n, d, kind, to, scale):
     assert _negative(aspis.embed(_zeros((4, d), kind), tokens, scale=scale, out=out)).all()
 
 
+@pytest.mark.parametrize("kind,to", [(k, t) for k in KINDS for t in KINDS])
+@pytest.mark.parametrize("n,d", [(5, 1), (9, 7), (33, 257), (3, 2501), (1_050_000, 7), (300_000, 33)])
+def test_padding_is_zero_whatever_the_scale(n, d, kind, to):
+    import torch
+    tokens = torch.arange(n, device=device()) % 6 - 1            # of a table of 4 rows
+    table = torch.ones((4, d), dtype=_type(kind), device=device())
+    out = torch.empty((n, d), dtype=_type(to), device=device())
+    aspis.embed(table, tokens, scale=-3.0, out=out)
+    none = (tokens < 0) | (tokens > 3)
+    assert not _negative(out[none]).any()
+    assert (out[~none] == -3.0).all()
+
+
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("rows,d,pad", [(1, 1003, 0), (9, 5, 3), (40, 33, 1), (7, 2049, 63)])
 @pytest.mark.parametrize("offset", [0, 3])
