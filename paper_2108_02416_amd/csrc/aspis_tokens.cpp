@@ -192,8 +192,8 @@ aspis_status aspis_dropout(const void *x, int64_t rows, int64_t d, int64_t ld,
 }
 
 size_t aspis_policy_workspace(int64_t rows, int64_t vocab, aspis_dtype dtype) {
-    if (elem_bytes(dtype) == 0 || rows < 0 || vocab < 0 || vocab > aspis::kMaxLogits ||
-        (rows > 0 && vocab > kMaxElements / rows))
+    if (elem_bytes(dtype) == 0 || rows < 0 || rows > aspis::kMaxTokens || vocab < 0 ||
+        vocab > aspis::kMaxLogits)
         return SIZE_MAX;
     return aspis::policy_plan(rows, vocab, elem_bytes(dtype)).bytes;
 }
@@ -206,7 +206,7 @@ aspis_status check_logits(const char *who, const Rows &z, const void *tokens, in
                           size_t ws_bytes, size_t &need) {
     CHECK(check_rows(who, z));
     need = aspis_policy_workspace(z.rows, z.d, (aspis_dtype)z.dtype);
-    if (need == SIZE_MAX || z.rows > aspis::kMaxTokens)
+    if (need == SIZE_MAX)
         return fail(ASPIS_ERR_OVERFLOW, "%s: rows=%lld vocab=%lld", who, (long long)z.rows,
                     (long long)z.d);
     CHECK(check_tokens(who, tokens, z.rows, index));

@@ -24,7 +24,7 @@ struct Tokens {
 };
 
 constexpr int64_t kMaxVocab = INT32_MAX;          // rows of a table
-constexpr int64_t kMaxTokens = int64_t(1) << 30;  // of one embedding gradient
+constexpr int64_t kMaxTokens = int64_t(1) << 30;  // of one embedding gradient, rows of logits
 
 struct EmbedArgs {
     const void *table;
