@@ -1120,7 +1120,8 @@ def embed_grad(grad, tokens, vocab: int, scale: float = 1.0, out=None, accumulat
     (float32 unless given) is scale times the sum of the rows of grad [..., d]
     whose token is v, in the tokens' order, so that equal inputs give equal
     bits.  Rows without a token are zeroed; with accumulate the sums are added
-    to what out holds, and those rows are left alone."""
+    to what out holds, and those rows are left alone.  (An expanded grad, as a
+    mean over positions sends back, holds no rows: hand in grad.contiguous().)"""
     at, n, d, ld, code, index = _place("grad", grad)
     ids, wide = _token_place(tokens, n, index)
     if out is None:

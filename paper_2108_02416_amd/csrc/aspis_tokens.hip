@@ -663,7 +663,8 @@ __global__ __launch_bounds__(kBlock) void join_pieces_kernel(SumArgs g, int64_t 
 // rows' tokens out of all of them, sorts those few, and its waves share them
 // evenly; sums of a segment that several waves hold are joined in LDS, in
 // order.  Latency bounds it, in one launch instead of three: 515 tokens of 257
-// f32 into 4,099 rows in 9.1 us, 15.0 by sorting all.
+// f32 into 4,099 rows in 9.1 us, 15.0 by sorting all.  (Columns after the last
+// vector take workgroups of their own: at 257, half of them.)
 constexpr int kFewRows = 64;   // of a workgroup, at most
 
 struct FewArgs {
